@@ -417,6 +417,66 @@ int lss_linear_bwd_input_gelu(const void *dc, const void *w, const void *u,
 int lss_gelu_fwd(const void *u, int64_t n, void *g, void *stream);
 int lss_gelu_bwd(const void *u, const void *dg, int64_t n, void *du, void *stream);
 
+/*
+ * Answering with a trained model: prompts of different lengths run together, and what is kept of them for the tokens that
+ * follow.  Keys and values may have fewer heads than queries (H a multiple of H_kv; query head h reads head h / (H / H_kv)).
+ * Rows of a tensor [rows, heads, d] lie `*_stride` elements apart (heads * d where it is contiguous, more for a slice of a wider product; a
+ * multiple of 16 bytes), the heads of a row one behind the other.  elem_bytes 2: bf16, 4: float.  int32 arrays are DEVICE memory, read when the
+ * kernels run: a captured call follows them.  Whatever they hold, nothing outside the tensors is read or written.
+ *
+ * The cache: k_cache, v_cache [n_pages, page_size, H_kv, d] contiguous; block_table [B, max_pages] int32: token p of sequence b lies in
+ * page block_table[b, p / page_size], slot p % page_size.  Sequences may share pages.  A number outside [0, n_pages) is no page: nothing
+ * is written there and its tokens are seen by nobody.  page_size a power of two from 16 to 65536, max_pages * page_size <= 2^30, pages of at most 2^29
+ * elements (LSS_ERR_SHAPE otherwise).
+ *
+ * lss_paged_append puts new tokens into the cache, keys rotated by their positions on the way:
+ *     rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 of k and v are the last n_b tokens of sequence b, which has lengths[b] with them: row t has
+ *     position p = lengths[b] - n_b + (t - cu_seqlens[b]);
+ *     (x_i, y_i) -> (x_i cos a - y_i sin a, x_i sin a + y_i cos a),  a = p * inv_freq[i],  of every head of k, and of q where it is given.
+ *   cu_seqlens   [B + 1] int32, ascending; NULL: row b is the last token of sequence b, rows = B
+ *   inv_freq     [rot_dim / 2] double, radians per position; rot_dim a multiple of 16, at most d; 0: no rotation.  Columns rot_dim .. d - 1 stay
+ *                as they are.  x_i, y_i: columns i and i + rot_dim / 2 of a head, with `interleaved` 2 i and 2 i + 1
+ *   q, q_rot     [rows, H, d]; both or neither NULL.  q_rot contiguous (written), may be q where that is contiguous
+ *   k_rot        NULL or [rows, H_kv, d] contiguous (written): the keys as they went into the cache; may be k where that is contiguous
+ * The angle is taken in 64 bits, its cosine and sine and the products in 32, rounded to the tensors' type once.  Rows before cu_seqlens[0]
+ * and from cu_seqlens[B] on are not touched.  A row whose position is negative or past its table goes into no cache.  Two rows that go to one place
+ * (pages that are shared and written) leave either.  Uses no workspace.
+ */
+int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
+                     const int32_t *cu_seqlens, const int32_t *lengths, const int32_t *block_table,
+                     int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes,
+                     int64_t n_pages, int64_t page_size, int64_t max_pages,
+                     const double *inv_freq, int64_t rot_dim, int interleaved,
+                     void *k_cache, void *v_cache, void *q_rot, void *k_rot, void *stream);
+
+/*
+ * Attention of one token per sequence over its pages:
+ *     out[b, h] = softmax_j(q[b, h] . K_j / sqrt(d)) V_j  over the tokens j < lengths[b] of sequence b
+ *   q     [B, H, d];  out [B, H, d] contiguous (written);  lse [B, H] float (written)
+ *   lengths  [B] int32, the tokens of each sequence, the new one among them.  A sequence without tokens gives zeros and lse = -infinity
+ *   max_len  bound on the lengths, at most max_pages * page_size: a longer sequence counts as that long
+ * Arithmetic and accumulation in fp32.  What lies in a page behind a sequence's last token does not reach the result.
+ */
+int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
+                          const int32_t *lengths, const int32_t *block_table,
+                          int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes,
+                          int64_t n_pages, int64_t page_size, int64_t max_pages, int64_t max_len,
+                          void *out, float *lse, void *stream);
+
+/*
+ * Attention within each of B sequences that are packed one behind the other:
+ *   q     [rows_q, H, d]; rows cu_q[b] .. cu_q[b + 1] - 1 are sequence b's n_q;  k, v [rows_k, H_kv, d], its n_k by cu_k likewise
+ *   cu_q, cu_k  [B + 1] int32, ascending; cu_k may be cu_q
+ *   out   [rows_q, H, d] contiguous (written);  lse [H, rows_q] float (written)
+ * With causal != 0 a sequence's rows stand at the end of its keys: row r sees keys j <= n_k - n_q + r (all rows of a prompt: n_k = n_q; rows that
+ * continue one whose keys are there: n_k > n_q).  A row that sees no key gives zeros and lse = -infinity.  Rows of out and lse that belong to no
+ * sequence are not touched.  A key that a row does not see does not reach its result, whatever its value.  Uses no workspace.
+ */
+int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                        const int32_t *cu_q, const int32_t *cu_k, int64_t rows_q, int64_t rows_k,
+                        int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes, int causal,
+                        void *out, float *lse, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

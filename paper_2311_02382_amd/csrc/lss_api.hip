@@ -784,6 +784,138 @@ int lss_reduce_partials(const float *const *parts, int n, const int64_t *rows_va
     return LSS_OK;
 }
 
+// ---- the paged cache and packed sequences
+static int check_heads(const char *what, int64_t H, int64_t H_kv, int64_t d, int elem_bytes)
+{
+    if (d != 64 && d != 128) return fail(LSS_ERR_UNSUPPORTED_D, "%s: d = %lld: only 64 and 128 are supported", what, (long long)d);
+    if (elem_bytes != 2 && elem_bytes != 4) return fail(LSS_ERR_SHAPE, "%s: elem_bytes = %d: 2 (bf16) or 4 (float)", what, elem_bytes);
+    if (H_kv < 1 || H < 1 || H > 65535 || H_kv > 65535) return fail(LSS_ERR_SHAPE, "%s: bad shape: H=%lld H_kv=%lld", what, (long long)H, (long long)H_kv);
+    return LSS_OK;
+}
+static int check_groups(const char *what, int64_t H, int64_t H_kv)
+{
+    if (H % H_kv != 0) return fail(LSS_ERR_SHAPE, "%s: H = %lld is not a multiple of H_kv = %lld", what, (long long)H, (long long)H_kv);
+    return LSS_OK;
+}
+// rows of `heads` heads, `stride` elements apart: 16-byte aligned, none over the next, byte offsets far from 2^63
+static int check_rows(const char *what, const char *name, int64_t rows, int64_t stride, int64_t heads, int64_t d, int elem_bytes)
+{
+    if (rows < 0 || rows > (int64_t)1 << 30) return fail(LSS_ERR_SHAPE, "%s: %lld rows of %s (0 .. 2^30)", what, (long long)rows, name);
+    if (stride < heads * d || stride > (int64_t)1 << 30) return fail(LSS_ERR_SHAPE, "%s: rows of %s are %lld elements apart (at least %lld, at most 2^30)", what, name, (long long)stride, (long long)(heads * d));
+    if (stride * elem_bytes % 16 != 0) return fail(LSS_ERR_ALIGN, "%s: rows of %s must be 16-byte aligned", what, name);
+    return LSS_OK;
+}
+static bool off_by(const void *p, size_t alignment) { return reinterpret_cast<uintptr_t>(p) % alignment != 0; }
+static int check_arrays(const char *what, std::initializer_list<const void *> words, const void *doubles = nullptr)
+{
+    for (const void *p : words)
+        if (off_by(p, 4)) return fail(LSS_ERR_ALIGN, "%s: int32 arrays and lse must be 4-byte aligned", what);
+    if (off_by(doubles, 8)) return fail(LSS_ERR_ALIGN, "%s: inv_freq must be 8-byte aligned", what);
+    return LSS_OK;
+}
+static int check_cache(const char *what, int64_t B, int64_t H_kv, int64_t d, int64_t n_pages, int64_t page_size, int64_t max_pages, const int32_t *table,
+                       lss::PageTable *pt)
+{
+    if (B < 0 || B > (int64_t)1 << 24) return fail(LSS_ERR_SHAPE, "%s: B = %lld (0 .. 2^24)", what, (long long)B);
+    if (page_size < 16 || page_size > 65536 || (page_size & (page_size - 1)) != 0)
+        return fail(LSS_ERR_SHAPE, "%s: page_size = %lld (a power of two from 16 to 65536)", what, (long long)page_size);
+    if (n_pages < 1 || n_pages > INT32_MAX) return fail(LSS_ERR_SHAPE, "%s: n_pages = %lld (1 .. 2^31 - 1)", what, (long long)n_pages);
+    if (max_pages < 1 || max_pages * page_size > (int64_t)1 << 30 || max_pages > (int64_t)1 << 30)
+        return fail(LSS_ERR_SHAPE, "%s: max_pages = %lld (at least 1, tables of at most 2^30 tokens)", what, (long long)max_pages);
+    if (H_kv * d * page_size > (int64_t)1 << 29)
+        return fail(LSS_ERR_SHAPE, "%s: pages of %lld elements (at most 2^29)", what, (long long)(H_kv * d * page_size));
+    *pt = {table, (int)n_pages, 63 - __builtin_clzll((unsigned long long)page_size), (int)max_pages};
+    return LSS_OK;
+}
+
+int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride, const int32_t *cu_seqlens,
+                     const int32_t *lengths, const int32_t *block_table, int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes,
+                     int64_t n_pages, int64_t page_size, int64_t max_pages, const double *inv_freq, int64_t rot_dim, int interleaved, void *k_cache,
+                     void *v_cache, void *q_rot, void *k_rot, void *stream)
+{
+    const char *what = "paged_append";
+    lss::PageTable pt;
+    if (int rc = check_heads(what, q ? H : 1, H_kv, d, elem_bytes)) return rc;
+    if (int rc = check_cache(what, B, H_kv, d, n_pages, page_size, max_pages, block_table, &pt)) return rc;
+    if (int rc = check_rows(what, "k", rows, k_stride, H_kv, d, elem_bytes)) return rc;
+    if (int rc = check_rows(what, "v", rows, v_stride, H_kv, d, elem_bytes)) return rc;
+    if (q)
+        if (int rc = check_rows(what, "q", rows, q_stride, H, d, elem_bytes)) return rc;
+    if (rot_dim < 0 || rot_dim > d || rot_dim % 16 != 0) return fail(LSS_ERR_SHAPE, "%s: rot_dim = %lld (a multiple of 16, at most d)", what, (long long)rot_dim);
+    if (rows == 0 || B == 0) return LSS_OK;
+    if (!k || !v || !k_cache || !v_cache || !lengths || !block_table || (rot_dim > 0 && !inv_freq) || (q != nullptr) != (q_rot != nullptr))
+        return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
+    if (misaligned(k) || misaligned(v) || misaligned(q) || misaligned(k_cache) || misaligned(v_cache) || misaligned(q_rot) || misaligned(k_rot))
+        return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
+    if (int rc = check_arrays(what, {cu_seqlens, lengths, block_table}, inv_freq)) return rc;
+    const lss::AppendArgs a{pt, cu_seqlens, lengths, inv_freq, k_stride, v_stride, q_stride, (int)rows, (int)B, (int)H, (int)H_kv, (int)d, (int)rot_dim,
+                            interleaved ? 1 : 0, 0};
+    const auto go = [&](auto zero) {
+        typedef decltype(zero) T;
+        return lss::launch_paged_append<T>(a, static_cast<const T *>(k), static_cast<const T *>(v), static_cast<const T *>(q), static_cast<T *>(k_cache),
+                                           static_cast<T *>(v_cache), static_cast<T *>(q_rot), static_cast<T *>(k_rot), static_cast<hipStream_t>(stream));
+    };
+    const hipError_t e = elem_bytes == 2 ? go(lss::bf16_t{}) : go(float{});
+    if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));
+    return LSS_OK;
+}
+
+int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache, const int32_t *lengths, const int32_t *block_table,
+                          int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes, int64_t n_pages, int64_t page_size, int64_t max_pages,
+                          int64_t max_len, void *out, float *lse, void *stream)
+{
+    const char *what = "paged_attn_decode";
+    lss::PageTable pt;
+    if (int rc = check_heads(what, H, H_kv, d, elem_bytes)) return rc;
+    if (int rc = check_groups(what, H, H_kv)) return rc;
+    if (int rc = check_cache(what, B, H_kv, d, n_pages, page_size, max_pages, block_table, &pt)) return rc;
+    if (int rc = check_rows(what, "q", B, q_stride, H, d, elem_bytes)) return rc;
+    if (max_len < 0 || max_len > max_pages * page_size)
+        return fail(LSS_ERR_RANGE, "%s: max_len = %lld, the tables hold %lld tokens", what, (long long)max_len, (long long)(max_pages * page_size));
+    if (B * H > (int64_t)1 << 24) return fail(LSS_ERR_SHAPE, "%s: B*H = %lld exceeds 2^24", what, (long long)(B * H));
+    if (B == 0) return LSS_OK;
+    if (!q || !k_cache || !v_cache || !lengths || !block_table || !out || !lse) return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
+    if (misaligned(q) || misaligned(k_cache) || misaligned(v_cache) || misaligned(out))
+        return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
+    if (int rc = check_arrays(what, {lengths, block_table, lse})) return rc;
+    const lss::DecodeArgs a{pt, lengths, q_stride, (int)B, (int)H, (int)H_kv, (int)d, (int)max_len};
+    const auto go = [&](auto zero) {
+        typedef decltype(zero) T;
+        return lss::launch_paged_decode<T>(a, static_cast<const T *>(q), static_cast<const T *>(k_cache), static_cast<const T *>(v_cache),
+                                           static_cast<T *>(out), lse, static_cast<hipStream_t>(stream));
+    };
+    const hipError_t e = elem_bytes == 2 ? go(lss::bf16_t{}) : go(float{});
+    if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));
+    return LSS_OK;
+}
+
+int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *cu_q,
+                        const int32_t *cu_k, int64_t rows_q, int64_t rows_k, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes, int causal,
+                        void *out, float *lse, void *stream)
+{
+    const char *what = "packed_attn_fwd";
+    if (int rc = check_heads(what, H, H_kv, d, elem_bytes)) return rc;
+    if (int rc = check_groups(what, H, H_kv)) return rc;
+    if (B < 0 || B > (int64_t)1 << 24) return fail(LSS_ERR_SHAPE, "%s: B = %lld (0 .. 2^24)", what, (long long)B);
+    if (int rc = check_rows(what, "q", rows_q, q_stride, H, d, elem_bytes)) return rc;
+    if (int rc = check_rows(what, "k", rows_k, k_stride, H_kv, d, elem_bytes)) return rc;
+    if (int rc = check_rows(what, "v", rows_k, v_stride, H_kv, d, elem_bytes)) return rc;
+    if (B == 0 || rows_q == 0) return LSS_OK;
+    if (!q || !cu_q || !cu_k || !out || !lse || (rows_k > 0 && (!k || !v))) return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
+    if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out))
+        return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
+    if (int rc = check_arrays(what, {cu_q, cu_k, lse})) return rc;
+    const lss::PackedArgs a{cu_q, cu_k, q_stride, k_stride, v_stride, (int)rows_q, (int)rows_k, (int)B, (int)H, (int)H_kv, (int)d, causal ? 1 : 0};
+    const auto go = [&](auto zero) {
+        typedef decltype(zero) T;
+        return lss::launch_packed_attn<T>(a, static_cast<const T *>(q), static_cast<const T *>(k), static_cast<const T *>(v), static_cast<T *>(out), lse,
+                                          static_cast<hipStream_t>(stream));
+    };
+    const hipError_t e = elem_bytes == 2 ? go(lss::bf16_t{}) : go(float{});
+    if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));
+    return LSS_OK;
+}
+
 // ---- lss_plan.h
 static int plan_shape(int64_t s0, int64_t l_s, int64_t l_x, int64_t B, int64_t H, int64_t d, int causal, int elem_bytes, const int *plan, lss::SegShape *s)
 {

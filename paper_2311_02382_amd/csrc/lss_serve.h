@@ -1,0 +1,101 @@
+// What the kernels of the paged cache and of packed sequences share: which sequence a row belongs to, where a token lies in
+// the cache, and the attention of one row by one wavefront.
+#pragma once
+#include "lss_common.h"
+#include "lss_kernels.h"
+
+namespace lss {
+
+// The sequence of packed row t: the last b in [0, B) with cu[b] <= t, if t < cu[b + 1] too, else -1.  By the whole wavefront, 64 starts at a
+// time: as many dependent loads as B has digits to the base 64.  (cu ascending; whatever it holds, only its B + 1 entries are read.)
+__device__ __forceinline__ int find_sequence(const int32_t *__restrict__ cu, int B, int t, int lane, int &begin, int &end)
+{
+    int lo = 0, n = B + 1;
+    while (n > 1) {
+        const int step = (n + 63) / 64, at = lane * step;
+        const uint64_t below = __ballot(at < n && cu[lo + min(at, n - 1)] <= t);
+        if (below == 0) return -1;
+        const int last = 63 - __clzll((long long)below);
+        lo += last * step;
+        n = min(step, n - last * step);
+    }
+    if (lo >= B) return -1;
+    begin = cu[lo];
+    end = cu[lo + 1];
+    return begin <= t && t < end ? lo : -1;
+}
+
+// Index of the cache row that holds token `position` of sequence b, in units of H_kv * d elements; -1 where the table names no page.
+__device__ __forceinline__ int64_t cache_row(const PageTable &pt, int b, int position)
+{
+    const int nth = position >> pt.page_shift;
+    if (position < 0 || nth >= pt.max_pages) return -1;
+    const int page = pt.table[(int64_t)b * pt.max_pages + nth];
+    if ((uint32_t)page >= (uint32_t)pt.n_pages) return -1;
+    return ((int64_t)page << pt.page_shift) + (position & ((1 << pt.page_shift) - 1));
+}
+
+template <typename T> struct Vec16;
+template <> struct Vec16<bf16_t> { typedef bf16x8 type; };
+template <> struct Vec16<float> { typedef f32x4 type; };
+
+__device__ __forceinline__ float wave_max(float x)
+{
+#pragma unroll
+    for (int sh = 32; sh >= 1; sh >>= 1) x = fmaxf(x, __shfl_xor(x, sh));
+    return x;
+}
+__device__ __forceinline__ float wave_total(float x)
+{
+#pragma unroll
+    for (int sh = 32; sh >= 1; sh >>= 1) x += __shfl_xor(x, sh);
+    return x;
+}
+
+// Attention of one query row against n_keys keys by one wavefront: lanes own keys for the scores and columns lane, lane + 64, ..
+// for the sum of the values, everything in fp32.  row_of(j): key j's row in k and v, or -1 for a key that is not there.  A
+// value is multiplied only where its key is seen, so that what lies in other rows cannot reach the result.
+template <typename T, int D, typename F>
+__device__ void row_attention(const T *q, const T *k, int64_t k_stride, const T *v, int64_t v_stride, int n_keys, int lane, F row_of, T *out,
+                              float *lse)
+{
+    typedef typename Vec16<T>::type Vec;
+    constexpr int VEC = 16 / sizeof(T);
+    const float c = kLog2e / sqrtf((float)D);
+    float acc[D / 64], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) acc[i] = 0.f;
+    for (int j0 = 0; j0 < n_keys; j0 += 64) {
+        const int64_t row = j0 + lane < n_keys ? row_of(j0 + lane) : -1;
+        float s = -INFINITY;
+        if (row >= 0) {
+            s = 0.f;
+#pragma unroll
+            for (int i = 0; i < D; i += VEC) {
+                const Vec a = *reinterpret_cast<const Vec *>(q + i), b = *reinterpret_cast<const Vec *>(k + row * k_stride + i);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s = fmaf((float)a[e], (float)b[e], s);
+            }
+        }
+        s *= c;
+        const float m_new = fmaxf(m, wave_max(s)), m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = fast_exp2(m - m_use), p = row >= 0 ? fast_exp2(s - m_use) : 0.f;
+        m = m_new;
+        l = l * alpha + wave_total(p);
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) acc[i] *= alpha;
+        for (int j = 0; j < min(64, n_keys - j0); ++j) {
+            const int64_t at = __shfl(row, j);
+            const float w = __shfl(p, j);
+            if (at < 0) continue;
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) acc[i] = fmaf(w, (float)v[at * v_stride + lane + 64 * i], acc[i]);
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;         // no key: zeros and -infinity
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) out[lane + 64 * i] = (T)(acc[i] * inv);
+    if (lane == 0) *lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+} // namespace lss

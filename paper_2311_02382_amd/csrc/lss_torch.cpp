@@ -499,6 +499,109 @@ PyObject *gelu_bwd(PyObject *const *p)
     invoke(lss_gelu_bwd, ptr(u), ptr(dg), u.numel(), ptr(du), stream_of(p[3]));
     return give(p[2], du);
 }
+
+// ------------------------------------------------------------------------------------ paged cache, packed sequences
+// Every tensor on the GPU that is current, whose stream the call runs on
+void on_current_gpu(std::initializer_list<const at::Tensor *> all)
+{
+    const auto index = c10::hip::getCurrentHIPStream().device_index();
+    for (const at::Tensor *t : all)
+        if (t->defined()) require(t->is_cuda() && t->device().index() == index, "tensors must be on the current GPU");
+}
+// [rows, heads, d] with the columns and heads of a row one behind the other; rows may lie apart (a slice of a wider product)
+struct Rows { int64_t rows, heads, d, stride; };
+Rows head_rows(const at::Tensor &t, const char *what)
+{
+    if (t.dim() != 3 || (t.scalar_type() != kBf16 && t.scalar_type() != kF32)) throw ValueError(std::string(what) + " must be a bfloat16 or float32 tensor [rows, heads, d]");
+    const Rows r{t.size(0), t.size(1), t.size(2), t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2)};
+    if ((r.d > 1 && t.stride(2) != 1) || (r.heads > 1 && t.stride(1) != r.d)) throw ValueError(std::string("the heads of a row of ") + what + " must be contiguous");
+    return r;
+}
+void int32_array(const at::Tensor &t, int64_t dims, const char *what)
+{
+    if (t.dim() != dims || t.scalar_type() != at::kInt || !on_gpu(t)) throw ValueError(std::string(what) + " must be a contiguous torch.int32 device tensor of " + std::to_string(dims) + (dims == 1 ? " dimension" : " dimensions"));
+}
+struct Cache { int64_t n_pages, page_size, H_kv, d, B, max_pages; int eb; at::ScalarType dt; };
+Cache cache_of(const at::Tensor &k, const at::Tensor &v, const at::Tensor &table, const at::Tensor &lengths)
+{
+    require(k.dim() == 4 && k.sizes() == v.sizes() && on_gpu(k) && on_gpu(v) && k.scalar_type() == v.scalar_type() &&
+                (k.scalar_type() == kBf16 || k.scalar_type() == kF32),
+            "k_cache and v_cache must be contiguous bfloat16 or float32 device tensors [n_pages, page_size, H_kv, d] of one shape and dtype");
+    int32_array(table, 2, "block_table");
+    int32_array(lengths, 1, "lengths");
+    require(lengths.size(0) == table.size(0), "lengths and block_table disagree on the number of sequences");
+    return {k.size(0), k.size(1), k.size(2), k.size(3), table.size(0), table.size(1), k.scalar_type() == kF32 ? 4 : 2, k.scalar_type()};
+}
+// k v k_cache v_cache block_table lengths cu_seqlens q inv_freq interleaved q_rot k_rot stream
+PyObject *paged_append(PyObject *const *a)
+{
+    const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &kc = tensor(a[2]), &vc = tensor(a[3]), &table = tensor(a[4]), &lengths = tensor(a[5]);
+    const Cache m = cache_of(kc, vc, table, lengths);
+    const Rows rk = head_rows(k, "k"), rv = head_rows(v, "v");
+    require(k.scalar_type() == m.dt && v.scalar_type() == m.dt && rk.heads == m.H_kv && rk.d == m.d && k.sizes() == v.sizes(),
+            "k and v must be [rows, H_kv, d] in the cache's dtype");
+    at::Tensor cu, q, freq, q_rot, k_rot;
+    if (none(a[6])) require(rk.rows == m.B, "without cu_seqlens there is one row for every sequence");
+    else {
+        cu = tensor(a[6]);
+        int32_array(cu, 1, "cu_seqlens");
+        require(cu.size(0) == m.B + 1, "cu_seqlens must have one entry more than there are sequences");
+    }
+    Rows rq{0, 1, 0, 0};
+    if (!none(a[7])) {
+        q = tensor(a[7]);
+        rq = head_rows(q, "q");
+        require(q.scalar_type() == m.dt && rq.rows == rk.rows && rq.d == m.d, "q must be [rows, H, d] in the cache's dtype");
+        q_rot = output(a[10], q.sizes(), m.dt, q);
+    } else require(none(a[10]), "q_rot without q");
+    if (!none(a[8])) {
+        freq = tensor(a[8]);
+        require(freq.dim() == 1 && freq.scalar_type() == at::kDouble && on_gpu(freq), "inv_freq must be a contiguous torch.float64 device tensor of 1 dimension");
+    }
+    if (!none(a[11])) k_rot = output(a[11], k.sizes(), m.dt, k);
+    on_current_gpu({&k, &v, &kc, &vc, &table, &lengths, &cu, &q, &freq, &q_rot, &k_rot});
+    const auto ints = [](const at::Tensor &t) { return t.defined() ? static_cast<const int32_t *>(t.data_ptr()) : nullptr; };
+    const auto any = [](const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+    invoke(lss_paged_append, ptr(k), rk.stride, ptr(v), rv.stride, any(q), rq.stride, ints(cu), ints(lengths), ints(table), rk.rows, m.B, rq.heads,
+           m.H_kv, m.d, m.eb, m.n_pages, m.page_size, m.max_pages, freq.defined() ? static_cast<const double *>(freq.data_ptr()) : nullptr,
+           freq.defined() ? 2 * freq.size(0) : 0, truth(a[9]), ptr(kc), ptr(vc), any(q_rot), any(k_rot), stream_of(a[12]));
+    const auto result = [](PyObject *passed, const at::Tensor &t) -> PyObject * {
+        if (t.defined()) return give(passed, t);
+        Py_RETURN_NONE;
+    };
+    return pack({result(a[10], q_rot), result(a[11], k_rot)});
+}
+// q k_cache v_cache block_table lengths max_len out lse stream
+PyObject *paged_attn_decode(PyObject *const *a)
+{
+    const at::Tensor &q = tensor(a[0]), &kc = tensor(a[1]), &vc = tensor(a[2]), &table = tensor(a[3]), &lengths = tensor(a[4]);
+    const Cache m = cache_of(kc, vc, table, lengths);
+    const Rows rq = head_rows(q, "q");
+    require(q.scalar_type() == m.dt && rq.rows == m.B && rq.d == m.d, "q must be [B, H, d] in the cache's dtype");
+    const int64_t max_len = none(a[5]) ? m.max_pages * m.page_size : integer(a[5]);
+    const at::Tensor out = output(a[6], q.sizes(), m.dt, q), lse = output(a[7], {m.B, rq.heads}, kF32, q);
+    on_current_gpu({&q, &kc, &vc, &table, &lengths, &out, &lse});
+    invoke(lss_paged_attn_decode, ptr(q), rq.stride, ptr(kc), ptr(vc), static_cast<const int32_t *>(ptr(lengths)), static_cast<const int32_t *>(ptr(table)), m.B,
+           rq.heads, m.H_kv, m.d, m.eb, m.n_pages, m.page_size, m.max_pages, max_len, ptr(out), fptr(lse), stream_of(a[8]));
+    return pack({give(a[6], out), give(a[7], lse)});
+}
+// q k v cu_q cu_k causal out lse stream
+PyObject *packed_attn_fwd(PyObject *const *a)
+{
+    const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]), &cu_q = tensor(a[3]), &cu_k = none(a[4]) ? cu_q : tensor(a[4]);
+    const Rows rq = head_rows(q, "q"), rk = head_rows(k, "k"), rv = head_rows(v, "v");
+    require(k.sizes() == v.sizes() && rk.d == rq.d && k.scalar_type() == q.scalar_type() && v.scalar_type() == q.scalar_type(),
+            "k and v must be [rows, H_kv, d] of one shape, with q's d and dtype");
+    int32_array(cu_q, 1, "cu_q");
+    int32_array(cu_k, 1, "cu_k");
+    require(cu_q.size(0) >= 1 && cu_q.size(0) == cu_k.size(0), "cu_q and cu_k must have one entry more than there are sequences");
+    const at::Tensor out = output(a[6], q.sizes(), q.scalar_type(), q), lse = output(a[7], {rq.heads, rq.rows}, kF32, q);
+    on_current_gpu({&q, &k, &v, &cu_q, &cu_k, &out, &lse});
+    invoke(lss_packed_attn_fwd, ptr(q), rq.stride, ptr(k), rk.stride, ptr(v), rv.stride, static_cast<const int32_t *>(ptr(cu_q)),
+           static_cast<const int32_t *>(ptr(cu_k)), rq.rows, rk.rows, cu_q.size(0) - 1, rq.heads, rk.heads, rq.d, q.scalar_type() == kF32 ? 4 : 2, truth(a[5]),
+           ptr(out), fptr(lse), stream_of(a[8]));
+    return pack({give(a[6], out), give(a[7], lse)});
+}
 PyObject *set_error_type(PyObject *const *p)
 {
     Py_INCREF(p[0]);
@@ -531,7 +634,8 @@ PyMethodDef g_methods[] = {
     LSS_FN(project_bwd, 10), LSS_FN(project_bwd_weight, 10), LSS_FN(embed_pe_fwd, 5), LSS_FN(embed_pe_bwd, 3),
     LSS_FN(residual_dropout_add, 7), LSS_FN(layernorm_fwd, 8), LSS_FN(layernorm_bwd, 10), LSS_FN(linear_fwd, 4),
     LSS_FN(linear_bwd_input, 4), LSS_FN(linear_bwd_weight, 5), LSS_FN(linear_gelu_fwd, 5), LSS_FN(linear_bwd_input_gelu, 5),
-    LSS_FN(gelu_fwd, 3), LSS_FN(gelu_bwd, 4), LSS_FN(set_error_type, 1), {nullptr, nullptr, 0, nullptr}};
+    LSS_FN(gelu_fwd, 3), LSS_FN(gelu_bwd, 4), LSS_FN(paged_append, 13), LSS_FN(paged_attn_decode, 9),
+    LSS_FN(packed_attn_fwd, 9), LSS_FN(set_error_type, 1), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_lss_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace

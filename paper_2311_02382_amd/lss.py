@@ -32,7 +32,7 @@ EXPORTS = ["lss_version", "lss_last_error", "lss_workspace_bytes", "lss_set_work
            "lss_embed_pe_fwd", "lss_embed_pe_bwd", "lss_residual_dropout_add", "lss_layernorm_fwd", "lss_layernorm_bwd_scratch_bytes",
            "lss_layernorm_bwd", "lss_linear_fwd", "lss_linear_bwd_input", "lss_linear_bwd_weight_scratch_bytes", "lss_linear_bwd_weight",
            "lss_linear_gelu_fwd",
-           "lss_linear_bwd_input_gelu", "lss_gelu_fwd", "lss_gelu_bwd"]
+           "lss_linear_bwd_input_gelu", "lss_gelu_fwd", "lss_gelu_bwd", "lss_paged_append", "lss_paged_attn_decode", "lss_packed_attn_fwd"]
 
 LSS_FLAG_SKIP_MASKED_TAIL = 1
 
@@ -108,6 +108,11 @@ def load():
     lib.lss_linear_bwd_input_gelu.argtypes = [vp, vp, vp, i64, i64, i64, vp, vp]
     lib.lss_gelu_fwd.argtypes = [vp, i64, vp, vp]
     lib.lss_gelu_bwd.argtypes = [vp, vp, i64, vp, vp]
+    lib.lss_paged_append.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, i64, i64, ci, i64, i64, i64, vp, i64, ci, vp, vp, vp, vp, vp]
+    lib.lss_paged_attn_decode.argtypes = [vp, i64, vp, vp, vp, vp, i64, i64, i64, i64, ci, i64, i64, i64, i64, vp, vp, vp]
+    lib.lss_packed_attn_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i64, i64, ci, ci, vp, vp, vp]
+    for name in ("lss_paged_append", "lss_paged_attn_decode", "lss_packed_attn_fwd"):
+        getattr(lib, name).restype = ci
     for name in ("lss_embed_pe_fwd", "lss_embed_pe_bwd", "lss_residual_dropout_add", "lss_layernorm_fwd", "lss_layernorm_bwd", "lss_linear_fwd",
                  "lss_linear_bwd_input", "lss_linear_gelu_fwd", "lss_linear_bwd_input_gelu", "lss_gelu_fwd", "lss_gelu_bwd"):
         getattr(lib, name).restype = ci
@@ -293,3 +298,34 @@ def lss_gelu_fwd(u, g=None, stream=None):
 def lss_gelu_bwd(u, dg, du=None, stream=None):
     """du = dg * GeLU'(u), elementwise, bf16."""
     return (_native or _bind()).gelu_bwd(u, dg, du, stream)
+
+
+def lss_paged_append(k, v, k_cache, v_cache, block_table, lengths, cu_seqlens=None, q=None, inv_freq=None, interleaved=False,
+                     q_rot=None, k_rot=None, stream=None):
+    """New tokens into a paged cache, keys (and queries) rotated by their positions on the way.
+
+    k, v [rows, H_kv, d]: rows cu_seqlens[b] .. cu_seqlens[b + 1] are the last tokens of sequence b, which has lengths[b] with
+    them (without cu_seqlens: row b is the last token of sequence b).  Caches [n_pages, page_size, H_kv, d], block_table
+    int32 [B, max_pages].  inv_freq float64 [rot_dim / 2]: radians per position of the pairs (i, i + rot_dim / 2), or with
+    `interleaved` (2 i, 2 i + 1), of every head of k and q; None: no rotation.  Rows may lie apart (stride of the first dimension).
+
+    Returns (q_rot, k_rot): the rotated q [rows, H, d] if q was given, and k_rot if it was passed (the keys as they went into the cache), else None.
+    """
+    return (_native or _bind()).paged_append(k, v, k_cache, v_cache, block_table, lengths, cu_seqlens, q, inv_freq, interleaved, q_rot, k_rot, stream)
+
+
+def lss_paged_attn_decode(q, k_cache, v_cache, block_table, lengths, max_len=None, out=None, lse=None, stream=None):
+    """Attention of one token per sequence, q [B, H, d], over the first lengths[b] tokens of its pages; H a multiple of H_kv.
+
+    max_len: a bound on the lengths (a longer sequence counts as that long); None: what the tables hold.
+    Returns (out [B, H, d] in q's dtype, lse [B, H] float32)."""
+    return (_native or _bind()).paged_attn_decode(q, k_cache, v_cache, block_table, lengths, max_len, out, lse, stream)
+
+
+def lss_packed_attn_fwd(q, k, v, cu_q, cu_k=None, causal=True, out=None, lse=None, stream=None):
+    """Attention within each of the sequences that are packed one behind the other: q [rows, H, d] with starts cu_q int32 [B + 1],
+    k, v [rows, H_kv, d] with starts cu_k (None: cu_q), H a multiple of H_kv.  With `causal` the rows of a sequence stand at the end of
+    its keys: row r of n_q sees keys up to n_k - n_q + r.
+
+    Returns (out [rows, H, d] in q's dtype, lse [H, rows] float32)."""
+    return (_native or _bind()).packed_attn_fwd(q, k, v, cu_q, cu_k, causal, out, lse, stream)
