@@ -455,13 +455,16 @@ int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_s
  *   q     [B, H, d];  out [B, H, d] contiguous (written);  lse [B, H] float (written)
  *   lengths  [B] int32, the tokens of each sequence, the new one among them.  A sequence without tokens gives zeros and lse = -infinity
  *   max_len  bound on the lengths, at most max_pages * page_size: a longer sequence counts as that long
+ *   workspace  DEVICE buffer of lss_paged_attn_workspace_bytes(H, H_kv, d, max_len) bytes (0 where max_len is small), 16-byte aligned;
+ *            NULL: the one registered with lss_set_workspace().  Calls that overlap in time on one GPU need a buffer each
  * Arithmetic and accumulation in fp32.  What lies in a page behind a sequence's last token does not reach the result.
  */
+size_t lss_paged_attn_workspace_bytes(int64_t H, int64_t H_kv, int64_t d, int64_t max_len);
 int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
                           const int32_t *lengths, const int32_t *block_table,
                           int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes,
                           int64_t n_pages, int64_t page_size, int64_t max_pages, int64_t max_len,
-                          void *out, float *lse, void *stream);
+                          void *workspace, size_t workspace_bytes, void *out, float *lse, void *stream);
 
 /*
  * Attention within each of B sequences that are packed one behind the other:

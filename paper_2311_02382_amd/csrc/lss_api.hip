@@ -860,9 +860,33 @@ int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_s
     return LSS_OK;
 }
 
+// The scratch of a call that needs `need` bytes: the caller's own (`*base`, `bytes`) if given, else the one registered for the current GPU
+static int get_scratch(const char *what, size_t need, void **base, size_t bytes)
+{
+    const bool own = *base != nullptr;
+    if (need == 0) return LSS_OK;
+    if (!own) {
+        int dev = 0;
+        if (int rc = current_device(&dev)) return rc;
+        std::lock_guard<std::mutex> lock(g_ws_mutex);
+        *base = g_ws_ptr[dev];
+        bytes = g_ws_bytes[dev];
+    }
+    if (*base == nullptr || bytes < need)
+        return fail(LSS_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu %s", what, need, *base ? bytes : (size_t)0,
+                    own ? "passed" : "registered for this GPU (lss_set_workspace)");
+    return LSS_OK;
+}
+
+size_t lss_paged_attn_workspace_bytes(int64_t H, int64_t H_kv, int64_t d, int64_t max_len)
+{
+    if (H < 1 || H > 65535 || H_kv < 1 || H % H_kv != 0 || (d != 64 && d != 128) || max_len < 0 || max_len > (int64_t)1 << 30) return 0;
+    return lss::paged_decode_workspace_bytes((int)H, (int)H_kv, (int)d, (int)max_len);
+}
+
 int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache, const int32_t *lengths, const int32_t *block_table,
                           int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes, int64_t n_pages, int64_t page_size, int64_t max_pages,
-                          int64_t max_len, void *out, float *lse, void *stream)
+                          int64_t max_len, void *workspace, size_t workspace_bytes, void *out, float *lse, void *stream)
 {
     const char *what = "paged_attn_decode";
     lss::PageTable pt;
@@ -877,12 +901,14 @@ int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, 
     if (!q || !k_cache || !v_cache || !lengths || !block_table || !out || !lse) return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
     if (misaligned(q) || misaligned(k_cache) || misaligned(v_cache) || misaligned(out))
         return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
+    if (misaligned(workspace)) return fail(LSS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", what);
     if (int rc = check_arrays(what, {lengths, block_table, lse})) return rc;
+    if (int rc = get_scratch(what, lss::paged_decode_workspace_bytes((int)H, (int)H_kv, (int)d, (int)max_len), &workspace, workspace_bytes)) return rc;
     const lss::DecodeArgs a{pt, lengths, q_stride, (int)B, (int)H, (int)H_kv, (int)d, (int)max_len};
     const auto go = [&](auto zero) {
         typedef decltype(zero) T;
         return lss::launch_paged_decode<T>(a, static_cast<const T *>(q), static_cast<const T *>(k_cache), static_cast<const T *>(v_cache),
-                                           static_cast<T *>(out), lse, static_cast<hipStream_t>(stream));
+                                           static_cast<T *>(out), lse, static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
     };
     const hipError_t e = elem_bytes == 2 ? go(lss::bf16_t{}) : go(float{});
     if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));

@@ -1,4 +1,4 @@
-// A paged cache of keys and values: what puts new tokens into it and the attention of one token per sequence over it.
+// A paged cache of keys and values: what puts new tokens into it.
 //
 // Token `position` of sequence b lies in page table[b, position / page_size], slot position % page_size, of both caches,
 // [n_pages, page_size, H_kv, d] each.  A number outside [0, n_pages) is no page: nothing is written there and nobody sees its tokens.
@@ -97,20 +97,6 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(AppendArgs
     }
 }
 
-// ---- attention of one token per sequence: a wavefront per sequence and head
-template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_decode_kernel(DecodeArgs a, const T *__restrict__ q, const T *__restrict__ k_cache,
-                                                          const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse)
-{
-    const int lane = threadIdx.x & 63, item = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (item >= a.B * a.H) return;
-    const int b = item / a.H, h = item % a.H, h_kv = h / (a.H / a.H_kv);
-    const int n = max(0, min(a.lengths[b], a.max_len));
-    const int64_t ld = (int64_t)a.H_kv * D;
-    row_attention<T, D>(q + b * a.q_stride + (int64_t)h * D, k_cache + (int64_t)h_kv * D, ld, v_cache + (int64_t)h_kv * D, ld, n, lane,
-                        [&](int j) { return cache_row(a.pt, b, j); }, out + (int64_t)item * D, lse + item);
-}
-
 } // namespace
 
 template <typename T>
@@ -124,21 +110,9 @@ hipError_t launch_paged_append(const AppendArgs &args, const T *k, const T *v, c
     return hipGetLastError();
 }
 
-template <typename T>
-hipError_t launch_paged_decode(const DecodeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, hipStream_t st)
-{
-    const dim3 grid((unsigned)((a.B * a.H + 3) / 4)), block(256);
-    TimedLaunch tl(K_PAGED_DECODE, st);
-    if (a.d == 64) hipLaunchKernelGGL((paged_decode_kernel<T, 64>), grid, block, 0, st, a, q, k_cache, v_cache, out, lse);
-    else hipLaunchKernelGGL((paged_decode_kernel<T, 128>), grid, block, 0, st, a, q, k_cache, v_cache, out, lse);
-    return hipGetLastError();
-}
-
 template hipError_t launch_paged_append<bf16_t>(const AppendArgs &, const bf16_t *, const bf16_t *, const bf16_t *, bf16_t *, bf16_t *, bf16_t *, bf16_t *,
                                                 hipStream_t);
 template hipError_t launch_paged_append<float>(const AppendArgs &, const float *, const float *, const float *, float *, float *, float *, float *,
                                                hipStream_t);
-template hipError_t launch_paged_decode<bf16_t>(const DecodeArgs &, const bf16_t *, const bf16_t *, const bf16_t *, bf16_t *, float *, hipStream_t);
-template hipError_t launch_paged_decode<float>(const DecodeArgs &, const float *, const float *, const float *, float *, float *, hipStream_t);
 
 } // namespace lss

@@ -571,7 +571,7 @@ PyObject *paged_append(PyObject *const *a)
     };
     return pack({result(a[10], q_rot), result(a[11], k_rot)});
 }
-// q k_cache v_cache block_table lengths max_len out lse stream
+// q k_cache v_cache block_table lengths max_len out lse stream workspace
 PyObject *paged_attn_decode(PyObject *const *a)
 {
     const at::Tensor &q = tensor(a[0]), &kc = tensor(a[1]), &vc = tensor(a[2]), &table = tensor(a[3]), &lengths = tensor(a[4]);
@@ -581,8 +581,19 @@ PyObject *paged_attn_decode(PyObject *const *a)
     const int64_t max_len = none(a[5]) ? m.max_pages * m.page_size : integer(a[5]);
     const at::Tensor out = output(a[6], q.sizes(), m.dt, q), lse = output(a[7], {m.B, rq.heads}, kF32, q);
     on_current_gpu({&q, &kc, &vc, &table, &lengths, &out, &lse});
+    const size_t need = lss_paged_attn_workspace_bytes(rq.heads, m.H_kv, m.d, max_len);
+    size_t wn = 0;
+    void *wp = nullptr;
+    if (!none(a[9])) {
+        const at::Tensor &w = tensor(a[9]);
+        require(on_gpu(w), "workspace must be a contiguous device tensor");
+        on_current_gpu({&w});
+        wn = (size_t)w.numel() * w.element_size();
+        wp = ptr(w);
+        if (wn < need) throw ValueError("workspace of " + std::to_string(wn) + " bytes, need " + std::to_string(need));
+    } else if (need > 0) wp = shared_workspace(need, q, wn);
     invoke(lss_paged_attn_decode, ptr(q), rq.stride, ptr(kc), ptr(vc), static_cast<const int32_t *>(ptr(lengths)), static_cast<const int32_t *>(ptr(table)), m.B,
-           rq.heads, m.H_kv, m.d, m.eb, m.n_pages, m.page_size, m.max_pages, max_len, ptr(out), fptr(lse), stream_of(a[8]));
+           rq.heads, m.H_kv, m.d, m.eb, m.n_pages, m.page_size, m.max_pages, max_len, wp, wn, ptr(out), fptr(lse), stream_of(a[8]));
     return pack({give(a[6], out), give(a[7], lse)});
 }
 // q k v cu_q cu_k causal out lse stream
@@ -634,7 +645,7 @@ PyMethodDef g_methods[] = {
     LSS_FN(project_bwd, 10), LSS_FN(project_bwd_weight, 10), LSS_FN(embed_pe_fwd, 5), LSS_FN(embed_pe_bwd, 3),
     LSS_FN(residual_dropout_add, 7), LSS_FN(layernorm_fwd, 8), LSS_FN(layernorm_bwd, 10), LSS_FN(linear_fwd, 4),
     LSS_FN(linear_bwd_input, 4), LSS_FN(linear_bwd_weight, 5), LSS_FN(linear_gelu_fwd, 5), LSS_FN(linear_bwd_input_gelu, 5),
-    LSS_FN(gelu_fwd, 3), LSS_FN(gelu_bwd, 4), LSS_FN(paged_append, 13), LSS_FN(paged_attn_decode, 9),
+    LSS_FN(gelu_fwd, 3), LSS_FN(gelu_bwd, 4), LSS_FN(paged_append, 13), LSS_FN(paged_attn_decode, 10),
     LSS_FN(packed_attn_fwd, 9), LSS_FN(set_error_type, 1), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_lss_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

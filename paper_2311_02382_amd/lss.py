@@ -32,7 +32,8 @@ EXPORTS = ["lss_version", "lss_last_error", "lss_workspace_bytes", "lss_set_work
            "lss_embed_pe_fwd", "lss_embed_pe_bwd", "lss_residual_dropout_add", "lss_layernorm_fwd", "lss_layernorm_bwd_scratch_bytes",
            "lss_layernorm_bwd", "lss_linear_fwd", "lss_linear_bwd_input", "lss_linear_bwd_weight_scratch_bytes", "lss_linear_bwd_weight",
            "lss_linear_gelu_fwd",
-           "lss_linear_bwd_input_gelu", "lss_gelu_fwd", "lss_gelu_bwd", "lss_paged_append", "lss_paged_attn_decode", "lss_packed_attn_fwd"]
+           "lss_linear_bwd_input_gelu", "lss_gelu_fwd", "lss_gelu_bwd", "lss_paged_append", "lss_paged_attn_workspace_bytes", "lss_paged_attn_decode",
+           "lss_packed_attn_fwd"]
 
 LSS_FLAG_SKIP_MASKED_TAIL = 1
 
@@ -109,7 +110,9 @@ def load():
     lib.lss_gelu_fwd.argtypes = [vp, i64, vp, vp]
     lib.lss_gelu_bwd.argtypes = [vp, vp, i64, vp, vp]
     lib.lss_paged_append.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, i64, i64, ci, i64, i64, i64, vp, i64, ci, vp, vp, vp, vp, vp]
-    lib.lss_paged_attn_decode.argtypes = [vp, i64, vp, vp, vp, vp, i64, i64, i64, i64, ci, i64, i64, i64, i64, vp, vp, vp]
+    lib.lss_paged_attn_decode.argtypes = [vp, i64, vp, vp, vp, vp, i64, i64, i64, i64, ci, i64, i64, i64, i64, vp, sz, vp, vp, vp]
+    lib.lss_paged_attn_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.lss_paged_attn_workspace_bytes.restype = sz
     lib.lss_packed_attn_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i64, i64, ci, ci, vp, vp, vp]
     for name in ("lss_paged_append", "lss_paged_attn_decode", "lss_packed_attn_fwd"):
         getattr(lib, name).restype = ci
@@ -314,12 +317,17 @@ def lss_paged_append(k, v, k_cache, v_cache, block_table, lengths, cu_seqlens=No
     return (_native or _bind()).paged_append(k, v, k_cache, v_cache, block_table, lengths, cu_seqlens, q, inv_freq, interleaved, q_rot, k_rot, stream)
 
 
-def lss_paged_attn_decode(q, k_cache, v_cache, block_table, lengths, max_len=None, out=None, lse=None, stream=None):
+def lss_paged_attn_workspace_bytes(H, H_kv, d, max_len) -> int:
+    return int(load().lss_paged_attn_workspace_bytes(int(H), int(H_kv), int(d), int(max_len)))
+
+
+def lss_paged_attn_decode(q, k_cache, v_cache, block_table, lengths, max_len=None, out=None, lse=None, stream=None, workspace=None):
     """Attention of one token per sequence, q [B, H, d], over the first lengths[b] tokens of its pages; H a multiple of H_kv.
 
-    max_len: a bound on the lengths (a longer sequence counts as that long); None: what the tables hold.
+    max_len: a bound on the lengths (a longer sequence counts as that long); None: what the tables hold.  workspace: a device tensor of
+    lss_paged_attn_workspace_bytes() bytes used by this call alone; None: the binding's buffer of that GPU.
     Returns (out [B, H, d] in q's dtype, lse [B, H] float32)."""
-    return (_native or _bind()).paged_attn_decode(q, k_cache, v_cache, block_table, lengths, max_len, out, lse, stream)
+    return (_native or _bind()).paged_attn_decode(q, k_cache, v_cache, block_table, lengths, max_len, out, lse, stream, workspace)
 
 
 def lss_packed_attn_fwd(q, k, v, cu_q, cu_k=None, causal=True, out=None, lse=None, stream=None):

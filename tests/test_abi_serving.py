@@ -19,8 +19,8 @@ def _append(lib, k=0x1000, ks=128, v=0x2000, vs=128, q=0x3000, qs=256, cu=0x4004
 
 
 def _decode(lib, q=0x1000, qs=256, kc=0x2000, vc=0x3000, lengths=0x4004, table=0x5004, B=2, H=4, H_kv=2, d=64, eb=2, n_pages=8, page=16, max_pages=4,
-            max_len=64, out=0x6000, lse=0x7004):
-    return lib.lss_paged_attn_decode(q, qs, kc, vc, lengths, table, B, H, H_kv, d, eb, n_pages, page, max_pages, max_len, out, lse, None)
+            max_len=64, ws=0, wn=0, out=0x6000, lse=0x7004):
+    return lib.lss_paged_attn_decode(q, qs, kc, vc, lengths, table, B, H, H_kv, d, eb, n_pages, page, max_pages, max_len, ws, wn, out, lse, None)
 
 
 def _packed(lib, q=0x1000, qs=256, k=0x2000, ks=128, v=0x3000, vs=128, cu_q=0x4004, cu_k=0x5004, rows_q=5, rows_k=7, B=2, H=4, H_kv=2, d=64, eb=2,
@@ -47,8 +47,10 @@ def test_append(lib, change, code):
     (dict(n_pages=-1), -2), (dict(max_len=65), -5), (dict(max_len=-1), -5), (dict(qs=200), -2), (dict(qs=257), -4), (dict(q=0), -1), (dict(kc=0), -1),
     (dict(vc=0), -1), (dict(lengths=0), -1), (dict(table=0), -1), (dict(out=0), -1), (dict(lse=0), -1), (dict(q=0x1004), -4), (dict(vc=0x3008), -4),
     (dict(out=0x6004), -4), (dict(table=0x5002), -4), (dict(lse=0x7001), -4), (dict(H=4096, H_kv=1, B=1 << 13, qs=4096 * 64), -2),
+    (dict(max_pages=4096, max_len=65536), -6), (dict(max_pages=4096, max_len=65536, ws=0x10000, wn=100), -6), (dict(ws=0x10008, wn=1 << 30), -4),
     (dict(B=0), 0), (dict(B=0, q=0, out=0), 0)])
 def test_decode(lib, change, code):
+    assert lib.lss_set_workspace(None, 0) == 0
     assert _decode(lib, **change) == code
     assert code == 0 or "paged_attn_decode" in lss.lss_last_error()
 
@@ -64,3 +66,11 @@ def test_packed(lib, change, code):
         return
     assert _packed(lib, **change) == code
     assert code == 0 or "packed_attn_fwd" in lss.lss_last_error()
+
+
+def test_scratch_of_the_attention_of_one_token(lib):
+    need = lib.lss_paged_attn_workspace_bytes
+    assert need(4, 2, 64, 64) == 0 and need(4, 2, 64, 1 << 20) > 0
+    assert need(32, 4, 128, 1 << 20) == need(32, 4, 128, 1 << 21) > need(16, 4, 128, 1 << 20)        # of the heads of a group, not of the lengths
+    for bad in ((0, 1, 64, 4096), (4, 0, 64, 4096), (5, 2, 64, 4096), (4, 2, 96, 4096), (4, 2, 64, -1)):
+        assert need(*bad) == 0
