@@ -28,6 +28,7 @@
 #include "lss_bf16.h"
 #include <type_traits>
 #include "lss_kernels.h"
+#include "lss_serve.h"
 
 namespace lss {
 
@@ -48,41 +49,35 @@ struct FwdBf16Cfg {
     static constexpr float kMaxBlockSum = 256.0f;       // 2^8: largest sum of a lane's weights of one block without a fix-up
 };
 
+// What a workgroup's rows are and what they read, in elements: row r is head r % G (D columns further on) of token r / G, whose position is s0 + r / G.
+struct FwdView {
+    const bf16_t *q, *k, *v;    // first rows
+    int64_t q_ld, k_ld, v_ld;   // from a token to the next
+    int64_t s0;
+    int l_s, l_x, causal, G;    // rows, keys
+};
+
 // DROP: dropout on the weights (Section 2.2): the weight that multiplies V is dropped or (the finished sum) scaled by
 // 1 / (1 - p) according to drop_keep() of (seed, batch*head, global row, key); row sum and lse are
 // those of the softmax.
-template <int D, bool DROP, int RB, int KG>
-__global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void fwd_bf16_kernel(SegShape s, DropArgs dr, const bf16_t *__restrict__ q,
-                                                                       const bf16_t *__restrict__ k,
-                                                                       const bf16_t *__restrict__ v,
-                                                                       bf16_t *__restrict__ out, float *__restrict__ lse,
-                                                                       float *__restrict__ o_part,
-                                                                       float *__restrict__ lse_part, int n_splits, int n_q_tiles)
+// The rows r0 .. of a workgroup: put(u, values) takes columns 8 u + 4 (lane / 32) .. + 3 of row r0 + 32 (wavefront) + lane % 32, normalised,
+// put_lse its lse.  `bh`: batch * head for the dropout's decisions.
+template <int D, bool DROP, int RB, int KG, typename Put, typename PutLse>
+__device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, const DropArgs &dr, int bh, int r0, int split, int n_splits, Put &&put,
+                                              PutLse &&put_lse)
 {
     using C = FwdBf16Cfg<D, RB, KG>;
     using Tile = typename C::Tile;
     constexpr int NU = C::NU;
-    __shared__ __attribute__((aligned(1024))) char smem[C::lds(DROP)];
 
     const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, hh = lane >> 5;
     const int all_waves = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = KG > 1 ? all_waves / RB : 0, wave = KG > 1 ? all_waves % RB : all_waves;      // wave: within the group
     char *const ring = smem + group * C::group_lds(DROP);
-    // 1-D grid in XCD order (xcd_item): one head at a time per XCD, whose workgroups share its K and
-    // V in that XCD's L2.  Within a head: query tiles, last first -- under the causal mask the last
-    // tiles see the most keys, and starting the longest workgroups first shortens the tail of the
-    // launch -- then key splits.
-    const int bhs = s.B * s.H;
-    int bh, inner;
-    if (!xcd_item(blockIdx.x, bhs, n_q_tiles * n_splits, s.causal && s.s0 < s.l_s, bh, inner)) return;
-    const int b = bh / s.H, h = bh % s.H;
-    const int q_tile = inner % n_q_tiles, split = inner / n_q_tiles;
-    const int r0 = (n_q_tiles - 1 - q_tile) * C::BR;
     const int rw0 = r0 + wave * C::RW;                  // first row of this wavefront
-    const int64_t ld = (int64_t)s.H * D;
 
     const int r_last = min(r0 + C::BR, s.l_s) - 1;
-    const int kv_end = s.causal ? (int)min<int64_t>(s.l_x, s.s0 + r_last + 1) : s.l_x;
+    const int kv_end = s.causal ? (int)max<int64_t>(min<int64_t>(s.l_x, s.s0 + r_last / s.G + 1), 0) : s.l_x;
     const int n_tiles = (kv_end + C::BC - 1) / C::BC;
     const int per = (n_tiles + n_splits - 1) / n_splits;
     const int s_begin = split * per, s_tiles = max(min(n_tiles, s_begin + per) - s_begin, 0);
@@ -94,9 +89,11 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void fwd_bf16_kernel
     // (unconditional loads), are computed like any other and never stored
     const int r = rw0 + lq;
     const bool row_ok = r < s.l_s;
+    const int position = (int)s.s0 + r / s.G;
     Frag<bf16_t> qf[NU];
     {
-        const bf16_t *qp = q + ((int64_t)b * s.l_s + min(r, s.l_s - 1)) * ld + (int64_t)h * D + hh * 8;
+        const int rr = min(r, s.l_s - 1);
+        const bf16_t *qp = s.q + (int64_t)(rr / s.G) * s.q_ld + (rr % s.G) * D + hh * 8;
 #pragma unroll
         for (int kb = 0; kb < NU; ++kb) qf[kb] = load_frag<bf16_t>(qp + kb * 16);
     }
@@ -109,45 +106,44 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void fwd_bf16_kernel
     const float c = kLog2e / sqrtf((float)D);
 
     if (s_tiles > 0) {
-        const bf16_t *kbase = k + (int64_t)b * s.l_x * ld + (int64_t)h * D;
-        const bf16_t *vbase = v + (int64_t)b * s.l_x * ld + (int64_t)h * D;
-
         // dropout: this lane's row key; the column seed; the column keys of tile t (global tile index)
         // are computed once, by one wavefront when the tile's loads are issued, into quarter t % 4 of
         // a small ring behind the tiles -- published by the same barrier as the tile
         uint32_t drop_rk = 0u, drop_cs = 0u;
-        if (DROP) { drop_rk = drop_row_key(dr.seed_lo, (uint32_t)bh, (uint32_t)(s.s0 + r)); drop_cs = drop_col_seed(dr.seed_hi); }
+        if (DROP) { drop_rk = drop_row_key(dr.seed_lo, (uint32_t)bh, (uint32_t)position); drop_cs = drop_col_seed(dr.seed_hi); }
         char *const ck_ring = ring + C::RING;
 
         // ---- tile loads, by all wavefronts of the group.  No branch and few scalar instructions on purpose: a branch inside a
         // pipeline step splits it into basic blocks, and the vector work that was meant to sit between the step's matrix
         // instructions is then moved behind the branch in one lump; addresses move on between the iterations instead.
-        uint32_t offK[Tile::NI], offV[Tile::NI], offD[Tile::NI];    // this lane's global offsets within the next K and V tile; and
-        Tile::pair_offsets(offK, ld, C::BC, wave, lane);            // what must be added to them in the sequence's last, partial
-        const int t_part = s.l_x % C::BC ? s.l_x / C::BC : -1;     // tile (rows past the end re-read the last row)
-        {
-            uint32_t offL[Tile::NI];
+        uint32_t offK[Tile::NI], offV[Tile::NI], offDK[Tile::NI], offDV[Tile::NI];     // this lane's global offsets within the next K and V
+        const int t_part = s.l_x % C::BC ? s.l_x / C::BC : -1;     // tile; and what must be added to them in the sequence's last, partial tile
+        auto tile_offsets = [&](uint32_t (&off)[Tile::NI], uint32_t (&offD)[Tile::NI], int64_t ld) __attribute__((always_inline)) {
+            uint32_t offL[Tile::NI];                                // (rows past the end re-read the last row)
+            Tile::pair_offsets(off, ld, C::BC, wave, lane);
             Tile::pair_offsets(offL, ld, t_part >= 0 ? s.l_x % C::BC : C::BC, wave, lane);
 #pragma unroll
-            for (int i = 0; i < Tile::NI; ++i) { offD[i] = offL[i] - offK[i]; offV[i] = offK[i]; }
-        }
-        const uint32_t tile_bytes = (uint32_t)(C::BC * ld * 2);
+            for (int i = 0; i < Tile::NI; ++i) offD[i] = offL[i] - off[i];
+        };
+        tile_offsets(offK, offDK, s.k_ld);
+        tile_offsets(offV, offDV, s.v_ld);
+        const uint32_t k_bytes = (uint32_t)(C::BC * s.k_ld * 2), v_bytes = (uint32_t)(C::BC * s.v_ld * 2);
         // the next tile of K to load, and of V, one behind; past the group's last one that one again
         const int t_last = t_begin + max(T, 1) - 1;
         int k_tile_next = t_begin, v_tile_next = t_begin;
-        const char *k_next = tile_ptr(Tile::pair_base(kbase), t_begin, tile_bytes), *v_next = tile_ptr(Tile::pair_base(vbase), t_begin, tile_bytes);
-        auto to_part = [&](int t, uint32_t (&off)[Tile::NI]) __attribute__((always_inline)) {
+        const char *k_next = tile_ptr(Tile::pair_base(s.k), t_begin, k_bytes), *v_next = tile_ptr(Tile::pair_base(s.v), t_begin, v_bytes);
+        auto to_part = [&](int t, uint32_t (&off)[Tile::NI], const uint32_t (&offD)[Tile::NI]) __attribute__((always_inline)) {
             if (t == t_part)
 #pragma unroll
                 for (int i = 0; i < Tile::NI; ++i) off[i] += offD[i];
         };
-        to_part(k_tile_next, offK);
-        to_part(v_tile_next, offV);
+        to_part(k_tile_next, offK, offDK);
+        to_part(v_tile_next, offV, offDV);
         auto advance_k = [&] {
-            if (k_tile_next < t_last) { ++k_tile_next; k_next += tile_bytes; to_part(k_tile_next, offK); }
+            if (k_tile_next < t_last) { ++k_tile_next; k_next += k_bytes; to_part(k_tile_next, offK, offDK); }
         };
         auto advance_v = [&] {
-            if (v_tile_next < t_last) { ++v_tile_next; v_next += tile_bytes; to_part(v_tile_next, offV); }
+            if (v_tile_next < t_last) { ++v_tile_next; v_next += v_bytes; to_part(v_tile_next, offV, offDV); }
         };
         // Iteration t's loads, behind its barrier: K of tile t + 2 in the place of tile t's, whose last rows have been read
         // by then, and V of tile t + 1 in the place of tile t - 1's.  (Past the end a tile is loaded once more: K where it
@@ -186,10 +182,10 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void fwd_bf16_kernel
         // 0: keys after the lane's row, and keys past the sequence (whose loads re-read its last
         // row).  C-tile element e of this lane is key 8*(e/4) + 4*hh + e%4 of the block.
         // (positions are below 2^30, checked on the host: one 32-bit scalar compare, no vector work per step)
-        const int last_whole = min(s.causal ? (int)s.s0 + rw0 - 31 : s.l_x, s.l_x - 32);       // blocks from here on need no mask
+        const int last_whole = min(s.causal ? (int)s.s0 + rw0 / s.G - 31 : s.l_x, s.l_x - 32);       // blocks from here on need no mask
         auto mask_s = [&](int jb, f32x16 &sc) __attribute__((always_inline)) {
             if (jb > last_whole) {
-                const int last = s.causal ? min((int)s.s0 + r, s.l_x - 1) : s.l_x - 1;
+                const int last = s.causal ? min(position, s.l_x - 1) : s.l_x - 1;
                 const int rel = max(min(last - jb - 4 * hh, 64), -1);
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
@@ -396,18 +392,6 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void fwd_bf16_kernel
         wait_vmem_all();                                // the last, redundant prefetches must land before the workgroup's LDS is given away
     }
 
-    // this lane's row of the result: column group u, columns 8 u + 4 hh .. + 3 (a split's normalised output travels to the
-    // merge kernel in fp32: rounded to bf16 once, there)
-    const int64_t part_row = ((int64_t)split * bhs + bh) * s.l_s + r;
-    auto put = [&](int u, const f32x4 &val) __attribute__((always_inline)) {
-        if (n_splits == 1)
-            *reinterpret_cast<bf16x4 *>(out + ((int64_t)b * s.l_s + r) * ld + (int64_t)h * D + 8 * u + 4 * hh) = pack4(val[0], val[1], val[2], val[3]);
-        else *reinterpret_cast<f32x4 *>(o_part + part_row * D + 8 * u + 4 * hh) = val;
-    };
-    auto put_lse = [&](float v) {
-        if (n_splits == 1) lse[(int64_t)bh * s.l_s + r] = v;
-        else lse_part[part_row] = v;
-    };
     const float l_own = l + __shfl_xor(l, 32);
     const float kept = DROP ? dr.scale : 1.f;           // of the kept weights: applied to their sum
     if constexpr (KG == 1) {
@@ -463,6 +447,86 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void fwd_bf16_kernel
     }
 }
 
+template <int D, bool DROP, int RB, int KG>
+__global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void fwd_bf16_kernel(SegShape s, DropArgs dr, const bf16_t *__restrict__ q,
+                                                                       const bf16_t *__restrict__ k,
+                                                                       const bf16_t *__restrict__ v,
+                                                                       bf16_t *__restrict__ out, float *__restrict__ lse,
+                                                                       float *__restrict__ o_part,
+                                                                       float *__restrict__ lse_part, int n_splits, int n_q_tiles)
+{
+    using C = FwdBf16Cfg<D, RB, KG>;
+    __shared__ __attribute__((aligned(1024))) char smem[C::lds(DROP)];
+    // 1-D grid in XCD order (xcd_item): one head at a time per XCD, whose workgroups share its K and
+    // V in that XCD's L2.  Within a head: query tiles, last first -- under the causal mask the last
+    // tiles see the most keys, and starting the longest workgroups first shortens the tail of the
+    // launch -- then key splits.
+    const int bhs = s.B * s.H;
+    int bh, inner;
+    if (!xcd_item(blockIdx.x, bhs, n_q_tiles * n_splits, s.causal && s.s0 < s.l_s, bh, inner)) return;
+    const int b = bh / s.H, h = bh % s.H;
+    const int q_tile = inner % n_q_tiles, split = inner / n_q_tiles;
+    const int r0 = (n_q_tiles - 1 - q_tile) * C::BR;
+    const int64_t ld = (int64_t)s.H * D, head = (int64_t)h * D;
+    const FwdView view{q + (int64_t)b * s.l_s * ld + head, k + (int64_t)b * s.l_x * ld + head, v + (int64_t)b * s.l_x * ld + head, ld, ld, ld, s.s0, s.l_s,
+                       s.l_x, s.causal, 1};
+    // this lane's row of the result (a split's normalised output travels to the merge kernel in fp32: rounded to bf16 once, there)
+    const int lane = threadIdx.x & 63, r = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % RB * C::RW + (lane & 31), hh = lane >> 5;
+    const int64_t part_row = ((int64_t)split * bhs + bh) * s.l_s + r;
+    fwd_bf16_body<D, DROP, RB, KG>(
+        smem, view, dr, bh, r0, split, n_splits,
+        [&](int u, const f32x4 &val) __attribute__((always_inline)) {
+            if (n_splits == 1)
+                *reinterpret_cast<bf16x4 *>(out + ((int64_t)b * s.l_s + r) * ld + (int64_t)h * D + 8 * u + 4 * hh) = pack4(val[0], val[1], val[2], val[3]);
+            else *reinterpret_cast<f32x4 *>(o_part + part_row * D + 8 * u + 4 * hh) = val;
+        },
+        [&](float v) {
+            if (n_splits == 1) lse[(int64_t)bh * s.l_s + r] = v;
+            else lse_part[part_row] = v;
+        });
+}
+
+// Packed sequences (lss_packed_attn_fwd).  A row of a workgroup is a query head of a token: the G heads that share a head of keys and values are
+// neighbours, so that a tile of keys serves 128 / G tokens of all of them, the causal diagonal crosses fewer of a wavefront's blocks,
+// and short prompts fill the rows.
+template <int D, int RB, int KG>
+__global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void packed_bf16_kernel(PackedArgs a, const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
+                                                                                   const bf16_t *__restrict__ v, bf16_t *__restrict__ out,
+                                                                                   float *__restrict__ lse, int n_inner)
+{
+    using C = FwdBf16Cfg<D, RB, KG>;
+    __shared__ __attribute__((aligned(1024))) char smem[C::lds(false)];
+    const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5, G = a.H / a.H_kv;
+    int h_kv, rank;
+    if (!xcd_item(blockIdx.x, a.H_kv, n_inner, a.causal != 0, h_kv, rank)) return;
+    PackedTile t;
+    if (!packed_tile<C::BR>(a, G, rank, lane, t)) return;
+    const FwdView view{q + (int64_t)t.q_begin * a.q_stride + (int64_t)h_kv * G * D, k + (int64_t)t.k_begin * a.k_stride + (int64_t)h_kv * D,
+                       v + (int64_t)t.k_begin * a.v_stride + (int64_t)h_kv * D, a.q_stride, a.k_stride, a.v_stride, t.n_k - t.n_q, t.n_q * G, t.n_k, a.causal, G};
+    const int r0 = t.tile * C::BR, rw0 = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % RB * C::RW, r = rw0 + lq;
+    const int token = t.q_begin + r / G, h = h_kv * G + r % G;
+    bf16_t *const row = out + ((int64_t)token * a.H + h) * D;
+    bool finite = true;
+    fwd_bf16_body<D, false, RB, KG>(
+        smem, view, DropArgs{}, 0, r0, 0, 1,
+        [&](int u, const f32x4 &val) __attribute__((always_inline)) {
+            *reinterpret_cast<bf16x4 *>(row + 8 * u + 4 * hh) = pack4(val[0], val[1], val[2], val[3]);
+            finite = finite && fabsf(val[0]) < INFINITY && fabsf(val[1]) < INFINITY && fabsf(val[2]) < INFINITY && fabsf(val[3]) < INFINITY;
+        },
+        [&](float v) { lse[(int64_t)h * a.rows_q + token] = v; });
+    // A key's weight is 0 for the rows of its block that do not see it, but 0 times a value that is not finite is NaN: rows with such a result are done over,
+    // over the keys that they see alone.
+    if (KG > 1) __syncthreads();                // (the groups have written parts of one row)
+    const uint64_t bad = __ballot(!finite);
+    for (uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32); rows != 0; rows &= rows - 1) {
+        const int again = rw0 + __builtin_ctz(rows), at = again / G, head = h_kv * G + again % G;
+        const int seen = a.causal ? max(0, min(t.n_k, t.n_k - t.n_q + at + 1)) : t.n_k;
+        row_attention<bf16_t, D>(view.q + (int64_t)at * a.q_stride + again % G * D, view.k, a.k_stride, view.v, a.v_stride, seen, lane,
+                                 [](int j) { return (int64_t)j; }, out + ((int64_t)(t.q_begin + at) * a.H + head) * D,
+                                 lse + (int64_t)head * a.rows_q + t.q_begin + at);
+    }
+}
+
 int fwd_bf16_rows_per_workgroup(int d) { return d == 64 ? 128 : 256; }
 
 template <int D, int RB, int KG>
@@ -496,6 +560,24 @@ hipError_t launch_fwd_bf16_main(const SegShape &s, const DropArgs &drop, const b
     }
     if (plan.form == FWD_4x2) return launch_fwd_main<128, 4, 2>(s, drop, q, k, v, out, lse, ws, plan.splits, st);
     return launch_fwd_main<128, 8, 1>(s, drop, q, k, v, out, lse, ws, plan.splits, st);
+}
+
+template <int D, int RB, int KG>
+static hipError_t launch_packed(const PackedArgs &a, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse, hipStream_t st)
+{
+    using C = FwdBf16Cfg<D, RB, KG>;
+    const int n_inner = packed_tiles(a, C::BR);
+    TimedLaunch tl(K_PACKED_BF16, st);
+    hipLaunchKernelGGL((packed_bf16_kernel<D, RB, KG>), dim3((unsigned)xcd_grid(a.H_kv, n_inner)), dim3(C::NT), 0, st, a, q, k, v, out, lse, n_inner);
+    return hipGetLastError();
+}
+
+hipError_t launch_packed_bf16(const PackedArgs &a, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse, hipStream_t st)
+{
+    if (a.d == 64) {
+        return launch_packed<64, 4, 1>(a, q, k, v, out, lse, st);
+    }
+    return launch_packed<128, 8, 1>(a, q, k, v, out, lse, st);
 }
 
 } // namespace lss

@@ -110,7 +110,7 @@ hipError_t allow_lds(K kernel, int bytes, DeviceOnce &once)
 enum KernelId { K_FWD_F32 = 0, K_FWD_MERGE, K_ROWDOT, K_BWD_MAIN_F32, K_DQ_MERGE, K_REDUCE, K_BWD_MAIN_BF16, K_PROJ_FWD, K_PROJ_BWD,
                 K_PE_FWD, K_PE_BWD, K_LN_FWD, K_LN_BWD, K_LN_PARAMS, K_GELU_FWD, K_GELU_BWD, K_LINEAR_FWD, K_LINEAR_BWD, K_RESIDUAL, K_LINEAR_WGRAD,
                 K_FWD_BF16, K_BWD_PREP_BF16, K_BWD_SKINNY_BF16, K_LN_BWD_SHORT, K_PROJ_FWD_SMALL, K_PROJ_BWD_SMALL, K_LINEAR_FWD_SMALL,
-                K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_ATTN, K_COUNT };
+                K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_ATTN, K_PACKED_BF16, K_COUNT };
 void timing_begin(int id, hipStream_t st);
 void timing_end(int id, hipStream_t st);
 struct TimedLaunch {    // RAII bracket around one kernel launch
@@ -198,6 +198,12 @@ struct PackedArgs {
     int64_t q_stride, k_stride, v_stride;
     int rows_q, rows_k, B, H, H_kv, d, causal;
 };
+// most tiles of `rows` rows (query heads of tokens) that the sequences can have per head of keys and values
+inline int packed_tiles(const PackedArgs &a, int rows)
+{
+    return (int)((int64_t)a.rows_q * (a.H / a.H_kv) / rows) + (a.B <= 64 && a.rows_q < a.B ? a.rows_q : a.B);
+}
+hipError_t launch_packed_bf16(const PackedArgs &a, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse, hipStream_t st);
 template <typename T>
 hipError_t launch_packed_attn(const PackedArgs &a, const T *q, const T *k, const T *v, T *out, float *lse, hipStream_t st);
 

@@ -36,7 +36,11 @@ hipError_t launch_packed_attn(const PackedArgs &a, const T *q, const T *k, const
     return hipGetLastError();
 }
 
-template hipError_t launch_packed_attn<bf16_t>(const PackedArgs &, const bf16_t *, const bf16_t *, const bf16_t *, bf16_t *, float *, hipStream_t);
+template <>
+hipError_t launch_packed_attn<bf16_t>(const PackedArgs &a, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse, hipStream_t st)
+{
+    return launch_packed_bf16(a, q, k, v, out, lse, st);
+}
 template hipError_t launch_packed_attn<float>(const PackedArgs &, const float *, const float *, const float *, float *, float *, hipStream_t);
 
 } // namespace lss

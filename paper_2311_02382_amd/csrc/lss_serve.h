@@ -35,6 +35,75 @@ __device__ __forceinline__ int64_t cache_row(const PageTable &pt, int b, int pos
     return ((int64_t)page << pt.page_shift) + (position & ((1 << pt.page_shift) - 1));
 }
 
+// ---- tiles of packed sequences: BR rows each, a row being one of a token's G heads
+__device__ __forceinline__ int lane_sum_scan(int x)     // inclusive over the wavefront; all lanes active
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+struct PackedTile { int q_begin, n_q, k_begin, n_k, tile; };
+// Tile `rank` of a head of keys and values; false: there are fewer.  Up to 64 sequences, a lane each: tiles in the order of the keys they see (in
+// steps of 64), most first, so that no long one starts last.  More sequences: in the sequences' order, sequence b's tiles from number
+// floor(cu[b] G / BR) + b on -- room for all of them, one at most too much --, which is found like a row's sequence.
+template <int BR>
+__device__ __forceinline__ bool packed_tile(const PackedArgs &a, int G, int rank, int lane, PackedTile &t)
+{
+    const auto ends = [](const int32_t *cu, int b, int rows, int &begin, int &n) {
+        begin = max(0, min(cu[b], rows));
+        n = max(0, min(cu[b + 1], rows) - begin);
+    };
+    int b, begin = 0, n_q = 0, k_begin = 0, n_k = 0, tile;
+    if (a.B <= 64) {
+        if (lane < a.B) {
+            ends(a.cu_q, lane, a.rows_q, begin, n_q);
+            ends(a.cu_k, lane, a.rows_k, k_begin, n_k);
+        }
+        const int tiles = (n_q * G + BR - 1) / BR;
+        // its tiles that see keys from number 64 (x - 1) on: tile j's last row is of token ((j + 1) BR - 1) / G
+        const auto count = [&](int x) {
+            if (x <= 1) return tiles;
+            const int last = 64 * (x - 1);              // some row's position must reach it
+            if (last >= n_k) return 0;
+            return a.causal ? max(0, tiles - max(0, last - (n_k - n_q)) * G / BR) : tiles;
+        };
+        const auto total = [&](int x) { return __builtin_amdgcn_readlane(lane_sum_scan(count(x)), 63); };
+        int lo = 1, hi = (a.rows_k + 63) / 64 + 1;      // total(lo) > rank >= total(hi)
+        if (rank >= total(1)) return false;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (total(mid) > rank) lo = mid;
+            else hi = mid;
+        }
+        const int above = count(lo + 1), mine = count(lo) - above, scan = lane_sum_scan(mine), in = rank - total(lo + 1);
+        b = __ffsll((long long)__ballot(scan > in)) - 1;
+        tile = tiles - count(lo) + in - (scan - mine);
+        const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, b); };
+        t = {of(begin), of(n_q), of(k_begin), of(n_k), of(tile)};
+        return true;
+    }
+    const auto first = [&](int i) { return (int)((int64_t)max(0, min(a.cu_q[i], a.rows_q)) * G / BR) + i; };
+    int lo = 0, n = a.B;
+    while (n > 1) {
+        const int step = (n + 63) / 64, at = lane * step;
+        const uint64_t below = __ballot(at < n && first(lo + min(at, n - 1)) <= rank);
+        if (below == 0) return false;
+        const int last = 63 - __clzll((long long)below);
+        lo += last * step;
+        n = min(step, n - last * step);
+    }
+    b = __builtin_amdgcn_readfirstlane(lo);
+    ends(a.cu_q, b, a.rows_q, begin, n_q);
+    ends(a.cu_k, b, a.rows_k, k_begin, n_k);
+    t = {__builtin_amdgcn_readfirstlane(begin), __builtin_amdgcn_readfirstlane(n_q), __builtin_amdgcn_readfirstlane(k_begin),
+         __builtin_amdgcn_readfirstlane(n_k), __builtin_amdgcn_readfirstlane(rank - first(b))};
+    return t.tile >= 0 && t.tile < (t.n_q * G + BR - 1) / BR;
+}
+
 template <typename T> struct Vec16;
 template <> struct Vec16<bf16_t> { typedef bf16x8 type; };
 template <> struct Vec16<float> { typedef f32x4 type; };
