@@ -3,6 +3,7 @@
 #include "lss_attn.h"
 #include "lss_common.h"
 #include "lss_kernels.h"
+#include "lss_packed_plan.h"
 #include "lss_plan.h"
 
 #include <cmath>
@@ -801,7 +802,7 @@ static int check_groups(const char *what, int64_t H, int64_t H_kv)
 static int check_rows(const char *what, const char *name, int64_t rows, int64_t stride, int64_t heads, int64_t d, int elem_bytes)
 {
     if (rows < 0 || rows > (int64_t)1 << 30) return fail(LSS_ERR_SHAPE, "%s: %lld rows of %s (0 .. 2^30)", what, (long long)rows, name);
-    if (stride < heads * d || stride > (int64_t)1 << 30) return fail(LSS_ERR_SHAPE, "%s: rows of %s are %lld elements apart (at least %lld, at most 2^30)", what, name, (long long)stride, (long long)(heads * d));
+    if (stride < heads * d || stride > (int64_t)1 << 23) return fail(LSS_ERR_SHAPE, "%s: rows of %s are %lld elements apart (at least %lld, at most 2^23)", what, name, (long long)stride, (long long)(heads * d));
     if (stride * elem_bytes % 16 != 0) return fail(LSS_ERR_ALIGN, "%s: rows of %s must be 16-byte aligned", what, name);
     return LSS_OK;
 }
@@ -926,18 +927,20 @@ int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t 
     if (int rc = check_rows(what, "q", rows_q, q_stride, H, d, elem_bytes)) return rc;
     if (int rc = check_rows(what, "k", rows_k, k_stride, H_kv, d, elem_bytes)) return rc;
     if (int rc = check_rows(what, "v", rows_k, v_stride, H_kv, d, elem_bytes)) return rc;
+    if (H_kv * (rows_q * (H / H_kv) / 32 + B) > (int64_t)1 << 30 || rows_q * (H / H_kv) > (int64_t)1 << 30)
+        return fail(LSS_ERR_SHAPE, "%s: %lld rows of %lld heads in %lld sequences are too many", what, (long long)rows_q, (long long)H, (long long)B);
     if (B == 0 || rows_q == 0) return LSS_OK;
     if (!q || !cu_q || !cu_k || !out || !lse || (rows_k > 0 && (!k || !v))) return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
     if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out))
         return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
     if (int rc = check_arrays(what, {cu_q, cu_k, lse})) return rc;
     const lss::PackedArgs a{cu_q, cu_k, q_stride, k_stride, v_stride, (int)rows_q, (int)rows_k, (int)B, (int)H, (int)H_kv, (int)d, causal ? 1 : 0};
-    const auto go = [&](auto zero) {
-        typedef decltype(zero) T;
-        return lss::launch_packed_attn<T>(a, static_cast<const T *>(q), static_cast<const T *>(k), static_cast<const T *>(v), static_cast<T *>(out), lse,
-                                          static_cast<hipStream_t>(stream));
-    };
-    const hipError_t e = elem_bytes == 2 ? go(lss::bf16_t{}) : go(float{});
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    using lss::bf16_t;
+    const hipError_t e = elem_bytes == 2 ? lss::launch_packed_bf16(a, static_cast<const bf16_t *>(q), static_cast<const bf16_t *>(k),
+                                                                   static_cast<const bf16_t *>(v), static_cast<bf16_t *>(out), lse, st)
+                                         : lss::launch_packed_f32(a, static_cast<const float *>(q), static_cast<const float *>(k),
+                                                                  static_cast<const float *>(v), static_cast<float *>(out), lse, st);
     if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));
     return LSS_OK;
 }
@@ -978,6 +981,17 @@ int lss_plan_bwd(int64_t s0, int64_t l_s, int64_t l_x, int64_t B, int64_t H, int
     const lss::BwdLaunch p = lss::plan_bwd(s, with_dropout != 0, elem_bytes, !over_out);
     const int all[6] = {p.splits, p.groups, p.one_pass, p.own, p.skinny, p.narrow};
     std::copy(all, all + 6, plan);
+    return LSS_OK;
+}
+
+int lss_plan_packed(int64_t rows_q, int64_t rows_k, int64_t B, int64_t H, int64_t H_kv, int64_t d, int *plan)
+{
+    if (int rc = check_heads("plan", H, H_kv, d, 2)) return rc;
+    if (rows_q < 1 || rows_k < 0 || B < 1 || H % H_kv != 0) return fail(LSS_ERR_SHAPE, "plan: no launch of such a call");
+    if (!plan) return fail(LSS_ERR_NULL, "plan: NULL");
+    const lss::PackedForm f = lss::pick_packed_form(rows_q, rows_k, B, H, H_kv, d);
+    plan[0] = f.row_blocks;
+    plan[1] = f.groups;
     return LSS_OK;
 }
 

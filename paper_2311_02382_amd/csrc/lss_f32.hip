@@ -27,6 +27,7 @@
 // multiplies.
 #include "lss_bf16.h"
 #include "lss_kernels.h"
+#include "lss_serve.h"
 
 #include <type_traits>
 
@@ -355,39 +356,45 @@ __device__ __forceinline__ bool missed(const Sums<D, NJ> &acc)
 }
 
 // ------------------------------------------------------------------------------------------ forward
-template <int D, bool DROP>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fwd_f32_kernel(SegShape s, DropArgs dr, const float *__restrict__ q,
-                                                         const float *__restrict__ k, const float *__restrict__ v,
-                                                         float *__restrict__ out, float *__restrict__ lse,
-                                                         float *__restrict__ o_part, float *__restrict__ lse_part, int n_splits,
-                                                         int n_q_tiles)
+// What a workgroup's rows are and what they read, in elements: row r is head r % G (D columns further on) of token r / G, whose position is s0 + r / G.
+struct FwdView {
+    const float *q, *k, *v;     // first rows
+    int64_t q_ld, k_ld, v_ld;   // from a token to the next
+    int64_t s0;
+    int l_s, l_x, causal, G;    // rows, keys
+};
+
+// Rows r0 .. r0 + 127: put(j, db, values) takes columns 16 db + 4 (lane / 16) .. + 3 of row r0 + 32 (wavefront) + 16 j + lane % 16, normalised, put_lse(j, .) its
+// lse.  `bh`: batch * head for the dropout's decisions.
+template <int D, bool DROP, typename Put, typename PutLse>
+__device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const DropArgs &dr, int bh, int r0, int split, int n_splits, Put &&put,
+                                             PutLse &&put_lse)
 {
     using Tile = PlaneTile<D>;
     constexpr int NS = D / 32, BC = Tile::ROWS;
-    __shared__ __attribute__((aligned(1024))) char smem[2 * Tile::BYTES + 16];
     char *const sk = smem, *const sv = smem + Tile::BYTES;
     uint32_t *const tiny_word = reinterpret_cast<uint32_t *>(smem + 2 * Tile::BYTES);
 
     const int tid = threadIdx.x, lane = tid & 63, lq = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int bhs = s.B * s.H;
-    int bh, inner;
-    if (!xcd_item(blockIdx.x, bhs, n_q_tiles * n_splits, s.causal && s.s0 < s.l_s, bh, inner)) return;
-    const int b = bh / s.H, h = bh % s.H, split = inner / n_q_tiles;
-    const int r0 = (n_q_tiles - 1 - inner % n_q_tiles) * kRowsPerWg, rw0 = r0 + wave * 32;
-    const int64_t ld = (int64_t)s.H * D;
+    const int rw0 = r0 + wave * 32;
 
     // the keys any row of this tile sees, and this split's share of their tiles
     const int r_last = min(r0 + kRowsPerWg, s.l_s) - 1;
-    const int kv_end = s.causal ? (int)min<int64_t>(s.l_x, s.s0 + r_last + 1) : s.l_x;
+    const int kv_end = s.causal ? (int)max<int64_t>(min<int64_t>(s.l_x, s.s0 + r_last / s.G + 1), 0) : s.l_x;
     const int n_tiles = (kv_end + BC - 1) / BC, per = (n_tiles + n_splits - 1) / n_splits;
     const int t_begin = split * per, t_end = min(n_tiles, t_begin + per);
 
     // this lane's two query rows, r + 16 j; rows past the segment re-read its last row and are never stored
     const int r = rw0 + lq;
     Frag3 qf[NS][2];
-    const float *const qp = q + (int64_t)b * s.l_s * ld + (int64_t)h * D + g * 8;
-    const bool tiny = split_rows<D, 2>(qp, {min(r, s.l_s - 1) * ld, min(r + 16, s.l_s - 1) * ld}, qf);
+    const float *const qp = s.q + g * 8;
+    const auto row_at = [&](int j) {
+        const int rr = min(r + 16 * j, s.l_s - 1);
+        return (int64_t)(rr / s.G) * s.q_ld + (rr % s.G) * D;
+    };
+    const bool tiny = split_rows<D, 2>(qp, {row_at(0), row_at(1)}, qf);
+    const int position[2] = {(int)s.s0 + r / s.G, (int)s.s0 + (r + 16) / s.G}, first_position = (int)s.s0 + rw0 / s.G, last_position = (int)s.s0 + (rw0 + 31) / s.G;
     if (tid == 0) *tiny_word = 0u;
     Sums<D, 2> o;
     o.clear();
@@ -397,10 +404,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fwd_f32_kernel(SegShape 
     if (DROP) {
         drop_cs = drop_col_seed(dr.seed_hi);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) drop_rk[j] = drop_row_key(dr.seed_lo, (uint32_t)bh, (uint32_t)(s.s0 + r + 16 * j));
+        for (int j = 0; j < 2; ++j) drop_rk[j] = drop_row_key(dr.seed_lo, (uint32_t)bh, (uint32_t)position[j]);
     }
 
-    const float *kbase = k + (int64_t)b * s.l_x * ld + (int64_t)h * D, *vbase = v + (int64_t)b * s.l_x * ld + (int64_t)h * D;
     int a_off[NS], t_off[D / 16];
 #pragma unroll
     for (int ks = 0; ks < NS; ++ks) a_off[ks] = Tile::chunk_offset(lq, 4 * ks + g);
@@ -411,21 +417,21 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fwd_f32_kernel(SegShape 
     auto block = [&](auto exact, int jb, int kb2) __attribute__((always_inline)) {
         constexpr bool EXACT = decltype(exact)::value;
         // a block no row of this wavefront sees
-        if (jb >= s.l_x || (s.causal && jb > (int)s.s0 + rw0 + 31)) return;
+        if (jb >= s.l_x || (s.causal && jb > last_position)) return;
         Block<2> sc;
         Frag3 ahead;
         if constexpr (EXACT) {
-            sc = product_f32<D, 2>(kbase, {(int64_t)min(jb + lq, s.l_x - 1) * ld + g * 8, (int64_t)min(jb + 16 + lq, s.l_x - 1) * ld + g * 8}, qp,
-                                   {min(r, s.l_s - 1) * ld, min(r + 16, s.l_s - 1) * ld});
+            sc = product_f32<D, 2>(s.k, {(int64_t)min(jb + lq, s.l_x - 1) * s.k_ld + g * 8, (int64_t)min(jb + 16 + lq, s.l_x - 1) * s.k_ld + g * 8}, qp,
+                                   {row_at(0), row_at(1)});
         } else {
             ahead = Tile::rows_frag(sk, kb2 * 32, a_off[0]);
             sc = Tile::product(sk, kb2 * 32, a_off, qf, ahead, [&] { return Tile::cols_frag(sv, kb2 * 32, t_off[0]); });
         }
         // element (i, e) of this lane is key jb + 16 i + 4 g + e
-        if ((s.causal && jb + 31 > (int)s.s0 + rw0) || jb + 32 > s.l_x) {
+        if ((s.causal && jb + 31 > first_position) || jb + 32 > s.l_x) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int last = s.causal ? min((int)s.s0 + r + 16 * j, s.l_x - 1) : s.l_x - 1, rel = last - jb - 4 * g;
+                const int last = s.causal ? min(position[j], s.l_x - 1) : s.l_x - 1, rel = last - jb - 4 * g;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     if (16 * (e >> 2) + (e & 3) > rel) sc.v[e >> 2][j][e & 3] = -INFINITY;
@@ -473,7 +479,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fwd_f32_kernel(SegShape 
             }
         }
         if constexpr (EXACT) {
-            add_product_f32<D>(vbase + (int64_t)jb * ld, ld, s.l_x - jb, sc, o, lq, g);
+            add_product_f32<D>(s.v + (int64_t)jb * s.v_ld, s.v_ld, s.l_x - jb, sc, o, lq, g);
         } else {
             const Frag3 pf[2] = {split_acc(sc, 0), split_acc(sc, 1)};
             Tile::columns(sv, kb2 * 32, t_off, ahead, [&](int db, const Frag3 &a) __attribute__((always_inline)) { mma6(a, pf, o.v[db]); },
@@ -483,8 +489,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fwd_f32_kernel(SegShape 
     for (int t = t_begin; t < t_end; ++t) {
         {
             typename Tile::Regs gk, gv;
-            Tile::fetch(gk, kbase + (int64_t)t * BC * ld, ld, s.l_x - t * BC, tid);
-            Tile::fetch(gv, vbase + (int64_t)t * BC * ld, ld, s.l_x - t * BC, tid);
+            Tile::fetch(gk, s.k + (int64_t)t * BC * s.k_ld, s.k_ld, s.l_x - t * BC, tid);
+            Tile::fetch(gv, s.v + (int64_t)t * BC * s.v_ld, s.v_ld, s.l_x - t * BC, tid);
             __syncthreads();                    // the tile before has been read
             Tile::store(sk, gk, tid);
             Tile::store(sv, gv, tid);
@@ -508,18 +514,80 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fwd_f32_kernel(SegShape 
         l_tot += __shfl_xor(l_tot, 32);
         const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
         const float lse_nat = l_tot > 0.f ? (m[j] + log2f(l_tot)) * kLn2 : -INFINITY;
-        const int rj = r + 16 * j;
-        if (rj >= s.l_s) continue;
-        const int64_t row = ((int64_t)split * bhs + bh) * s.l_s + rj;
-        float *op = n_splits == 1 ? out + ((int64_t)b * s.l_s + rj) * ld + (int64_t)h * D : o_part + row * D;
+        if (r + 16 * j >= s.l_s) continue;
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) {
             const f32x4 a = o.v[db][j];
-            *reinterpret_cast<f32x4 *>(op + db * 16 + 4 * g) = f32x4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv};
+            put(j, db, f32x4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv});
         }
-        if (g == 0) {
-            if (n_splits == 1) lse[(int64_t)bh * s.l_s + rj] = lse_nat;
-            else lse_part[row] = lse_nat;
+        if (g == 0) put_lse(j, lse_nat);
+    }
+}
+
+template <int D, bool DROP>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fwd_f32_kernel(SegShape s, DropArgs dr, const float *__restrict__ q,
+                                                         const float *__restrict__ k, const float *__restrict__ v,
+                                                         float *__restrict__ out, float *__restrict__ lse,
+                                                         float *__restrict__ o_part, float *__restrict__ lse_part, int n_splits,
+                                                         int n_q_tiles)
+{
+    __shared__ __attribute__((aligned(1024))) char smem[2 * PlaneTile<D>::BYTES + 16];
+    const int bhs = s.B * s.H;
+    int bh, inner;
+    if (!xcd_item(blockIdx.x, bhs, n_q_tiles * n_splits, s.causal && s.s0 < s.l_s, bh, inner)) return;
+    const int b = bh / s.H, h = bh % s.H, split = inner / n_q_tiles, r0 = (n_q_tiles - 1 - inner % n_q_tiles) * kRowsPerWg;
+    const int64_t ld = (int64_t)s.H * D, head = (int64_t)h * D;
+    const FwdView view{q + (int64_t)b * s.l_s * ld + head, k + (int64_t)b * s.l_x * ld + head, v + (int64_t)b * s.l_x * ld + head, ld, ld, ld, s.s0, s.l_s,
+                       s.l_x, s.causal, 1};
+    const int lane = threadIdx.x & 63, r = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32 + (lane & 15), g = lane >> 4;
+    const auto part_row = [&](int j) { return ((int64_t)split * bhs + bh) * s.l_s + r + 16 * j; };
+    fwd_f32_body<D, DROP>(
+        smem, view, dr, bh, r0, split, n_splits,
+        [&](int j, int db, const f32x4 &val) __attribute__((always_inline)) {
+            float *op = n_splits == 1 ? out + ((int64_t)b * s.l_s + r + 16 * j) * ld + (int64_t)h * D : o_part + part_row(j) * D;
+            *reinterpret_cast<f32x4 *>(op + db * 16 + 4 * g) = val;
+        },
+        [&](int j, float v) __attribute__((always_inline)) {
+            if (n_splits == 1) lse[(int64_t)bh * s.l_s + r + 16 * j] = v;
+            else lse_part[part_row(j)] = v;
+        });
+}
+
+// Packed sequences (lss_packed_attn_fwd): rows are query heads of tokens, as in packed_bf16_kernel
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_f32_kernel(PackedArgs a, const float *__restrict__ q, const float *__restrict__ k,
+                                                                         const float *__restrict__ v, float *__restrict__ out, float *__restrict__ lse,
+                                                                         int n_inner)
+{
+    __shared__ __attribute__((aligned(1024))) char smem[2 * PlaneTile<D>::BYTES + 16];
+    const int lane = threadIdx.x & 63, g = lane >> 4, G = a.H / a.H_kv;
+    int h_kv, rank;
+    if (!xcd_item(blockIdx.x, a.H_kv, n_inner, a.causal != 0, h_kv, rank)) return;
+    PackedTile t;
+    if (!packed_tile<kRowsPerWg>(a, G, rank, lane, t)) return;
+    const FwdView view{q + (int64_t)t.q_begin * a.q_stride + (int64_t)h_kv * G * D, k + (int64_t)t.k_begin * a.k_stride + (int64_t)h_kv * D,
+                       v + (int64_t)t.k_begin * a.v_stride + (int64_t)h_kv * D, a.q_stride, a.k_stride, a.v_stride, t.n_k - t.n_q, t.n_q * G, t.n_k, a.causal, G};
+    const int r0 = t.tile * kRowsPerWg, rw0 = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32, r = rw0 + (lane & 15);
+    const auto token = [&](int j) { return t.q_begin + (r + 16 * j) / G; };
+    const auto head = [&](int j) { return h_kv * G + (r + 16 * j) % G; };
+    bool finite[2] = {true, true};
+    fwd_f32_body<D, false>(
+        smem, view, DropArgs{}, 0, r0, 0, 1,
+        [&](int j, int db, const f32x4 &val) __attribute__((always_inline)) {
+            *reinterpret_cast<f32x4 *>(out + ((int64_t)token(j) * a.H + head(j)) * D + db * 16 + 4 * g) = val;
+            finite[j] = finite[j] && fabsf(val[0]) < INFINITY && fabsf(val[1]) < INFINITY && fabsf(val[2]) < INFINITY && fabsf(val[3]) < INFINITY;
+        },
+        [&](int j, float v) __attribute__((always_inline)) { lse[(int64_t)head(j) * a.rows_q + token(j)] = v; });
+    // rows with a result that is not finite are done over, over the keys that they see alone (packed_bf16_kernel)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint64_t bad = __ballot(!finite[j]);
+        for (uint32_t rows = (uint32_t)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffffu; rows != 0; rows &= rows - 1) {
+            const int again = rw0 + 16 * j + __builtin_ctz(rows), at = again / G, hd = h_kv * G + again % G;
+            const int seen = a.causal ? max(0, min(t.n_k, t.n_k - t.n_q + at + 1)) : t.n_k;
+            row_attention<float, D>(view.q + (int64_t)at * a.q_stride + again % G * D, view.k, a.k_stride, view.v, a.v_stride, seen, lane,
+                                    [](int i) { return (int64_t)i; }, out + ((int64_t)(t.q_begin + at) * a.H + hd) * D,
+                                    lse + (int64_t)hd * a.rows_q + t.q_begin + at);
         }
     }
 }
@@ -969,6 +1037,20 @@ hipError_t launch_bwd_f32_main(const SegShape &s, const DropArgs &drop, const fl
 {
     if (s.d == 64) return launch_bwd_d<64>(s, drop, q, k, v, lse, dO, dq, dk_part, dv_part, ws, n_splits, st);
     return launch_bwd_d<128>(s, drop, q, k, v, lse, dO, dq, dk_part, dv_part, ws, n_splits, st);
+}
+
+template <int D>
+static hipError_t launch_packed(const PackedArgs &a, const float *q, const float *k, const float *v, float *out, float *lse, hipStream_t st)
+{
+    const int n_inner = packed_tiles(a, kRowsPerWg);
+    TimedLaunch tl(K_PACKED_F32, st);
+    hipLaunchKernelGGL(packed_f32_kernel<D>, dim3((unsigned)xcd_grid(a.H_kv, n_inner)), dim3(256), 0, st, a, q, k, v, out, lse, n_inner);
+    return hipGetLastError();
+}
+
+hipError_t launch_packed_f32(const PackedArgs &a, const float *q, const float *k, const float *v, float *out, float *lse, hipStream_t st)
+{
+    return a.d == 64 ? launch_packed<64>(a, q, k, v, out, lse, st) : launch_packed<128>(a, q, k, v, out, lse, st);
 }
 
 } // namespace lss

@@ -28,6 +28,7 @@
 #include "lss_bf16.h"
 #include <type_traits>
 #include "lss_kernels.h"
+#include "lss_packed_plan.h"
 #include "lss_serve.h"
 
 namespace lss {
@@ -574,10 +575,20 @@ static hipError_t launch_packed(const PackedArgs &a, const bf16_t *q, const bf16
 
 hipError_t launch_packed_bf16(const PackedArgs &a, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse, hipStream_t st)
 {
+    const PackedForm f = pick_packed_form(a.rows_q, a.rows_k, a.B, a.H, a.H_kv, a.d);
+    const auto is = [&](int row_blocks, int groups) { return f.row_blocks == row_blocks && f.groups == groups; };
     if (a.d == 64) {
+        if (is(2, 1)) return launch_packed<64, 2, 1>(a, q, k, v, out, lse, st);
+        if (is(2, 2)) return launch_packed<64, 2, 2>(a, q, k, v, out, lse, st);
+        if (is(4, 2)) return launch_packed<64, 4, 2>(a, q, k, v, out, lse, st);
+        if (is(2, 4)) return launch_packed<64, 2, 4>(a, q, k, v, out, lse, st);
+        if (is(1, 4)) return launch_packed<64, 1, 4>(a, q, k, v, out, lse, st);
         return launch_packed<64, 4, 1>(a, q, k, v, out, lse, st);
     }
-    return launch_packed<128, 8, 1>(a, q, k, v, out, lse, st);
+    if (is(2, 2)) return launch_packed<128, 2, 2>(a, q, k, v, out, lse, st);
+    if (is(4, 2)) return launch_packed<128, 4, 2>(a, q, k, v, out, lse, st);
+    if (is(8, 1)) return launch_packed<128, 8, 1>(a, q, k, v, out, lse, st);
+    return launch_packed<128, 4, 1>(a, q, k, v, out, lse, st);
 }
 
 } // namespace lss

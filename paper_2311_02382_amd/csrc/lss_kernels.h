@@ -110,7 +110,7 @@ hipError_t allow_lds(K kernel, int bytes, DeviceOnce &once)
 enum KernelId { K_FWD_F32 = 0, K_FWD_MERGE, K_ROWDOT, K_BWD_MAIN_F32, K_DQ_MERGE, K_REDUCE, K_BWD_MAIN_BF16, K_PROJ_FWD, K_PROJ_BWD,
                 K_PE_FWD, K_PE_BWD, K_LN_FWD, K_LN_BWD, K_LN_PARAMS, K_GELU_FWD, K_GELU_BWD, K_LINEAR_FWD, K_LINEAR_BWD, K_RESIDUAL, K_LINEAR_WGRAD,
                 K_FWD_BF16, K_BWD_PREP_BF16, K_BWD_SKINNY_BF16, K_LN_BWD_SHORT, K_PROJ_FWD_SMALL, K_PROJ_BWD_SMALL, K_LINEAR_FWD_SMALL,
-                K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_ATTN, K_PACKED_BF16, K_COUNT };
+                K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_BF16, K_PACKED_F32, K_COUNT };
 void timing_begin(int id, hipStream_t st);
 void timing_end(int id, hipStream_t st);
 struct TimedLaunch {    // RAII bracket around one kernel launch
@@ -170,7 +170,7 @@ hipError_t launch_layernorm_bwd(const bf16_t *x, const float *gamma, const float
 hipError_t launch_gelu_fwd(const bf16_t *u, int64_t n, bf16_t *g, hipStream_t st);
 hipError_t launch_gelu_bwd(const bf16_t *u, const bf16_t *dg, int64_t n, bf16_t *du, hipStream_t st);
 
-// the paged cache (lss_paged.hip, lss_decode.hip) and packed sequences (lss_packed.hip); int32 arrays are device memory, strides count elements
+// the paged cache (lss_paged.hip, lss_decode.hip) and packed sequences (lss_fwd_bf16.hip, lss_f32.hip); int32 arrays are device memory, strides count elements
 struct PageTable {
     const int32_t *table;       // [B, max_pages]
     int n_pages, page_shift, max_pages;
@@ -204,7 +204,6 @@ inline int packed_tiles(const PackedArgs &a, int rows)
     return (int)((int64_t)a.rows_q * (a.H / a.H_kv) / rows) + (a.B <= 64 && a.rows_q < a.B ? a.rows_q : a.B);
 }
 hipError_t launch_packed_bf16(const PackedArgs &a, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse, hipStream_t st);
-template <typename T>
-hipError_t launch_packed_attn(const PackedArgs &a, const T *q, const T *k, const T *v, T *out, float *lse, hipStream_t st);
+hipError_t launch_packed_f32(const PackedArgs &a, const float *q, const float *k, const float *v, float *out, float *lse, hipStream_t st);
 
 } // namespace lss

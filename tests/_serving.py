@@ -1,7 +1,10 @@
 """The serving operators' definitions in 64 bits (CPU) and error bounds of their results, for the tests of those operators."""
+import ctypes
 import math
 
 import torch
+
+from paper_2311_02382_amd import lss
 
 HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}      # half a step of the type, relative to the value
 DTYPES = [torch.bfloat16, torch.float32]
@@ -62,10 +65,10 @@ def attention(q, k, v, seen, dtype):
     q, k, v = q.double(), k.double(), v.double()
     n, d = k.shape
     score = q @ k.T / math.sqrt(d)
-    hidden = torch.arange(n) >= seen[:, None]
-    size = (q.abs() @ k.abs().T / math.sqrt(d)).masked_fill(hidden, 0.0).amax(-1) if n else torch.zeros(len(q), dtype=torch.float64)
+    hidden = torch.arange(n, device=q.device) >= seen[:, None]
+    size = (q.abs() @ k.abs().T / math.sqrt(d)).masked_fill(hidden, 0.0).amax(-1) if n else torch.zeros(len(q), dtype=torch.float64, device=q.device)
     score = score.masked_fill(hidden, -math.inf)
-    lse = torch.logsumexp(score, -1) if n else torch.full((len(q),), -math.inf, dtype=torch.float64)
+    lse = torch.logsumexp(score, -1) if n else torch.full((len(q),), -math.inf, dtype=torch.float64, device=q.device)
     weight = (score - lse[:, None]).exp().masked_fill(hidden, 0.0)
     out, absolute = weight @ v, weight @ v.abs()
     each = (d + 2) * 2.0 ** -24 * size + 2.0 ** -21 + (n + 8) * 2.0 ** -24
@@ -85,3 +88,10 @@ def check(got, want, bound, what):
 
 def bits(t):
     return t.contiguous().view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32).cpu()
+
+
+def packed_form(rows_q, rows_k, B, H, H_kv, d):
+    """(blocks of 32 rows, groups of wavefronts) of a packed bf16 launch's workgroups (csrc/lss_plan.h)"""
+    plan = (ctypes.c_int * 2)()
+    lss._check(lss.load().lss_plan_packed(*map(ctypes.c_int64, (rows_q, rows_k, B, H, H_kv, d)), plan))
+    return tuple(plan)

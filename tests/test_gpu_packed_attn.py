@@ -9,13 +9,14 @@ pytestmark = pytest.mark.gpu
 
 
 def _want(q, k, v, cu_q, cu_k, causal):
+    """The definition, where q, k and v are"""
     rows, H, d = q.shape
     H_kv = k.shape[1]
-    out, lse, ob, lb = (torch.zeros(s, dtype=torch.float64) for s in ((rows, H, d), (H, rows), (rows, H, d), (H, rows)))
+    out, lse, ob, lb = (torch.zeros(s, dtype=torch.float64, device=q.device) for s in ((rows, H, d), (H, rows), (rows, H, d), (H, rows)))
     for b in range(len(cu_q) - 1):
         mq, mk = slice(int(cu_q[b]), int(cu_q[b + 1])), slice(int(cu_k[b]), int(cu_k[b + 1]))
         n_q, n_k = mq.stop - mq.start, mk.stop - mk.start
-        seen = (n_k - n_q + 1 + torch.arange(n_q)).clamp(0, n_k) if causal else torch.full((n_q,), n_k)
+        seen = ((n_k - n_q + 1 + torch.arange(n_q)).clamp(0, n_k) if causal else torch.full((n_q,), n_k)).to(q.device)
         for h in range(H):
             g = h // (H // H_kv)
             out[mq, h], lse[h, mq], ob[mq, h], lb[h, mq] = sv.attention(q[mq, h], k[mk, g], v[mk, g], seen, q.dtype)
@@ -62,6 +63,34 @@ def test_longer_prompts(dtype, n_q, H, H_kv, d):
 def test_rows_behind_keys_that_are_there_and_rows_that_see_none(dtype, causal, d):
     # continued prompts; more rows than keys: the first rows see no key; no keys at all; keys without rows
     _run([1, 5, 130, 70, 90, 12, 0, 64], 4, 2, d, dtype, n_k=[300, 69, 131, 500, 40, 0, 77, 64], causal=causal, seed=80)
+
+
+def _some(n, B, seed):
+    return [int(x) for x in torch.randint(n // 2, n + n // 2, (B,), generator=torch.Generator().manual_seed(seed))]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("form,n_q,old,H,H_kv,d", [
+    ((4, 1), _some(200, 40, 1), 0, 16, 8, 64), ((4, 2), [500, 701], 3700, 32, 8, 64), ((2, 1), _some(100, 5, 2), 0, 4, 2, 64), ((1, 4), [700], 33, 2, 2, 64),
+    ((2, 4), [1301], 1234, 8, 8, 64), ((2, 2), [600, 901, 700], 0, 8, 4, 64), ((4, 1), _some(200, 40, 3), 0, 16, 8, 128), ((8, 1), [4203], 0, 32, 8, 128),
+    ((4, 2), [500, 701], 3700, 32, 8, 128), ((2, 2), [300, 901], 100, 6, 2, 128), ((4, 1), _some(100, 70, 4), 0, 5, 1, 64)])
+def test_every_form_of_workgroup(form, n_q, old, H, H_kv, d, causal):
+    n_k = [n + old for n in n_q]
+    assert sv.packed_form(sum(n_q), sum(n_k), len(n_q), H, H_kv, d) == form
+    q, k, v = (x.cuda() for x in _tensors(n_q, n_k, H, H_kv, d, torch.bfloat16, 150))
+    cu_q, cu_k = sv.starts(n_q), sv.starts(n_k)
+    out, lse = lss.lss_packed_attn_fwd(q, k, v, cu_q.cuda(), cu_k.cuda(), causal=causal)
+    want, want_lse, ob, lb = (x.cpu() for x in _want(q, k, v, cu_q, cu_k, causal))
+    sv.check(out, want, ob, "out")
+    sv.check(lse, want_lse, lb, "lse")
+    # a value that is not finite in the last sequence's middle: the rows in front of it
+    at = sum(n_k) - n_k[-1] + old + n_q[-1] // 2
+    v[at] = float("nan")
+    again, lse_again = lss.lss_packed_attn_fwd(q, k, v, cu_q.cuda(), cu_k.cuda(), causal=causal)
+    sees = sum(n_q) - n_q[-1] + (n_q[-1] // 2 if causal else 0)
+    sv.check(again[:sees], want[:sees], ob[:sees], "out in front")
+    sv.check(lse_again, want_lse, lb, "lse with it")
+    assert bool(torch.isnan(again[sees:]).all())
 
 
 def test_many_sequences():
