@@ -62,8 +62,9 @@ struct FwdView {
 // 1 / (1 - p) according to drop_keep() of (seed, batch*head, global row, key); row sum and lse are
 // those of the softmax.
 // The rows r0 .. of a workgroup: put(u, values) takes columns 8 u + 4 (lane / 32) .. + 3 of row r0 + 32 (wavefront) + lane % 32, normalised,
-// put_lse its lse.  `bh`: batch * head for the dropout's decisions.
-template <int D, bool DROP, int RB, int KG, typename Put, typename PutLse>
+// put_lse its lse.  `bh`: batch * head for the dropout's decisions.  PACKED: G heads of a token, K's and V's rows each with a distance of their own,
+// perhaps more rows than keys (a segment has none of that, and what is not there costs its kernels nothing: 1.2 % of lx24k's last segment).
+template <int D, bool DROP, int RB, int KG, bool PACKED, typename Put, typename PutLse>
 __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, const DropArgs &dr, int bh, int r0, int split, int n_splits, Put &&put,
                                               PutLse &&put_lse)
 {
@@ -78,7 +79,9 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
     const int rw0 = r0 + wave * C::RW;                  // first row of this wavefront
 
     const int r_last = min(r0 + C::BR, s.l_s) - 1;
-    const int kv_end = s.causal ? (int)max<int64_t>(min<int64_t>(s.l_x, s.s0 + r_last / s.G + 1), 0) : s.l_x;
+    const int G = PACKED ? s.G : 1;
+    int kv_end = s.causal ? (int)min<int64_t>(s.l_x, s.s0 + r_last / G + 1) : s.l_x;
+    if (PACKED) kv_end = max(kv_end, 0);                // (more rows than keys: the first ones see none)
     const int n_tiles = (kv_end + C::BC - 1) / C::BC;
     const int per = (n_tiles + n_splits - 1) / n_splits;
     const int s_begin = split * per, s_tiles = max(min(n_tiles, s_begin + per) - s_begin, 0);
@@ -90,11 +93,11 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
     // (unconditional loads), are computed like any other and never stored
     const int r = rw0 + lq;
     const bool row_ok = r < s.l_s;
-    const int position = (int)s.s0 + r / s.G;
+    const int position = (int)s.s0 + r / G;
     Frag<bf16_t> qf[NU];
     {
         const int rr = min(r, s.l_s - 1);
-        const bf16_t *qp = s.q + (int64_t)(rr / s.G) * s.q_ld + (rr % s.G) * D + hh * 8;
+        const bf16_t *qp = s.q + (int64_t)(rr / G) * s.q_ld + (rr % G) * D + hh * 8;
 #pragma unroll
         for (int kb = 0; kb < NU; ++kb) qf[kb] = load_frag<bf16_t>(qp + kb * 16);
     }
@@ -117,34 +120,39 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
         // ---- tile loads, by all wavefronts of the group.  No branch and few scalar instructions on purpose: a branch inside a
         // pipeline step splits it into basic blocks, and the vector work that was meant to sit between the step's matrix
         // instructions is then moved behind the branch in one lump; addresses move on between the iterations instead.
-        uint32_t offK[Tile::NI], offV[Tile::NI], offDK[Tile::NI], offDV[Tile::NI];     // this lane's global offsets within the next K and V
-        const int t_part = s.l_x % C::BC ? s.l_x / C::BC : -1;     // tile; and what must be added to them in the sequence's last, partial tile
-        auto tile_offsets = [&](uint32_t (&off)[Tile::NI], uint32_t (&offD)[Tile::NI], int64_t ld) __attribute__((always_inline)) {
-            uint32_t offL[Tile::NI];                                // (rows past the end re-read the last row)
-            Tile::pair_offsets(off, ld, C::BC, wave, lane);
-            Tile::pair_offsets(offL, ld, t_part >= 0 ? s.l_x % C::BC : C::BC, wave, lane);
+        uint32_t offK[Tile::NI], offV[Tile::NI], offD[Tile::NI];    // this lane's global offsets within the next K and V tile; and
+        Tile::pair_offsets(offK, s.k_ld, C::BC, wave, lane);        // what must be added to them in the sequence's last, partial
+        const int t_part = s.l_x % C::BC ? s.l_x / C::BC : -1;     // tile (rows past the end re-read the last row)
+        uint32_t offDV[PACKED ? Tile::NI : 1];                      // ... V's, where its rows are not as far apart as K's
+        {
+            uint32_t offL[Tile::NI];
+            Tile::pair_offsets(offL, s.k_ld, t_part >= 0 ? s.l_x % C::BC : C::BC, wave, lane);
 #pragma unroll
-            for (int i = 0; i < Tile::NI; ++i) offD[i] = offL[i] - off[i];
-        };
-        tile_offsets(offK, offDK, s.k_ld);
-        tile_offsets(offV, offDV, s.v_ld);
-        const uint32_t k_bytes = (uint32_t)(C::BC * s.k_ld * 2), v_bytes = (uint32_t)(C::BC * s.v_ld * 2);
+            for (int i = 0; i < Tile::NI; ++i) { offD[i] = offL[i] - offK[i]; offV[i] = offK[i]; }
+            if constexpr (PACKED) {
+                Tile::pair_offsets(offV, s.v_ld, C::BC, wave, lane);
+                Tile::pair_offsets(offL, s.v_ld, t_part >= 0 ? s.l_x % C::BC : C::BC, wave, lane);
+#pragma unroll
+                for (int i = 0; i < Tile::NI; ++i) offDV[i] = offL[i] - offV[i];
+            }
+        }
+        const uint32_t k_bytes = (uint32_t)(C::BC * s.k_ld * 2), v_bytes = PACKED ? (uint32_t)(C::BC * s.v_ld * 2) : k_bytes;
         // the next tile of K to load, and of V, one behind; past the group's last one that one again
         const int t_last = t_begin + max(T, 1) - 1;
         int k_tile_next = t_begin, v_tile_next = t_begin;
         const char *k_next = tile_ptr(Tile::pair_base(s.k), t_begin, k_bytes), *v_next = tile_ptr(Tile::pair_base(s.v), t_begin, v_bytes);
-        auto to_part = [&](int t, uint32_t (&off)[Tile::NI], const uint32_t (&offD)[Tile::NI]) __attribute__((always_inline)) {
+        auto to_part = [&](int t, uint32_t (&off)[Tile::NI], bool of_v) __attribute__((always_inline)) {
             if (t == t_part)
 #pragma unroll
-                for (int i = 0; i < Tile::NI; ++i) off[i] += offD[i];
+                for (int i = 0; i < Tile::NI; ++i) off[i] += PACKED && of_v ? offDV[PACKED ? i : 0] : offD[i];
         };
-        to_part(k_tile_next, offK, offDK);
-        to_part(v_tile_next, offV, offDV);
+        to_part(k_tile_next, offK, false);
+        to_part(v_tile_next, offV, true);
         auto advance_k = [&] {
-            if (k_tile_next < t_last) { ++k_tile_next; k_next += k_bytes; to_part(k_tile_next, offK, offDK); }
+            if (k_tile_next < t_last) { ++k_tile_next; k_next += k_bytes; to_part(k_tile_next, offK, false); }
         };
         auto advance_v = [&] {
-            if (v_tile_next < t_last) { ++v_tile_next; v_next += v_bytes; to_part(v_tile_next, offV, offDV); }
+            if (v_tile_next < t_last) { ++v_tile_next; v_next += v_bytes; to_part(v_tile_next, offV, true); }
         };
         // Iteration t's loads, behind its barrier: K of tile t + 2 in the place of tile t's, whose last rows have been read
         // by then, and V of tile t + 1 in the place of tile t - 1's.  (Past the end a tile is loaded once more: K where it
@@ -183,7 +191,7 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
         // 0: keys after the lane's row, and keys past the sequence (whose loads re-read its last
         // row).  C-tile element e of this lane is key 8*(e/4) + 4*hh + e%4 of the block.
         // (positions are below 2^30, checked on the host: one 32-bit scalar compare, no vector work per step)
-        const int last_whole = min(s.causal ? (int)s.s0 + rw0 / s.G - 31 : s.l_x, s.l_x - 32);       // blocks from here on need no mask
+        const int last_whole = min(s.causal ? (int)s.s0 + rw0 / G - 31 : s.l_x, s.l_x - 32);       // blocks from here on need no mask
         auto mask_s = [&](int jb, f32x16 &sc) __attribute__((always_inline)) {
             if (jb > last_whole) {
                 const int last = s.causal ? min(position, s.l_x - 1) : s.l_x - 1;
@@ -474,7 +482,7 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void fwd_bf16_kernel
     // this lane's row of the result (a split's normalised output travels to the merge kernel in fp32: rounded to bf16 once, there)
     const int lane = threadIdx.x & 63, r = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % RB * C::RW + (lane & 31), hh = lane >> 5;
     const int64_t part_row = ((int64_t)split * bhs + bh) * s.l_s + r;
-    fwd_bf16_body<D, DROP, RB, KG>(
+    fwd_bf16_body<D, DROP, RB, KG, false>(
         smem, view, dr, bh, r0, split, n_splits,
         [&](int u, const f32x4 &val) __attribute__((always_inline)) {
             if (n_splits == 1)
@@ -508,7 +516,7 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void packed_bf16_ker
     const int token = t.q_begin + r / G, h = h_kv * G + r % G;
     bf16_t *const row = out + ((int64_t)token * a.H + h) * D;
     bool finite = true;
-    fwd_bf16_body<D, false, RB, KG>(
+    fwd_bf16_body<D, false, RB, KG, true>(
         smem, view, DropArgs{}, 0, r0, 0, 1,
         [&](int u, const f32x4 &val) __attribute__((always_inline)) {
             *reinterpret_cast<bf16x4 *>(row + 8 * u + 4 * hh) = pack4(val[0], val[1], val[2], val[3]);
