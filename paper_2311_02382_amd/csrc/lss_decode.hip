@@ -24,8 +24,17 @@ namespace lss {
 
 namespace {
 
-constexpr int kWaves = 4, kParts = 512;                 // workgroups that share the rounds
-constexpr int kWholeLen = 512;
+constexpr int kWaves = 4, kWholeLen = 512;
+
+// Where a call's keys and values are more than half the last-level cache, they pass it by (non-temporal loads): 2.07 GB 366 -> 335 us, 268 MB 52 -> 47; but
+// 76 MB, of which two other calls' worth fits beside them, 17 -> 20.
+constexpr int64_t kStreamBytes = (int64_t)128 << 20;
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load16(const V *p)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load(p);
+    else return *p;
+}
 
 // how a tile's keys and values meet the matrix cores
 template <typename T, int D> struct Step;
@@ -43,11 +52,12 @@ template <int D> struct Step<bf16_t, D> {
             if (there) q.f[i] = load_frag<bf16_t>(row + 32 * i + 8 * g);
         }
     }
-    // half i of a tile: 16 keys from `row` (this lane's key's row)
-    static __device__ __forceinline__ void load_keys(Keys &k, int i, const bf16_t *row, int g)
+    // half i of a tile: 16 keys from `first` on, this lane's 16 bytes of the first step at lane_offset
+    template <bool STREAM>
+    static __device__ __forceinline__ void load_keys(Keys &k, int i, const char *first, uint32_t lane_offset)
     {
 #pragma unroll
-        for (int j = 0; j < NQ_FRAGS; ++j) k.f[i][j] = load_frag<bf16_t>(row + 32 * j + 8 * g);
+        for (int j = 0; j < NQ_FRAGS; ++j) k.f[i][j].v = load16<STREAM>(reinterpret_cast<const Vec *>(first + lane_offset + 64 * j));
     }
     // element e of half i: key 16 i + 4 (l / 16) + e, query l % 16
     static __device__ __forceinline__ f32x4 scores(const Keys &k, int i, const Queries &q)
@@ -99,10 +109,11 @@ template <int D> struct Step<float, D> {
             if (there) q.f[i] = *reinterpret_cast<const f32x4 *>(row + 16 * i + 4 * g);
         }
     }
-    static __device__ __forceinline__ void load_keys(Keys &k, int i, const float *row, int g)
+    template <bool STREAM>
+    static __device__ __forceinline__ void load_keys(Keys &k, int i, const char *first, uint32_t lane_offset)
     {
 #pragma unroll
-        for (int j = 0; j < NQ_FRAGS; ++j) k.f[i][j] = *reinterpret_cast<const f32x4 *>(row + 16 * j + 4 * g);
+        for (int j = 0; j < NQ_FRAGS; ++j) k.f[i][j] = load16<STREAM>(reinterpret_cast<const Vec *>(first + lane_offset + 64 * j));
     }
     static __device__ __forceinline__ f32x4 scores(const Keys &k, int i, const Queries &q)
     {
@@ -141,94 +152,82 @@ __device__ __forceinline__ int rounds_of(const DecodeArgs &a, int b)
 {
     return (max(1, min(a.lengths[b], a.max_len)) + ROUND - 1) / ROUND;
 }
-__device__ __forceinline__ int64_t wave_sum_i64(int64_t x)
-{
-#pragma unroll
-    for (int sh = 32; sh >= 1; sh >>= 1) x += __shfl_xor(x, sh);
-    return x;
-}
-// rounds of all sequences, per virtual head; by a whole wavefront
+// by whole wavefronts, 64 sequences at a time (a round is 64 tokens at least: 64 sequences have fewer than 2^31): rounds of all sequences, per virtual
+// head, ...
 template <int ROUND>
 __device__ __forceinline__ int64_t all_rounds(const DecodeArgs &a, int lane)
 {
     int64_t sum = 0;
-    for (int b = lane; b < a.B; b += 64) sum += rounds_of<ROUND>(a, b);
-    return wave_sum_i64(sum);
+    for (int b0 = 0; b0 < a.B; b0 += 64)
+        sum += __builtin_amdgcn_readlane(lane_sum_scan(b0 + lane < a.B ? rounds_of<ROUND>(a, b0 + lane) : 0), 63);
+    return sum;
 }
-// the sequence that round `at` belongs to (rounds counted per virtual head: at < all_rounds), and the rounds in front of it
+// ... and the sequence that round `at` of those belongs to, with the rounds in front of it
 template <int ROUND>
 __device__ __forceinline__ int sequence_at(const DecodeArgs &a, int64_t at, int lane, int64_t &before)
 {
     before = 0;
     for (int b0 = 0;; b0 += 64) {
-        int64_t upto = b0 + lane < a.B ? rounds_of<ROUND>(a, b0 + lane) : 0;
-        const int64_t mine = upto;
-#pragma unroll
-        for (int sh = 1; sh < 64; sh <<= 1) {
-            const int64_t other = __shfl_up(upto, sh);
-            if (lane >= sh) upto += other;
-        }
+        const int mine = b0 + lane < a.B ? rounds_of<ROUND>(a, b0 + lane) : 0, upto = lane_sum_scan(mine);
         const uint64_t past = __ballot(before + upto > at);
         if (past != 0) {
             const int l = __ffsll((long long)past) - 1;
-            before += __shfl(upto - mine, l);
+            before += __builtin_amdgcn_readlane(upto - mine, l);
             return b0 + l;
         }
-        before += __shfl(upto, 63);
+        before += __builtin_amdgcn_readlane(upto, 63);
         if (b0 + 64 >= a.B) return a.B - 1;
     }
 }
-__device__ __forceinline__ int64_t scalar(int64_t x)
-{
-    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) | (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
-}
-
-// What a part of a sequence leaves in scratch memory, for its query n of `rows`: sum of weight * value [d], then maximum (log2 domain) and sum
+// Scratch memory.  What a part of a sequence leaves there for its query n of `rows`: sum of weight * value [d], maximum (log2 domain) and sum.  A
+// workgroup has room for two parts: 2 w for its first and, if it begins there, 2 w + 1 for its last.  And for the joining launch, the sequences that
+// more than one workgroup has: by sequence and virtual head where those are not more than the workgroups, else by the workgroup that one begins in (as
+// its last: there is one at most).
+struct Chain { int b, v_head, w, count; };              // b < 0: none; it begins in part w and has `count` parts, one per workgroup
 struct Scratch {
     float *base;
-    int rows, d;
-    __device__ __forceinline__ float *values(int part, int n) const { return base + ((int64_t)part * rows + n) * d; }
-    __device__ __forceinline__ float *sums(int part, int n) const { return base + (int64_t)2 * kParts * rows * d + ((int64_t)part * rows + n) * 2; }
+    int rows, d, parts;     // workgroups
+    __device__ __forceinline__ Chain *chain(int i) const { return reinterpret_cast<Chain *>(base) + i; }
+    __device__ __forceinline__ float *sums(int part, int n) const { return base + 4 * parts + ((int64_t)part * rows + n) * 2; }
+    __device__ __forceinline__ float *values(int part, int n) const { return base + 4 * parts + (int64_t)2 * parts * rows * 2 + ((int64_t)part * rows + n) * d; }
+};
+size_t scratch_bytes(int rows, int d, int parts) { return sizeof(float) * (4 * parts + (size_t)2 * parts * rows * (d + 2)); }
+
+// a / b in 32 bits where both fit (a fifth of the instructions); wavefront-uniform
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b)
+{
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// workgroups that share the rounds: as many as there is room for at once
+constexpr int parts_of(int elem_bytes, int d, int nq) { return 256 * (d == 64 ? (nq == 1 ? 4 : 3) : nq == 1 || elem_bytes == 2 ? 2 : 1); }
+template <typename T, int D> struct Decode {
+    static constexpr int ROUND = kWaves * Step<T, D>::TILE, ROW_STRIDE = D + 4;       // (16 bytes more: rows of the joining start in other banks)
+    static constexpr int TILE_BYTES = Step<T, D>::TILE * D * (int)sizeof(T), JOIN_BYTES = 16 * ROW_STRIDE * 4;
+    static constexpr int REGION = TILE_BYTES > JOIN_BYTES ? TILE_BYTES : JOIN_BYTES;
 };
 
-template <typename T, int D, int NQ>
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_decode_kernel(DecodeArgs a, const T *__restrict__ q, const T *__restrict__ k_cache,
-                                                                      const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,
-                                                                      float *__restrict__ scratch, int whole)
+// Rounds at .. end - 1, the first of which is of sequence b and virtual head v_head; `base`: the first of (b, virtual head 0).  WHOLE: all of (b, v_head).
+template <typename T, int D, int NQ, bool STREAM>
+__device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, float (&sums)[kWaves][2][16], const T *__restrict__ q,
+                                              const T *__restrict__ k_cache, const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,
+                                              float *__restrict__ scratch, bool whole, int64_t at, int64_t end, int64_t share, int64_t base, int b, int v_head)
 {
+    typedef Decode<T, D> C;
     typedef Step<T, D> S;
     typedef typename S::Vec Vec;
-    constexpr int TILE = S::TILE, HALVES = TILE / 16, ROUND = kWaves * TILE, ROW_STRIDE = D + 4;       // (16 bytes more: rows of the joining start in other banks)
-    constexpr int REGION = 16 * ROW_STRIDE * 4 > TILE * D * (int)sizeof(T) ? 16 * ROW_STRIDE * 4 : TILE * D * (int)sizeof(T);
-    __shared__ __attribute__((aligned(1024))) char smem[kWaves * REGION];
-    __shared__ float sums[kWaves][2][16];               // maximum, sum
+    constexpr int TILE = S::TILE, HALVES = TILE / 16, ROUND = C::ROUND, ROW_STRIDE = C::ROW_STRIDE, REGION = C::REGION;
     const int tid = threadIdx.x, lane = tid & 63, lq = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     char *const mine = smem + wave * REGION;
     const int G = a.H / a.H_kv, groups = (G + 16 * NQ - 1) / (16 * NQ), v_heads = a.H_kv * groups;
-    const Scratch parts{scratch, min(G, 16 * NQ), D};
-    const int64_t ld = (int64_t)a.H_kv * D;
+    constexpr int PARTS = parts_of(sizeof(T), D, NQ);
+    const Scratch parts{scratch, min(G, 16 * NQ), D, PARTS};
+    const bool by_item = (int64_t)a.B * v_heads <= PARTS;
+    // (a page is at most 2^29 elements: what lies within 16 rows of one is 32 bits away)
+    const int64_t row_bytes = (int64_t)a.H_kv * D * (int)sizeof(T);
+    const uint32_t k_lane = (uint32_t)lq * (uint32_t)row_bytes + 16 * g, v_lane = (uint32_t)(lane / S::CHUNKS) * (uint32_t)row_bytes + lane % S::CHUNKS * 16;
     const float c = kLog2e / sqrtf((float)D);
-
-    int64_t at, end, share = 0;                         // rounds of all sequences and virtual heads
-    int b, v_head;
-    int64_t base = 0;                                   // first round of (b, virtual head 0)
-    if (whole) {
-        b = blockIdx.x / v_heads;
-        v_head = blockIdx.x % v_heads;
-        at = 0;
-        end = 1;                                        // (one piece)
-    } else {
-        const int64_t all = scalar(all_rounds<ROUND>(a, lane)) * v_heads;
-        share = (all + kParts - 1) / kParts;
-        at = blockIdx.x * share;
-        end = min(at + share, all);
-        if (at >= end) return;
-        int64_t before;
-        b = __builtin_amdgcn_readfirstlane(sequence_at<ROUND>(a, at / v_heads, lane, before));
-        base = scalar(before) * v_heads;
-        v_head = (int)((at - base) / rounds_of<ROUND>(a, b));
-    }
     const int64_t start = at;
     while (at < end) {
         const int n = max(0, min(a.lengths[b], a.max_len)), R = rounds_of<ROUND>(a, b);
@@ -256,7 +255,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_decode_kernel(DecodeArgs
         int window_at = j0 >> a.pt.page_shift;
         const auto numbers = [&](int from) { return table[min(from + lane, a.pt.max_pages - 1)]; };
         int window = numbers(window_at), next_window = numbers(window_at + 64);
-        const T *const k_head = k_cache + (int64_t)h_kv * D, *const v_head_base = v_cache + (int64_t)h_kv * D;
+        const char *const k_head = reinterpret_cast<const char *>(k_cache + (int64_t)h_kv * D), *const v_head_base = reinterpret_cast<const char *>(v_cache + (int64_t)h_kv * D);
 
         typename S::Keys keys;
         Vec values[S::V_LOADS];
@@ -267,7 +266,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_decode_kernel(DecodeArgs
                 window = next_window;
                 next_window = numbers(window_at + 64);
             }
-            const T *k_row[HALVES], *v_row[HALVES];
+            const char *k_row[HALVES], *v_row[HALVES];
 #pragma unroll
             for (int i = 0; i < HALVES; ++i) {
                 const int nth = (j + 16 * i) >> a.pt.page_shift;
@@ -276,15 +275,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_decode_kernel(DecodeArgs
                 if (nth - window_at >= 64) page = __builtin_amdgcn_readlane(next_window, 0);
                 ok[i] = (uint32_t)page < (uint32_t)a.pt.n_pages && j + 16 * i < j_end;
                 const int64_t row = ((int64_t)(ok[i] ? page : 0) << a.pt.page_shift) + ((j + 16 * i) & ((1 << a.pt.page_shift) - 1));
-                k_row[i] = k_head + row * ld;
-                v_row[i] = v_head_base + row * ld;
+                k_row[i] = k_head + row * row_bytes;
+                v_row[i] = v_head_base + row * row_bytes;
             }
 #pragma unroll
-            for (int i = 0; i < HALVES; ++i) S::load_keys(keys, i, k_row[i] + lq * (int)ld, g);
+            for (int i = 0; i < HALVES; ++i) S::template load_keys<STREAM>(keys, i, k_row[i], k_lane);
 #pragma unroll
             for (int i = 0; i < S::V_LOADS; ++i) {
-                const int row = (i * 64 + lane) / S::CHUNKS, half = i * 64 / S::CHUNKS / 16;
-                values[i] = *reinterpret_cast<const Vec *>(v_row[half] + (row & 15) * (int)ld + (lane % S::CHUNKS) * (16 / (int)sizeof(T)));
+                const int row = i * 64 / S::CHUNKS;        // (of lane 0)
+                values[i] = load16<STREAM>(reinterpret_cast<const Vec *>(v_row[row / 16] + (row & 15) * row_bytes + v_lane));
             }
         };
         if (j0 < j_end) load(j0);
@@ -386,6 +385,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_decode_kernel(DecodeArgs
             __syncthreads();
         }
         if (whole) return;
+        if (r0 == 0 && tid == 0 && (by_item || r1 < R))
+            *parts.chain(by_item ? b * v_heads + v_head : blockIdx.x) = {r1 < R ? b : -1, v_head, 2 * (int)blockIdx.x + (at == start ? 0 : 1),
+                                                                         1 + (int)divide(R - r1 + share - 1, share)};
         at = first + r1;
         if (r1 == R && ++v_head == v_heads) {
             base += (int64_t)R * v_heads;
@@ -395,56 +397,90 @@ __global__ __launch_bounds__(64 * kWaves, 2) void paged_decode_kernel(DecodeArgs
     }
 }
 
-// Joins the parts of the sequences that more than one workgroup had rounds of, in their order; a workgroup per sequence and query head.  Thread: four
-// columns of every eighth (sixteenth at d = 64) part.
-template <typename T, int D, int ROUND>
-__global__ __launch_bounds__(256) void decode_merge_kernel(DecodeArgs a, const float *__restrict__ scratch, int nq, T *__restrict__ out, float *__restrict__ lse)
+template <typename T, int D, int NQ>
+__global__ __launch_bounds__(64 * kWaves, parts_of(sizeof(T), D, NQ) / 256) void paged_decode_kernel(DecodeArgs a, const T *__restrict__ q, const T *__restrict__ k_cache,
+                                                                      const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,
+                                                                      float *__restrict__ scratch, int whole)
 {
-    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
-    __shared__ float4 acc[GROUPS][LANES];
+    typedef Decode<T, D> C;
+    constexpr int PARTS = parts_of(sizeof(T), D, NQ);
+    __shared__ __attribute__((aligned(1024))) char smem[kWaves * C::REGION];
+    __shared__ float sums[kWaves][2][16];               // maximum, sum
+    const int lane = threadIdx.x & 63;
+    const int G = a.H / a.H_kv, groups = (G + 16 * NQ - 1) / (16 * NQ), v_heads = a.H_kv * groups;
+    int64_t at = 0, end = 1, share = 0, base = 0, bytes;
+    int b, v_head;
+    if (whole) {
+        b = blockIdx.x / v_heads;
+        v_head = blockIdx.x % v_heads;
+        bytes = (int64_t)a.B * a.max_len * a.H_kv * (2 * D * (int)sizeof(T));
+    } else {
+        const int64_t rounds = all_rounds<C::ROUND>(a, lane), all = rounds * v_heads;
+        bytes = rounds * a.H_kv * (C::ROUND * 2 * D * (int)sizeof(T));
+        share = (all + PARTS - 1) / PARTS;
+        at = blockIdx.x * share;
+        end = min(at + share, all);
+        if (threadIdx.x == 0 && (int64_t)a.B * v_heads > PARTS) Scratch{scratch, 0, D, PARTS}.chain(blockIdx.x)->b = -1;
+        if (at >= end) return;
+        int64_t before;
+        b = sequence_at<C::ROUND>(a, divide(at, v_heads), lane, before);
+        base = before * v_heads;
+        v_head = (int)divide(at - base, rounds_of<C::ROUND>(a, b));
+    }
+    if (bytes >= kStreamBytes) decode_rounds<T, D, NQ, true>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, whole, at, end, share, base, b, v_head);
+    else decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, whole, at, end, share, base, b, v_head);
+}
+
+// Joins the parts of the sequences that more than one workgroup had rounds of, in their order: workgroup x those of chain x, queries y, y + gridDim.y ..
+// Thread: four columns of every (THREADS / (D / 4))th part.
+template <typename T, int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void decode_merge_kernel(DecodeArgs a, const float *__restrict__ scratch, int nq, int n_parts, T *__restrict__ out,
+                                                               float *__restrict__ lse)
+{
+    constexpr int LANES = D / 4, GROUPS = THREADS / LANES;
+    __shared__ f32x4 acc[GROUPS][LANES];
     __shared__ float totals[GROUPS];
-    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x / a.H, h = blockIdx.x % a.H;
-    const int G = a.H / a.H_kv, groups = (G + 16 * nq - 1) / (16 * nq), v_heads = a.H_kv * groups;
-    const Scratch parts{const_cast<float *>(scratch), min(G, 16 * nq), D};
-    const int v_head = h / G * groups + h % G / (16 * nq), n = h % G % (16 * nq);
-    const int64_t all = all_rounds<ROUND>(a, lane) * v_heads, share = (all + kParts - 1) / kParts;
-    int64_t before = 0;
-    for (int i = lane; i < b; i += 64) before += rounds_of<ROUND>(a, i);
-    before = wave_sum_i64(before);
-    const int R = rounds_of<ROUND>(a, b);
-    const int64_t first = before * v_heads + (int64_t)v_head * R, last = first + R - 1;
-    const int w0 = (int)(first / share), w1 = (int)(last / share);
-    if (w0 == w1) return;
-    const auto part_of = [&](int w) { return 2 * w + (w == w0 && first > w0 * share ? 1 : 0); };
-    float top = -INFINITY;
-    for (int w = w0 + lane; w <= w1; w += 64) top = fmaxf(top, parts.sums(part_of(w), n)[0]);
-    top = wave_max(top);
-    const float top_use = top == -INFINITY ? 0.f : top;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int G = a.H / a.H_kv, groups = (G + 16 * nq - 1) / (16 * nq);
+    const Scratch parts{const_cast<float *>(scratch), min(G, 16 * nq), D, n_parts};
+    const Chain chain = *parts.chain(blockIdx.x);
+    if (chain.b < 0) return;
+    const int sub = chain.v_head % groups, n_q = min(16 * nq, G - sub * 16 * nq), h0 = chain.v_head / groups * G + sub * 16 * nq;
+    const auto part_of = [&](int i) { return i == 0 ? chain.w : (chain.w & ~1) + 2 * i; };
     const int grp = tid / LANES, col = tid % LANES * 4;
-    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
+    for (int n = blockIdx.y; n < n_q; n += gridDim.y) {
+        float top = -INFINITY;
+        for (int i = lane; i < chain.count; i += 64) top = fmaxf(top, parts.sums(part_of(i), n)[0]);
+        top = wave_max(top);
+        const float top_use = top == -INFINITY ? 0.f : top;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        float total = 0.f;
 #pragma unroll 4
-    for (int w = w0 + grp; w <= w1; w += GROUPS) {
-        const int part = part_of(w);
-        const float weight = fast_exp2(parts.sums(part, n)[0] - top_use);
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(parts.values(part, n) + col);
-        total += weight * parts.sums(part, n)[1];
+        for (int i = grp; i < chain.count; i += GROUPS) {
+            const int part = part_of(i);
+            const float weight = fast_exp2(parts.sums(part, n)[0] - top_use);
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(parts.values(part, n) + col);
+            total += weight * parts.sums(part, n)[1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, v[e], sum[e]);
-    }
-    acc[grp][tid % LANES] = float4{sum[0], sum[1], sum[2], sum[3]};
-    if (tid % LANES == 0) totals[grp] = total;
-    __syncthreads();
-    if (tid >= D) return;
-    float value = 0.f;
-    total = 0.f;
+            for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, v[e], sum[e]);
+        }
+        acc[grp][tid % LANES] = sum;
+        if (tid % LANES == 0) totals[grp] = total;
+        __syncthreads();
+        if (tid < D) {
+            const int64_t row = (int64_t)chain.b * a.H + h0 + n;
+            float value = 0.f;
+            total = 0.f;
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-        value += reinterpret_cast<const float *>(&acc[i][0])[tid];
-        total += totals[i];
+            for (int i = 0; i < GROUPS; ++i) {
+                value += reinterpret_cast<const float *>(&acc[i][0])[tid];
+                total += totals[i];
+            }
+            out[row * D + tid] = (T)(total == 0.f ? 0.f : value / total);
+            if (tid == 0) lse[row] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
+        }
+        __syncthreads();
     }
-    out[((int64_t)b * a.H + h) * D + tid] = (T)(total == 0.f ? 0.f : value / total);
-    if (tid == 0) lse[(int64_t)b * a.H + h] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
 }
 
 int queries_per_wave(int H, int H_kv) { return H / H_kv > 16 ? 2 : 1; }       // in sixteens
@@ -454,14 +490,18 @@ hipError_t launch(const DecodeArgs &a, const T *q, const T *k_cache, const T *v_
 {
     const int G = a.H / a.H_kv, v_heads = a.H_kv * ((G + 16 * NQ - 1) / (16 * NQ));
     const bool whole = a.max_len <= kWholeLen;
+    constexpr int parts = parts_of(sizeof(T), D, NQ);
     {
         TimedLaunch tl(K_PAGED_DECODE, st);
-        hipLaunchKernelGGL((paged_decode_kernel<T, D, NQ>), dim3((unsigned)(whole ? a.B * v_heads : kParts)), dim3(64 * kWaves), 0, st, a, q, k_cache, v_cache,
+        hipLaunchKernelGGL((paged_decode_kernel<T, D, NQ>), dim3((unsigned)(whole ? a.B * v_heads : parts)), dim3(64 * kWaves), 0, st, a, q, k_cache, v_cache,
                            out, lse, scratch, whole ? 1 : 0);
     }
     if (whole) return hipGetLastError();
+    // (few chains may be long: more threads each)
+    const int chains = (int)std::min<int64_t>((int64_t)a.B * v_heads, parts), y = std::min(G, 8);
     TimedLaunch tl(K_DECODE_MERGE, st);
-    hipLaunchKernelGGL((decode_merge_kernel<T, D, kWaves * Step<T, D>::TILE>), dim3((unsigned)(a.B * a.H)), dim3(256), 0, st, a, scratch, NQ, out, lse);
+    if (chains * y <= 256) hipLaunchKernelGGL((decode_merge_kernel<T, D, 1024>), dim3((unsigned)chains, (unsigned)y), dim3(1024), 0, st, a, scratch, NQ, parts, out, lse);
+    else hipLaunchKernelGGL((decode_merge_kernel<T, D, 256>), dim3((unsigned)chains, (unsigned)y), dim3(256), 0, st, a, scratch, NQ, parts, out, lse);
     return hipGetLastError();
 }
 
@@ -470,8 +510,8 @@ hipError_t launch(const DecodeArgs &a, const T *q, const T *k_cache, const T *v_
 size_t paged_decode_workspace_bytes(int H, int H_kv, int d, int max_len)
 {
     if (max_len <= kWholeLen) return 0;
-    const int G = H / H_kv, rows = std::min(G, 16 * queries_per_wave(H, H_kv));
-    return (size_t)2 * kParts * rows * (d + 2) * sizeof(float);
+    const int nq = queries_per_wave(H, H_kv);
+    return scratch_bytes(std::min(H / H_kv, 16 * nq), d, parts_of(2, d, nq));       // (no fewer for bf16)
 }
 
 template <typename T>
