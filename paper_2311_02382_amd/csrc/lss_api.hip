@@ -850,7 +850,7 @@ int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_s
         return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
     if (int rc = check_arrays(what, {cu_seqlens, lengths, block_table}, inv_freq)) return rc;
     const lss::AppendArgs a{pt, cu_seqlens, lengths, inv_freq, k_stride, v_stride, q_stride, (int)rows, (int)B, (int)H, (int)H_kv, (int)d, (int)rot_dim,
-                            interleaved ? 1 : 0, 0};
+                            interleaved ? 1 : 0, 0, 0};
     const auto go = [&](auto zero) {
         typedef decltype(zero) T;
         return lss::launch_paged_append<T>(a, static_cast<const T *>(k), static_cast<const T *>(v), static_cast<const T *>(q), static_cast<T *>(k_cache),

@@ -180,7 +180,7 @@ struct AppendArgs {
     const int32_t *cu, *lengths;        // cu null: row t belongs to sequence t
     const double *inv_freq;             // [rot / 2] radians per position
     int64_t k_stride, v_stride, q_stride;
-    int rows, B, H, H_kv, d, rot, interleaved, rows_per_wg;
+    int rows, B, H, H_kv, d, rot, interleaved, rows_per_wg, unit_shift;
 };
 template <typename T>
 hipError_t launch_paged_append(const AppendArgs &a, const T *k, const T *v, const T *q, T *k_cache, T *v_cache, T *q_rot, T *k_rot, hipStream_t st);
