@@ -421,7 +421,7 @@ int lss_gelu_bwd(const void *u, const void *dg, int64_t n, void *du, void *strea
  * Answering with a trained model: prompts of different lengths run together, and what is kept of them for the tokens that
  * follow.  Keys and values may have fewer heads than queries (H a multiple of H_kv; query head h reads head h / (H / H_kv)).
  * Rows of a tensor [rows, heads, d] lie `*_stride` elements apart (heads * d where it is contiguous, more for a slice of a wider product; a
- * multiple of 16 bytes), the heads of a row one behind the other.  elem_bytes 2: bf16, 4: float.  int32 arrays are DEVICE memory, read when the
+ * multiple of 16 bytes, at most 2^23 elements), the heads of a row one behind the other.  elem_bytes 2: bf16, 4: float.  int32 arrays are DEVICE memory, read when the
  * kernels run: a captured call follows them.  Whatever they hold, nothing outside the tensors is read or written.
  *
  * The cache: k_cache, v_cache [n_pages, page_size, H_kv, d] contiguous; block_table [B, max_pages] int32: token p of sequence b lies in
@@ -440,7 +440,7 @@ int lss_gelu_bwd(const void *u, const void *dg, int64_t n, void *du, void *strea
  *   k_rot        NULL or [rows, H_kv, d] contiguous (written): the keys as they went into the cache; may be k where that is contiguous
  * The angle is taken in 64 bits, its cosine and sine and the products in 32, rounded to the tensors' type once.  Rows before cu_seqlens[0]
  * and from cu_seqlens[B] on are not touched.  A row whose position is negative or past its table goes into no cache.  Two rows that go to one place
- * (pages that are shared and written) leave either.  Uses no workspace.
+ * (pages that are shared and written) leave either.  rows <= 2^24 (LSS_ERR_SHAPE otherwise).  Uses no workspace.
  */
 int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
                      const int32_t *cu_seqlens, const int32_t *lengths, const int32_t *block_table,
@@ -457,7 +457,7 @@ int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_s
  *   max_len  bound on the lengths, at most max_pages * page_size: a longer sequence counts as that long
  *   workspace  DEVICE buffer of lss_paged_attn_workspace_bytes(H, H_kv, d, max_len) bytes (0 where max_len is small), 16-byte aligned;
  *            NULL: the one registered with lss_set_workspace().  Calls that overlap in time on one GPU need a buffer each
- * Arithmetic and accumulation in fp32.  What lies in a page behind a sequence's last token does not reach the result.
+ * B * H <= 2^23 (LSS_ERR_SHAPE otherwise).  Arithmetic and accumulation in fp32.  What lies in a page behind a sequence's last token does not reach the result.
  */
 size_t lss_paged_attn_workspace_bytes(int64_t H, int64_t H_kv, int64_t d, int64_t max_len);
 int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
@@ -473,12 +473,16 @@ int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, 
  *   out   [rows_q, H, d] contiguous (written);  lse [H, rows_q] float (written)
  * With causal != 0 a sequence's rows stand at the end of its keys: row r sees keys j <= n_k - n_q + r (all rows of a prompt: n_k = n_q; rows that
  * continue one whose keys are there: n_k > n_q).  A row that sees no key gives zeros and lse = -infinity.  Rows of out and lse that belong to no
- * sequence are not touched.  A key that a row does not see does not reach its result, whatever its value.  Uses no workspace.
+ * sequence are not touched.  A key that a row does not see does not reach its result, whatever its value.
+ *   workspace  DEVICE buffer of lss_packed_attn_workspace_bytes(rows_q, rows_k, B, H, H_kv, d, elem_bytes) bytes (0 for many rows), 16-byte aligned;
+ *         NULL: the one registered with lss_set_workspace().  Calls that overlap in time on one GPU need a buffer each
+ * rows_q * H <= 2^30, B * H_kv <= 2^22, rows_k <= 2^30 (LSS_ERR_SHAPE otherwise).
  */
+size_t lss_packed_attn_workspace_bytes(int64_t rows_q, int64_t rows_k, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes);
 int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                         const int32_t *cu_q, const int32_t *cu_k, int64_t rows_q, int64_t rows_k,
                         int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes, int causal,
-                        void *out, float *lse, void *stream);
+                        void *workspace, size_t workspace_bytes, void *out, float *lse, void *stream);
 
 #ifdef __cplusplus
 }

@@ -3,7 +3,6 @@
 #include "lss_attn.h"
 #include "lss_common.h"
 #include "lss_kernels.h"
-#include "lss_packed_plan.h"
 #include "lss_plan.h"
 
 #include <cmath>
@@ -842,6 +841,7 @@ int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_s
     if (int rc = check_rows(what, "v", rows, v_stride, H_kv, d, elem_bytes)) return rc;
     if (q)
         if (int rc = check_rows(what, "q", rows, q_stride, H, d, elem_bytes)) return rc;
+    if (rows > (int64_t)1 << 24) return fail(LSS_ERR_SHAPE, "%s: %lld rows exceed 2^24", what, (long long)rows);
     if (rot_dim < 0 || rot_dim > d || rot_dim % 16 != 0) return fail(LSS_ERR_SHAPE, "%s: rot_dim = %lld (a multiple of 16, at most d)", what, (long long)rot_dim);
     if (rows == 0 || B == 0) return LSS_OK;
     if (!k || !v || !k_cache || !v_cache || !lengths || !block_table || (rot_dim > 0 && !inv_freq) || (q != nullptr) != (q_rot != nullptr))
@@ -897,7 +897,7 @@ int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, 
     if (int rc = check_rows(what, "q", B, q_stride, H, d, elem_bytes)) return rc;
     if (max_len < 0 || max_len > max_pages * page_size)
         return fail(LSS_ERR_RANGE, "%s: max_len = %lld, the tables hold %lld tokens", what, (long long)max_len, (long long)(max_pages * page_size));
-    if (B * H > (int64_t)1 << 24) return fail(LSS_ERR_SHAPE, "%s: B*H = %lld exceeds 2^24", what, (long long)(B * H));
+    if (B * H > (int64_t)1 << 23) return fail(LSS_ERR_SHAPE, "%s: B*H = %lld exceeds 2^23", what, (long long)(B * H));
     if (B == 0) return LSS_OK;
     if (!q || !k_cache || !v_cache || !lengths || !block_table || !out || !lse) return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
     if (misaligned(q) || misaligned(k_cache) || misaligned(v_cache) || misaligned(out))
@@ -916,9 +916,17 @@ int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, 
     return LSS_OK;
 }
 
+size_t lss_packed_attn_workspace_bytes(int64_t rows_q, int64_t rows_k, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes)
+{
+    if (rows_q < 1 || rows_k < 0 || B < 1 || H < 1 || H > 65535 || H_kv < 1 || H % H_kv != 0 || (d != 64 && d != 128) || (elem_bytes != 2 && elem_bytes != 4) ||
+        rows_q > (int64_t)1 << 30 || rows_k > (int64_t)1 << 30 || rows_q * H > (int64_t)1 << 30 || B > (int64_t)1 << 22)
+        return 0;
+    return lss::packed_parts_bytes(rows_q, H, d, lss::pick_packed_plan(rows_q, rows_k, B, H, H_kv, d, elem_bytes).splits);
+}
+
 int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *cu_q,
                         const int32_t *cu_k, int64_t rows_q, int64_t rows_k, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes, int causal,
-                        void *out, float *lse, void *stream)
+                        void *workspace, size_t workspace_bytes, void *out, float *lse, void *stream)
 {
     const char *what = "packed_attn_fwd";
     if (int rc = check_heads(what, H, H_kv, d, elem_bytes)) return rc;
@@ -927,20 +935,22 @@ int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t 
     if (int rc = check_rows(what, "q", rows_q, q_stride, H, d, elem_bytes)) return rc;
     if (int rc = check_rows(what, "k", rows_k, k_stride, H_kv, d, elem_bytes)) return rc;
     if (int rc = check_rows(what, "v", rows_k, v_stride, H_kv, d, elem_bytes)) return rc;
-    if (H_kv * (rows_q * (H / H_kv) / 32 + B) > (int64_t)1 << 30 || rows_q * (H / H_kv) > (int64_t)1 << 30)
+    if (rows_q * H > (int64_t)1 << 30 || B * H_kv > (int64_t)1 << 22)     // (a launch has fewer than 2^32 threads)
         return fail(LSS_ERR_SHAPE, "%s: %lld rows of %lld heads in %lld sequences are too many", what, (long long)rows_q, (long long)H, (long long)B);
     if (B == 0 || rows_q == 0) return LSS_OK;
     if (!q || !cu_q || !cu_k || !out || !lse || (rows_k > 0 && (!k || !v))) return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
     if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out))
         return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
+    if (misaligned(workspace)) return fail(LSS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", what);
     if (int rc = check_arrays(what, {cu_q, cu_k, lse})) return rc;
+    if (int rc = get_scratch(what, lss_packed_attn_workspace_bytes(rows_q, rows_k, B, H, H_kv, d, elem_bytes), &workspace, workspace_bytes)) return rc;
     const lss::PackedArgs a{cu_q, cu_k, q_stride, k_stride, v_stride, (int)rows_q, (int)rows_k, (int)B, (int)H, (int)H_kv, (int)d, causal ? 1 : 0};
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    using lss::bf16_t;
-    const hipError_t e = elem_bytes == 2 ? lss::launch_packed_bf16(a, static_cast<const bf16_t *>(q), static_cast<const bf16_t *>(k),
-                                                                   static_cast<const bf16_t *>(v), static_cast<bf16_t *>(out), lse, st)
-                                         : lss::launch_packed_f32(a, static_cast<const float *>(q), static_cast<const float *>(k),
-                                                                  static_cast<const float *>(v), static_cast<float *>(out), lse, st);
+    const auto go = [&](auto zero) {
+        typedef decltype(zero) T;
+        return lss::launch_packed<T>(a, static_cast<const T *>(q), static_cast<const T *>(k), static_cast<const T *>(v), static_cast<T *>(out), lse,
+                                     static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
+    };
+    const hipError_t e = elem_bytes == 2 ? go(lss::bf16_t{}) : go(float{});
     if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));
     return LSS_OK;
 }
@@ -984,14 +994,14 @@ int lss_plan_bwd(int64_t s0, int64_t l_s, int64_t l_x, int64_t B, int64_t H, int
     return LSS_OK;
 }
 
-int lss_plan_packed(int64_t rows_q, int64_t rows_k, int64_t B, int64_t H, int64_t H_kv, int64_t d, int *plan)
+int lss_plan_packed(int64_t rows_q, int64_t rows_k, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes, int *plan)
 {
-    if (int rc = check_heads("plan", H, H_kv, d, 2)) return rc;
+    if (int rc = check_heads("plan", H, H_kv, d, elem_bytes)) return rc;
     if (rows_q < 1 || rows_k < 0 || B < 1 || H % H_kv != 0) return fail(LSS_ERR_SHAPE, "plan: no launch of such a call");
     if (!plan) return fail(LSS_ERR_NULL, "plan: NULL");
-    const lss::PackedForm f = lss::pick_packed_form(rows_q, rows_k, B, H, H_kv, d);
-    plan[0] = f.row_blocks;
-    plan[1] = f.groups;
+    const lss::PackedPlan p = lss::pick_packed_plan(rows_q, rows_k, B, H, H_kv, d, elem_bytes);
+    const int all[3] = {p.row_blocks, p.groups, p.splits};
+    std::copy(all, all + 3, plan);
     return LSS_OK;
 }
 

@@ -364,11 +364,11 @@ struct FwdView {
     int l_s, l_x, causal, G;    // rows, keys
 };
 
-// Rows r0 .. r0 + 127: put(j, db, values) takes columns 16 db + 4 (lane / 16) .. + 3 of row r0 + 32 (wavefront) + 16 j + lane % 16, normalised, put_lse(j, .) its
-// lse.  `bh`: batch * head for the dropout's decisions.
-template <int D, bool DROP, typename Put, typename PutLse>
-__device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const DropArgs &dr, int bh, int r0, int split, int n_splits, Put &&put,
-                                             PutLse &&put_lse)
+// Rows r0 .. r0 + 127: row_of(j) is where the result of row r0 + 32 (wavefront) + 16 j + lane % 16 goes, put(j, that, db, values) takes its columns 16 db +
+// 4 (lane / 16) .. + 3, normalised, put_lse(j, .) its lse.  `bh`: batch * head for the dropout's decisions.
+template <int D, bool DROP, typename RowOf, typename Put, typename PutLse>
+__device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const DropArgs &dr, int bh, int r0, int split, int n_splits, RowOf &&row_of,
+                                             Put &&put, PutLse &&put_lse)
 {
     using Tile = PlaneTile<D>;
     constexpr int NS = D / 32, BC = Tile::ROWS;
@@ -515,10 +515,11 @@ __device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const
         const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
         const float lse_nat = l_tot > 0.f ? (m[j] + log2f(l_tot)) * kLn2 : -INFINITY;
         if (r + 16 * j >= s.l_s) continue;
+        float *const to = row_of(j);
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) {
             const f32x4 a = o.v[db][j];
-            put(j, db, f32x4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv});
+            put(j, to, db, f32x4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv});
         }
         if (g == 0) put_lse(j, lse_nat);
     }
@@ -543,10 +544,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fwd_f32_kernel(SegShape 
     const auto part_row = [&](int j) { return ((int64_t)split * bhs + bh) * s.l_s + r + 16 * j; };
     fwd_f32_body<D, DROP>(
         smem, view, dr, bh, r0, split, n_splits,
-        [&](int j, int db, const f32x4 &val) __attribute__((always_inline)) {
-            float *op = n_splits == 1 ? out + ((int64_t)b * s.l_s + r + 16 * j) * ld + (int64_t)h * D : o_part + part_row(j) * D;
-            *reinterpret_cast<f32x4 *>(op + db * 16 + 4 * g) = val;
+        [&](int j) __attribute__((always_inline)) {
+            return n_splits == 1 ? out + ((int64_t)b * s.l_s + r + 16 * j) * ld + (int64_t)h * D : o_part + part_row(j) * D;
         },
+        [&](int, float *to, int db, const f32x4 &val) __attribute__((always_inline)) { *reinterpret_cast<f32x4 *>(to + db * 16 + 4 * g) = val; },
         [&](int j, float v) __attribute__((always_inline)) {
             if (n_splits == 1) lse[(int64_t)bh * s.l_s + r + 16 * j] = v;
             else lse_part[part_row(j)] = v;
@@ -554,30 +555,42 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fwd_f32_kernel(SegShape 
 }
 
 // Packed sequences (lss_packed_attn_fwd): rows are query heads of tokens, as in packed_bf16_kernel
-template <int D>
+template <int D, bool SPLIT>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_f32_kernel(PackedArgs a, const float *__restrict__ q, const float *__restrict__ k,
                                                                          const float *__restrict__ v, float *__restrict__ out, float *__restrict__ lse,
-                                                                         int n_inner)
+                                                                         PackedParts parts, int n_tiles)
 {
     __shared__ __attribute__((aligned(1024))) char smem[2 * PlaneTile<D>::BYTES + 16];
     const int lane = threadIdx.x & 63, g = lane >> 4, G = a.H / a.H_kv;
     int h_kv, rank;
-    if (!xcd_item(blockIdx.x, a.H_kv, n_inner, a.causal != 0, h_kv, rank)) return;
+    if (!xcd_item(blockIdx.x, a.H_kv, SPLIT ? n_tiles * parts.splits : n_tiles, a.causal != 0, h_kv, rank)) return;
+    const int split = SPLIT ? rank % parts.splits : 0;
+    if (SPLIT) rank /= parts.splits;
     PackedTile t;
     if (!packed_tile<kRowsPerWg>(a, G, rank, lane, t)) return;
     const FwdView view{q + (int64_t)t.q_begin * a.q_stride + (int64_t)h_kv * G * D, k + (int64_t)t.k_begin * a.k_stride + (int64_t)h_kv * D,
                        v + (int64_t)t.k_begin * a.v_stride + (int64_t)h_kv * D, a.q_stride, a.k_stride, a.v_stride, t.n_k - t.n_q, t.n_q * G, t.n_k, a.causal, G};
     const int r0 = t.tile * kRowsPerWg, rw0 = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32, r = rw0 + (lane & 15);
-    const auto token = [&](int j) { return t.q_begin + (r + 16 * j) / G; };
-    const auto head = [&](int j) { return h_kv * G + (r + 16 * j) % G; };
+    int token, head;
     bool finite[2] = {true, true};
     fwd_f32_body<D, false>(
-        smem, view, DropArgs{}, 0, r0, 0, 1,
-        [&](int j, int db, const f32x4 &val) __attribute__((always_inline)) {
-            *reinterpret_cast<f32x4 *>(out + ((int64_t)token(j) * a.H + head(j)) * D + db * 16 + 4 * g) = val;
+        smem, view, DropArgs{}, 0, r0, split, parts.splits,      // (1 as a constant: 34 registers of d = 64 go to memory)
+        [&](int j) __attribute__((always_inline)) {
+            int row = r + 16 * j;
+            asm volatile("" : "+v"(row));               // (so that its address is made here, not kept through the main loop)
+            token = t.q_begin + row / G;
+            head = h_kv * G + row % G;
+            return SPLIT ? parts.values(a, split, token, head) : out + ((int64_t)token * a.H + head) * D;
+        },
+        [&](int j, float *to, int db, const f32x4 &val) __attribute__((always_inline)) {
+            *reinterpret_cast<f32x4 *>(to + db * 16 + 4 * g) = val;
             finite[j] = finite[j] && fabsf(val[0]) < INFINITY && fabsf(val[1]) < INFINITY && fabsf(val[2]) < INFINITY && fabsf(val[3]) < INFINITY;
         },
-        [&](int j, float v) __attribute__((always_inline)) { lse[(int64_t)head(j) * a.rows_q + token(j)] = v; });
+        [&](int, float v) __attribute__((always_inline)) {
+            if (SPLIT) *parts.lse(a, split, token, head) = v;
+            else lse[(int64_t)head * a.rows_q + token] = v;
+        });
+    if (SPLIT) return;
     // rows with a result that is not finite are done over, over the keys that they see alone (packed_bf16_kernel)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -1039,18 +1052,21 @@ hipError_t launch_bwd_f32_main(const SegShape &s, const DropArgs &drop, const fl
     return launch_bwd_d<128>(s, drop, q, k, v, lse, dO, dq, dk_part, dv_part, ws, n_splits, st);
 }
 
-template <int D>
-static hipError_t launch_packed(const PackedArgs &a, const float *q, const float *k, const float *v, float *out, float *lse, hipStream_t st)
+template <int D, bool SPLIT>
+static hipError_t launch_packed(const PackedArgs &a, const float *q, const float *k, const float *v, float *out, float *lse, const PackedParts &parts,
+                                hipStream_t st)
 {
-    const int n_inner = packed_tiles(a, kRowsPerWg);
+    const int n_tiles = packed_tiles(a, kRowsPerWg);
     TimedLaunch tl(K_PACKED_F32, st);
-    hipLaunchKernelGGL(packed_f32_kernel<D>, dim3((unsigned)xcd_grid(a.H_kv, n_inner)), dim3(256), 0, st, a, q, k, v, out, lse, n_inner);
+    hipLaunchKernelGGL((packed_f32_kernel<D, SPLIT>), dim3((unsigned)xcd_grid(a.H_kv, n_tiles * parts.splits)), dim3(256), 0, st, a, q, k, v, out, lse, parts, n_tiles);
     return hipGetLastError();
 }
 
-hipError_t launch_packed_f32(const PackedArgs &a, const float *q, const float *k, const float *v, float *out, float *lse, hipStream_t st)
+hipError_t launch_packed_f32_main(const PackedArgs &a, const float *q, const float *k, const float *v, float *out, float *lse, const PackedParts &parts,
+                                  hipStream_t st)
 {
-    return a.d == 64 ? launch_packed<64>(a, q, k, v, out, lse, st) : launch_packed<128>(a, q, k, v, out, lse, st);
+    if (parts.splits > 1) return a.d == 64 ? launch_packed<64, true>(a, q, k, v, out, lse, parts, st) : launch_packed<128, true>(a, q, k, v, out, lse, parts, st);
+    return a.d == 64 ? launch_packed<64, false>(a, q, k, v, out, lse, parts, st) : launch_packed<128, false>(a, q, k, v, out, lse, parts, st);
 }
 
 } // namespace lss

@@ -28,7 +28,6 @@
 #include "lss_bf16.h"
 #include <type_traits>
 #include "lss_kernels.h"
-#include "lss_packed_plan.h"
 #include "lss_serve.h"
 
 namespace lss {
@@ -498,16 +497,18 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void fwd_bf16_kernel
 // Packed sequences (lss_packed_attn_fwd).  A row of a workgroup is a query head of a token: the G heads that share a head of keys and values are
 // neighbours, so that a tile of keys serves 128 / G tokens of all of them, the causal diagonal crosses fewer of a wavefront's blocks,
 // and short prompts fill the rows.
-template <int D, int RB, int KG>
+template <int D, int RB, int KG, bool SPLIT>
 __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void packed_bf16_kernel(PackedArgs a, const bf16_t *__restrict__ q, const bf16_t *__restrict__ k,
                                                                                    const bf16_t *__restrict__ v, bf16_t *__restrict__ out,
-                                                                                   float *__restrict__ lse, int n_inner)
+                                                                                   float *__restrict__ lse, PackedParts parts, int n_tiles)
 {
     using C = FwdBf16Cfg<D, RB, KG>;
     __shared__ __attribute__((aligned(1024))) char smem[C::lds(false)];
     const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5, G = a.H / a.H_kv;
     int h_kv, rank;
-    if (!xcd_item(blockIdx.x, a.H_kv, n_inner, a.causal != 0, h_kv, rank)) return;
+    if (!xcd_item(blockIdx.x, a.H_kv, SPLIT ? n_tiles * parts.splits : n_tiles, a.causal != 0, h_kv, rank)) return;
+    const int split = SPLIT ? rank % parts.splits : 0;
+    if (SPLIT) rank /= parts.splits;
     PackedTile t;
     if (!packed_tile<C::BR>(a, G, rank, lane, t)) return;
     const FwdView view{q + (int64_t)t.q_begin * a.q_stride + (int64_t)h_kv * G * D, k + (int64_t)t.k_begin * a.k_stride + (int64_t)h_kv * D,
@@ -517,14 +518,22 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void packed_bf16_ker
     bf16_t *const row = out + ((int64_t)token * a.H + h) * D;
     bool finite = true;
     fwd_bf16_body<D, false, RB, KG, true>(
-        smem, view, DropArgs{}, 0, r0, 0, 1,
+        smem, view, DropArgs{}, 0, r0, split, SPLIT ? parts.splits : 1,
         [&](int u, const f32x4 &val) __attribute__((always_inline)) {
+            if (SPLIT) {
+                *reinterpret_cast<f32x4 *>(parts.values(a, split, token, h) + 8 * u + 4 * hh) = val;
+                return;
+            }
             *reinterpret_cast<bf16x4 *>(row + 8 * u + 4 * hh) = pack4(val[0], val[1], val[2], val[3]);
             finite = finite && fabsf(val[0]) < INFINITY && fabsf(val[1]) < INFINITY && fabsf(val[2]) < INFINITY && fabsf(val[3]) < INFINITY;
         },
-        [&](float v) { lse[(int64_t)h * a.rows_q + token] = v; });
+        [&](float v) {
+            if (SPLIT) *parts.lse(a, split, token, h) = v;
+            else lse[(int64_t)h * a.rows_q + token] = v;
+        });
     // A key's weight is 0 for the rows of its block that do not see it, but 0 times a value that is not finite is NaN: rows with such a result are done over,
-    // over the keys that they see alone.
+    // over the keys that they see alone (of a tile whose keys are split: by packed_merge_kernel).
+    if (SPLIT) return;
     if (KG > 1) __syncthreads();                // (the groups have written parts of one row)
     const uint64_t bad = __ballot(!finite);
     for (uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32); rows != 0; rows &= rows - 1) {
@@ -571,32 +580,36 @@ hipError_t launch_fwd_bf16_main(const SegShape &s, const DropArgs &drop, const b
     return launch_fwd_main<128, 8, 1>(s, drop, q, k, v, out, lse, ws, plan.splits, st);
 }
 
-template <int D, int RB, int KG>
-static hipError_t launch_packed(const PackedArgs &a, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse, hipStream_t st)
+template <int D, int RB, int KG, bool SPLIT = false>
+static hipError_t launch_packed(const PackedArgs &a, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse, const PackedParts &parts,
+                                hipStream_t st)
 {
     using C = FwdBf16Cfg<D, RB, KG>;
-    const int n_inner = packed_tiles(a, C::BR);
+    const int n_tiles = packed_tiles(a, C::BR);
     TimedLaunch tl(K_PACKED_BF16, st);
-    hipLaunchKernelGGL((packed_bf16_kernel<D, RB, KG>), dim3((unsigned)xcd_grid(a.H_kv, n_inner)), dim3(C::NT), 0, st, a, q, k, v, out, lse, n_inner);
+    hipLaunchKernelGGL((packed_bf16_kernel<D, RB, KG, SPLIT>), dim3((unsigned)xcd_grid(a.H_kv, n_tiles * parts.splits)), dim3(C::NT), 0, st, a, q, k, v, out, lse,
+                       parts, n_tiles);
     return hipGetLastError();
 }
 
-hipError_t launch_packed_bf16(const PackedArgs &a, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse, hipStream_t st)
+hipError_t launch_packed_bf16_main(const PackedArgs &a, const PackedPlan &f, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse,
+                                   const PackedParts &parts, hipStream_t st)
 {
-    const PackedForm f = pick_packed_form(a.rows_q, a.rows_k, a.B, a.H, a.H_kv, a.d);
     const auto is = [&](int row_blocks, int groups) { return f.row_blocks == row_blocks && f.groups == groups; };
+    if (parts.splits > 1)        // (with splits: always this form)
+        return a.d == 64 ? launch_packed<64, 2, 2, true>(a, q, k, v, out, lse, parts, st) : launch_packed<128, 2, 2, true>(a, q, k, v, out, lse, parts, st);
     if (a.d == 64) {
-        if (is(2, 1)) return launch_packed<64, 2, 1>(a, q, k, v, out, lse, st);
-        if (is(2, 2)) return launch_packed<64, 2, 2>(a, q, k, v, out, lse, st);
-        if (is(4, 2)) return launch_packed<64, 4, 2>(a, q, k, v, out, lse, st);
-        if (is(2, 4)) return launch_packed<64, 2, 4>(a, q, k, v, out, lse, st);
-        if (is(1, 4)) return launch_packed<64, 1, 4>(a, q, k, v, out, lse, st);
-        return launch_packed<64, 4, 1>(a, q, k, v, out, lse, st);
+        if (is(2, 1)) return launch_packed<64, 2, 1>(a, q, k, v, out, lse, parts, st);
+        if (is(2, 2)) return launch_packed<64, 2, 2>(a, q, k, v, out, lse, parts, st);
+        if (is(4, 2)) return launch_packed<64, 4, 2>(a, q, k, v, out, lse, parts, st);
+        if (is(2, 4)) return launch_packed<64, 2, 4>(a, q, k, v, out, lse, parts, st);
+        if (is(1, 4)) return launch_packed<64, 1, 4>(a, q, k, v, out, lse, parts, st);
+        return launch_packed<64, 4, 1>(a, q, k, v, out, lse, parts, st);
     }
-    if (is(2, 2)) return launch_packed<128, 2, 2>(a, q, k, v, out, lse, st);
-    if (is(4, 2)) return launch_packed<128, 4, 2>(a, q, k, v, out, lse, st);
-    if (is(8, 1)) return launch_packed<128, 8, 1>(a, q, k, v, out, lse, st);
-    return launch_packed<128, 4, 1>(a, q, k, v, out, lse, st);
+    if (is(2, 2)) return launch_packed<128, 2, 2>(a, q, k, v, out, lse, parts, st);
+    if (is(4, 2)) return launch_packed<128, 4, 2>(a, q, k, v, out, lse, parts, st);
+    if (is(8, 1)) return launch_packed<128, 8, 1>(a, q, k, v, out, lse, parts, st);
+    return launch_packed<128, 4, 1>(a, q, k, v, out, lse, parts, st);
 }
 
 } // namespace lss

@@ -4,6 +4,7 @@
 #include "lss_bwd_plan.h"
 #include "lss_device_once.h"
 #include "lss_fwd_plan.h"
+#include "lss_packed_plan.h"
 #include "lss_shape.h"
 #include <stddef.h>
 #include <stdint.h>
@@ -110,7 +111,7 @@ hipError_t allow_lds(K kernel, int bytes, DeviceOnce &once)
 enum KernelId { K_FWD_F32 = 0, K_FWD_MERGE, K_ROWDOT, K_BWD_MAIN_F32, K_DQ_MERGE, K_REDUCE, K_BWD_MAIN_BF16, K_PROJ_FWD, K_PROJ_BWD,
                 K_PE_FWD, K_PE_BWD, K_LN_FWD, K_LN_BWD, K_LN_PARAMS, K_GELU_FWD, K_GELU_BWD, K_LINEAR_FWD, K_LINEAR_BWD, K_RESIDUAL, K_LINEAR_WGRAD,
                 K_FWD_BF16, K_BWD_PREP_BF16, K_BWD_SKINNY_BF16, K_LN_BWD_SHORT, K_PROJ_FWD_SMALL, K_PROJ_BWD_SMALL, K_LINEAR_FWD_SMALL,
-                K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_BF16, K_PACKED_F32, K_COUNT };
+                K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_BF16, K_PACKED_F32, K_PACKED_MERGE, K_COUNT };
 void timing_begin(int id, hipStream_t st);
 void timing_end(int id, hipStream_t st);
 struct TimedLaunch {    // RAII bracket around one kernel launch
@@ -170,7 +171,7 @@ hipError_t launch_layernorm_bwd(const bf16_t *x, const float *gamma, const float
 hipError_t launch_gelu_fwd(const bf16_t *u, int64_t n, bf16_t *g, hipStream_t st);
 hipError_t launch_gelu_bwd(const bf16_t *u, const bf16_t *dg, int64_t n, bf16_t *du, hipStream_t st);
 
-// the paged cache (lss_paged.hip, lss_decode.hip) and packed sequences (lss_fwd_bf16.hip, lss_f32.hip); int32 arrays are device memory, strides count elements
+// the paged cache (lss_paged.hip, lss_decode.hip) and packed sequences (lss_packed.hip, lss_fwd_bf16.hip, lss_f32.hip); int32 arrays are device memory, strides count elements
 struct PageTable {
     const int32_t *table;       // [B, max_pages]
     int n_pages, page_shift, max_pages;
@@ -203,7 +204,25 @@ inline int packed_tiles(const PackedArgs &a, int rows)
 {
     return (int)((int64_t)a.rows_q * (a.H / a.H_kv) / rows) + (a.B <= 64 && a.rows_q < a.B ? a.rows_q : a.B);
 }
-hipError_t launch_packed_bf16(const PackedArgs &a, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse, hipStream_t st);
-hipError_t launch_packed_f32(const PackedArgs &a, const float *q, const float *k, const float *v, float *out, float *lse, hipStream_t st);
+// what splits of the keys leave for packed_merge_kernel (splits = 1: nothing): a row's normalised result and lse over their part
+struct PackedParts {
+    float *base;
+    int splits;
+#if defined(__HIP__)
+    __device__ float *values(const PackedArgs &a, int split, int token, int h) const { return base + (((int64_t)split * a.rows_q + token) * a.H + h) * a.d; }
+    __device__ float *lse(const PackedArgs &a, int split, int token, int h) const
+    {
+        return base + (int64_t)splits * a.rows_q * a.H * a.d + ((int64_t)split * a.rows_q + token) * a.H + h;
+    }
+#endif
+};
+inline size_t packed_parts_bytes(int64_t rows_q, int64_t H, int64_t d, int splits) { return splits > 1 ? (size_t)splits * rows_q * H * (d + 1) * sizeof(float) : 0; }
+hipError_t launch_packed_bf16_main(const PackedArgs &a, const PackedPlan &plan, const bf16_t *q, const bf16_t *k, const bf16_t *v, bf16_t *out, float *lse,
+                                   const PackedParts &parts, hipStream_t st);
+hipError_t launch_packed_f32_main(const PackedArgs &a, const float *q, const float *k, const float *v, float *out, float *lse, const PackedParts &parts,
+                                  hipStream_t st);
+// `scratch`: packed_parts_bytes() of the plan's splits
+template <typename T>
+hipError_t launch_packed(const PackedArgs &a, const T *q, const T *k, const T *v, T *out, float *lse, float *scratch, hipStream_t st);
 
 } // namespace lss

@@ -8,7 +8,8 @@
  *                 plan[2] all three gradients in one pass, plan[3] no preprocess launch, plan[4] dK/dV workgroups for at most
  *                 64 rows, plan[5] wavefronts of 16 rows
  *
- *   lss_plan_packed  lss_packed_attn_fwd, bf16: plan[0] blocks of 32 rows of a workgroup, plan[1] groups of wavefronts that have a part of its keys each
+ *   lss_plan_packed  lss_packed_attn_fwd: plan[0] blocks of 32 rows of a workgroup, plan[1] groups of wavefronts that have a part of its keys each,
+ *                    plan[2] key splits
  *
  *   lss_plan_linear   op 0 lss_linear_fwd, 1 lss_linear_bwd_input, 2 lss_linear_bwd_weight (fused forms take the same tiles).  plan[0] tile (GemmTile
  *                     of lss_gemm_plan.h), plan[1] chunks of rows, plan[2] groups of wavefronts that share a contraction, plan[3] slots of their rings
@@ -31,7 +32,7 @@ int lss_plan_fwd(int64_t seg_offset, int64_t l_s, int64_t l_x, int64_t B, int64_
                  int elem_bytes, int *plan);
 int lss_plan_bwd(int64_t seg_offset, int64_t l_s, int64_t l_x, int64_t B, int64_t H, int64_t d, int causal, int with_dropout,
                  int elem_bytes, int over_out, int *plan);
-int lss_plan_packed(int64_t rows_q, int64_t rows_k, int64_t B, int64_t H, int64_t H_kv, int64_t d, int *plan);
+int lss_plan_packed(int64_t rows_q, int64_t rows_k, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes, int *plan);
 int lss_plan_linear(int op, int64_t rows, int64_t K, int64_t N, int *plan);
 int lss_plan_project(int op, int64_t l_s, int64_t l_x, int64_t rows_valid, int64_t B, int64_t H, int64_t d, int *plan);
 

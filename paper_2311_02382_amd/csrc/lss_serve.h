@@ -139,7 +139,7 @@ __device__ void row_attention(const T *q, const T *k, int64_t k_stride, const T 
         float s = -INFINITY;
         if (row >= 0) {
             s = 0.f;
-#pragma unroll
+#pragma unroll 2                                        // (its registers must not add to those of the kernels that fall back on it)
             for (int i = 0; i < D; i += VEC) {
                 const Vec a = *reinterpret_cast<const Vec *>(q + i), b = *reinterpret_cast<const Vec *>(k + row * k_stride + i);
 #pragma unroll

@@ -31,7 +31,7 @@ const char *const kNames[K_COUNT] = {"fwd_f32_kernel", "fwd_merge_kernel", "bwd_
                                      "residual_add_kernel", "wgrad_gemm_kernel", "fwd_bf16_kernel", "bwd_prep_bf16_kernel",
                                      "bwd_skinny_bf16_kernel", "layernorm_bwd_short_kernel", "proj_small_gemm_kernel:project_qkv",
                                      "proj_small_gemm_kernel:project_bwd", "proj_small_gemm_kernel:linear_fwd", "proj_small_gemm_kernel:linear_bwd_input", "paged_append_kernel", "paged_decode_kernel", "decode_merge_kernel",
-                                     "packed_bf16_kernel", "packed_f32_kernel"};
+                                     "packed_bf16_kernel", "packed_f32_kernel", "packed_merge_kernel"};
 
 hipEvent_t get_event()
 {

@@ -521,6 +521,18 @@ void int32_array(const at::Tensor &t, int64_t dims, const char *what)
 {
     if (t.dim() != dims || t.scalar_type() != at::kInt || !on_gpu(t)) throw ValueError(std::string(what) + " must be a contiguous torch.int32 device tensor of " + std::to_string(dims) + (dims == 1 ? " dimension" : " dimensions"));
 }
+// scratch of `need` bytes: the caller's own tensor (checked) or the shared one
+void *call_scratch(PyObject *workspace, size_t need, const at::Tensor &like, size_t &bytes)
+{
+    bytes = 0;
+    if (none(workspace)) return need > 0 ? shared_workspace(need, like, bytes) : nullptr;
+    const at::Tensor &w = tensor(workspace);
+    require(on_gpu(w), "workspace must be a contiguous device tensor");
+    on_current_gpu({&w});
+    bytes = (size_t)w.numel() * w.element_size();
+    if (bytes < need) throw ValueError("workspace of " + std::to_string(bytes) + " bytes, need " + std::to_string(need));
+    return ptr(w);
+}
 struct Cache { int64_t n_pages, page_size, H_kv, d, B, max_pages; int eb; at::ScalarType dt; };
 Cache cache_of(const at::Tensor &k, const at::Tensor &v, const at::Tensor &table, const at::Tensor &lengths)
 {
@@ -581,22 +593,13 @@ PyObject *paged_attn_decode(PyObject *const *a)
     const int64_t max_len = none(a[5]) ? m.max_pages * m.page_size : integer(a[5]);
     const at::Tensor out = output(a[6], q.sizes(), m.dt, q), lse = output(a[7], {m.B, rq.heads}, kF32, q);
     on_current_gpu({&q, &kc, &vc, &table, &lengths, &out, &lse});
-    const size_t need = lss_paged_attn_workspace_bytes(rq.heads, m.H_kv, m.d, max_len);
     size_t wn = 0;
-    void *wp = nullptr;
-    if (!none(a[9])) {
-        const at::Tensor &w = tensor(a[9]);
-        require(on_gpu(w), "workspace must be a contiguous device tensor");
-        on_current_gpu({&w});
-        wn = (size_t)w.numel() * w.element_size();
-        wp = ptr(w);
-        if (wn < need) throw ValueError("workspace of " + std::to_string(wn) + " bytes, need " + std::to_string(need));
-    } else if (need > 0) wp = shared_workspace(need, q, wn);
+    void *wp = call_scratch(a[9], lss_paged_attn_workspace_bytes(rq.heads, m.H_kv, m.d, max_len), q, wn);
     invoke(lss_paged_attn_decode, ptr(q), rq.stride, ptr(kc), ptr(vc), static_cast<const int32_t *>(ptr(lengths)), static_cast<const int32_t *>(ptr(table)), m.B,
            rq.heads, m.H_kv, m.d, m.eb, m.n_pages, m.page_size, m.max_pages, max_len, wp, wn, ptr(out), fptr(lse), stream_of(a[8]));
     return pack({give(a[6], out), give(a[7], lse)});
 }
-// q k v cu_q cu_k causal out lse stream
+// q k v cu_q cu_k causal out lse stream workspace
 PyObject *packed_attn_fwd(PyObject *const *a)
 {
     const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]), &cu_q = tensor(a[3]), &cu_k = none(a[4]) ? cu_q : tensor(a[4]);
@@ -608,8 +611,11 @@ PyObject *packed_attn_fwd(PyObject *const *a)
     require(cu_q.size(0) >= 1 && cu_q.size(0) == cu_k.size(0), "cu_q and cu_k must have one entry more than there are sequences");
     const at::Tensor out = output(a[6], q.sizes(), q.scalar_type(), q), lse = output(a[7], {rq.heads, rq.rows}, kF32, q);
     on_current_gpu({&q, &k, &v, &cu_q, &cu_k, &out, &lse});
+    const int eb = q.scalar_type() == kF32 ? 4 : 2;
+    size_t wn;
+    void *wp = call_scratch(a[9], lss_packed_attn_workspace_bytes(rq.rows, rk.rows, cu_q.size(0) - 1, rq.heads, rk.heads, rq.d, eb), q, wn);
     invoke(lss_packed_attn_fwd, ptr(q), rq.stride, ptr(k), rk.stride, ptr(v), rv.stride, static_cast<const int32_t *>(ptr(cu_q)),
-           static_cast<const int32_t *>(ptr(cu_k)), rq.rows, rk.rows, cu_q.size(0) - 1, rq.heads, rk.heads, rq.d, q.scalar_type() == kF32 ? 4 : 2, truth(a[5]),
+           static_cast<const int32_t *>(ptr(cu_k)), rq.rows, rk.rows, cu_q.size(0) - 1, rq.heads, rk.heads, rq.d, eb, truth(a[5]), wp, wn,
            ptr(out), fptr(lse), stream_of(a[8]));
     return pack({give(a[6], out), give(a[7], lse)});
 }
@@ -646,7 +652,7 @@ PyMethodDef g_methods[] = {
     LSS_FN(residual_dropout_add, 7), LSS_FN(layernorm_fwd, 8), LSS_FN(layernorm_bwd, 10), LSS_FN(linear_fwd, 4),
     LSS_FN(linear_bwd_input, 4), LSS_FN(linear_bwd_weight, 5), LSS_FN(linear_gelu_fwd, 5), LSS_FN(linear_bwd_input_gelu, 5),
     LSS_FN(gelu_fwd, 3), LSS_FN(gelu_bwd, 4), LSS_FN(paged_append, 13), LSS_FN(paged_attn_decode, 10),
-    LSS_FN(packed_attn_fwd, 9), LSS_FN(set_error_type, 1), {nullptr, nullptr, 0, nullptr}};
+    LSS_FN(packed_attn_fwd, 10), LSS_FN(set_error_type, 1), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_lss_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace

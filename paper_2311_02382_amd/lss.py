@@ -33,7 +33,7 @@ EXPORTS = ["lss_version", "lss_last_error", "lss_workspace_bytes", "lss_set_work
            "lss_layernorm_bwd", "lss_linear_fwd", "lss_linear_bwd_input", "lss_linear_bwd_weight_scratch_bytes", "lss_linear_bwd_weight",
            "lss_linear_gelu_fwd",
            "lss_linear_bwd_input_gelu", "lss_gelu_fwd", "lss_gelu_bwd", "lss_paged_append", "lss_paged_attn_workspace_bytes", "lss_paged_attn_decode",
-           "lss_packed_attn_fwd"]
+           "lss_packed_attn_workspace_bytes", "lss_packed_attn_fwd"]
 
 LSS_FLAG_SKIP_MASKED_TAIL = 1
 
@@ -113,7 +113,9 @@ def load():
     lib.lss_paged_attn_decode.argtypes = [vp, i64, vp, vp, vp, vp, i64, i64, i64, i64, ci, i64, i64, i64, i64, vp, sz, vp, vp, vp]
     lib.lss_paged_attn_workspace_bytes.argtypes = [i64, i64, i64, i64]
     lib.lss_paged_attn_workspace_bytes.restype = sz
-    lib.lss_packed_attn_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i64, i64, ci, ci, vp, vp, vp]
+    lib.lss_packed_attn_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i64, i64, ci, ci, vp, sz, vp, vp, vp]
+    lib.lss_packed_attn_workspace_bytes.argtypes = [i64, i64, i64, i64, i64, i64, ci]
+    lib.lss_packed_attn_workspace_bytes.restype = sz
     for name in ("lss_paged_append", "lss_paged_attn_decode", "lss_packed_attn_fwd"):
         getattr(lib, name).restype = ci
     for name in ("lss_embed_pe_fwd", "lss_embed_pe_bwd", "lss_residual_dropout_add", "lss_layernorm_fwd", "lss_layernorm_bwd", "lss_linear_fwd",
@@ -330,10 +332,15 @@ def lss_paged_attn_decode(q, k_cache, v_cache, block_table, lengths, max_len=Non
     return (_native or _bind()).paged_attn_decode(q, k_cache, v_cache, block_table, lengths, max_len, out, lse, stream, workspace)
 
 
-def lss_packed_attn_fwd(q, k, v, cu_q, cu_k=None, causal=True, out=None, lse=None, stream=None):
+def lss_packed_attn_workspace_bytes(rows_q, rows_k, B, H, H_kv, d, elem_bytes=2) -> int:
+    return int(load().lss_packed_attn_workspace_bytes(*map(int, (rows_q, rows_k, B, H, H_kv, d, elem_bytes))))
+
+
+def lss_packed_attn_fwd(q, k, v, cu_q, cu_k=None, causal=True, out=None, lse=None, stream=None, workspace=None):
     """Attention within each of the sequences that are packed one behind the other: q [rows, H, d] with starts cu_q int32 [B + 1],
     k, v [rows, H_kv, d] with starts cu_k (None: cu_q), H a multiple of H_kv.  With `causal` the rows of a sequence stand at the end of
-    its keys: row r of n_q sees keys up to n_k - n_q + r.
+    its keys: row r of n_q sees keys up to n_k - n_q + r.  workspace: a device tensor of lss_packed_attn_workspace_bytes() bytes used by this call
+    alone; None: the binding's buffer of that GPU.
 
     Returns (out [rows, H, d] in q's dtype, lse [H, rows] float32)."""
-    return (_native or _bind()).packed_attn_fwd(q, k, v, cu_q, cu_k, causal, out, lse, stream)
+    return (_native or _bind()).packed_attn_fwd(q, k, v, cu_q, cu_k, causal, out, lse, stream, workspace)

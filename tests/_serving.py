@@ -90,8 +90,8 @@ def bits(t):
     return t.contiguous().view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32).cpu()
 
 
-def packed_form(rows_q, rows_k, B, H, H_kv, d):
-    """(blocks of 32 rows, groups of wavefronts) of a packed bf16 launch's workgroups (csrc/lss_plan.h)"""
-    plan = (ctypes.c_int * 2)()
-    lss._check(lss.load().lss_plan_packed(*map(ctypes.c_int64, (rows_q, rows_k, B, H, H_kv, d)), plan))
+def packed_plan(rows_q, rows_k, B, H, H_kv, d, dtype=torch.bfloat16):
+    """(blocks of 32 rows, groups of wavefronts, key splits) of a packed launch (csrc/lss_plan.h)"""
+    plan = (ctypes.c_int * 3)()
+    lss._check(lss.load().lss_plan_packed(*map(ctypes.c_int64, (rows_q, rows_k, B, H, H_kv, d)), ctypes.c_int(dtype.itemsize), plan))
     return tuple(plan)

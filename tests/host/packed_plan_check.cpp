@@ -1,4 +1,4 @@
-// Goes over sizes of packed forward launches: every form that is chosen is one of the kernels that are built (lss_fwd_bf16.hip), and all of those
+// Goes over sizes of packed forward launches: splits only few rows' keys, and every bf16 form that is chosen is one of the kernels that are built (lss_fwd_bf16.hip), and all of those
 // are chosen somewhere.
 #include "lss_packed_plan.h"
 
@@ -16,13 +16,19 @@ int main()
             for (int64_t keys = 0; keys <= (int64_t)1 << 30; keys = keys * 7 / 3 + 1)
                 for (const auto &h : heads)
                     for (int64_t d = 64; d <= 128; d += 64) {
-                        const lss::PackedForm f = lss::pick_packed_form(rows, keys, B, h[0], h[1], d);
+                        const lss::PackedPlan f = lss::pick_packed_plan(rows, keys, B, h[0], h[1], d, 2);
                         const std::pair<int, int> form{f.row_blocks, f.groups};
                         if (!built[d / 128].count(form)) {
                             std::printf("no kernel of %d x %d for d = %d\n", f.row_blocks, f.groups, (int)d);
                             return 1;
                         }
                         seen[d / 128].insert(form);
+                        const lss::PackedPlan g = lss::pick_packed_plan(rows, keys, B, h[0], h[1], d, 4);
+                        for (const int splits : {f.splits, g.splits})       // (a lane each in the joining launch; none where rows alone fill the chip)
+                            if (splits < 1 || splits > 16 || (splits > 1 && rows * (h[0] / h[1]) * h[1] > 800 * 128)) {
+                                std::printf("%d splits of %lld rows\n", splits, (long long)rows);
+                                return 1;
+                            }
                     }
     if (seen[0] != built[0] || seen[1] != built[1]) {
         std::printf("a form is never chosen\n");

@@ -76,7 +76,7 @@ def _some(n, B, seed):
     ((4, 2), [500, 701], 3700, 32, 8, 128), ((2, 2), [300, 901], 100, 6, 2, 128), ((4, 1), _some(100, 70, 4), 0, 5, 1, 64)])
 def test_every_form_of_workgroup(form, n_q, old, H, H_kv, d, causal):
     n_k = [n + old for n in n_q]
-    assert sv.packed_form(sum(n_q), sum(n_k), len(n_q), H, H_kv, d) == form
+    assert sv.packed_plan(sum(n_q), sum(n_k), len(n_q), H, H_kv, d)[:2] == form
     q, k, v = (x.cuda() for x in _tensors(n_q, n_k, H, H_kv, d, torch.bfloat16, 150))
     cu_q, cu_k = sv.starts(n_q), sv.starts(n_k)
     out, lse = lss.lss_packed_attn_fwd(q, k, v, cu_q.cuda(), cu_k.cuda(), causal=causal)
@@ -91,6 +91,35 @@ def test_every_form_of_workgroup(form, n_q, old, H, H_kv, d, causal):
     sv.check(again[:sees], want[:sees], ob[:sees], "out in front")
     sv.check(lse_again, want_lse, lb, "lse with it")
     assert bool(torch.isnan(again[sees:]).all())
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,n_q,n_k,H,H_kv,d,splits", [
+    (torch.bfloat16, [64], [4100], 8, 2, 64, 8), (torch.bfloat16, [1, 3, 0], [2500, 3, 5000], 6, 1, 64, 8), (torch.bfloat16, [300], [9001], 8, 4, 64, 6),
+    (torch.bfloat16, [33, 70], [4100, 2100], 4, 4, 128, 8), (torch.bfloat16, [513], [3000], 8, 4, 128, 3), (torch.float32, [700], [700], 2, 2, 64, 5),
+    (torch.float32, [1, 40, 9], [900, 40, 1], 5, 1, 64, 2), (torch.float32, [130, 260], [1000, 260], 4, 2, 128, 4), (torch.float32, [300], [9001], 2, 1, 128, 16)])
+def test_key_splits(dtype, n_q, n_k, H, H_kv, d, splits, causal):
+    assert sv.packed_plan(sum(n_q), sum(n_k), len(n_q), H, H_kv, d, dtype)[2] == splits
+    q, k, v = (x.cuda() for x in _tensors(n_q, n_k, H, H_kv, d, dtype, 160))
+    cu_q, cu_k = sv.starts(n_q), sv.starts(n_k)
+    need = lss.lss_packed_attn_workspace_bytes(sum(n_q), sum(n_k), len(n_q), H, H_kv, d, dtype.itemsize)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    run = lambda: lss.lss_packed_attn_fwd(q, k, v, cu_q.cuda(), cu_k.cuda(), causal=causal, workspace=ws)
+    out, lse = run()
+    want, want_lse, ob, lb = (x.cpu() for x in _want(q, k, v, cu_q, cu_k, causal))
+    sv.check(out, want, ob, "out")
+    sv.check(lse, want_lse, lb, "lse")
+    assert all(torch.equal(sv.bits(a), sv.bits(b)) for a, b in zip(run(), (out, lse)))
+    # values that are not finite where the first sequence's last row alone sees them
+    v[n_k[0] - 1, :, 3] = float("inf")
+    again, _ = run()
+    if causal:
+        at = n_q[0] - 1
+        keep = torch.arange(sum(n_q)) != at
+        sv.check(again[keep.cuda()], want[keep], ob[keep], "the other rows")
+        assert not bool(torch.isfinite(again[at, :, 3]).any()) and bool(torch.isfinite(again[at, :, :3]).all())
+    with pytest.raises(ValueError, match="workspace of"):
+        lss.lss_packed_attn_fwd(q, k, v, cu_q.cuda(), cu_k.cuda(), workspace=ws[:-16])
 
 
 def test_many_sequences():
