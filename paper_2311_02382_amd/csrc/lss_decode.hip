@@ -26,14 +26,20 @@ namespace {
 
 constexpr int kWaves = 4, kWholeLen = 512;
 
-// Where a call's keys and values are more than half the last-level cache, they pass it by (non-temporal loads): 2.07 GB 366 -> 335 us, 268 MB 52 -> 47; but
-// 76 MB, of which two other calls' worth fits beside them, 17 -> 20.
-constexpr int64_t kStreamBytes = (int64_t)128 << 20;
+// Large calls' keys and values pass the last-level cache (256 MB) by, with non-temporal loads: 2.07 GB 378 -> 347 us, 268 MB 58.6 -> 53.1 with the first kernel that
+// had them.  From where?  Read again right away, calls gain from it up to its size (76 MB: 21.9 us, past it 23.3); after three or more others
+// of their size, as in a model of many layers, from 40 MB on they gain from staying out (41 MB: 18.2 -> 17.5, 111 MB: 30.6 -> 29.0, 196 MB: 54.6 -> 50.8).
+constexpr int64_t kStreamBytes = (int64_t)96 << 20;
+// Buffer loads: a lane past the end of the `bytes` from `first` on gets zeros and moves nothing -- the rows of a tile behind a sequence's last token, and those
+// of a page that is none.
 template <bool STREAM, typename V>
-__device__ __forceinline__ V load16(const V *p)
+__device__ __forceinline__ V load16(__amdgpu_buffer_rsrc_t buffer, uint32_t offset)
 {
-    if constexpr (STREAM) return __builtin_nontemporal_load(p);
-    else return *p;
+    return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(buffer, (int)offset, 0, STREAM ? 2 : 0));       // (2: non-temporal)
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const char *first, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(first), 0, (int)bytes, 0x00020000);       // (raw, 32-bit data)
 }
 
 // how a tile's keys and values meet the matrix cores
@@ -52,12 +58,12 @@ template <int D> struct Step<bf16_t, D> {
             if (there) q.f[i] = load_frag<bf16_t>(row + 32 * i + 8 * g);
         }
     }
-    // half i of a tile: 16 keys from `first` on, this lane's 16 bytes of the first step at lane_offset
+    // half i of a tile: 16 keys, this lane's 16 bytes of the first step at lane_offset
     template <bool STREAM>
-    static __device__ __forceinline__ void load_keys(Keys &k, int i, const char *first, uint32_t lane_offset)
+    static __device__ __forceinline__ void load_keys(Keys &k, int i, __amdgpu_buffer_rsrc_t half, uint32_t lane_offset)
     {
 #pragma unroll
-        for (int j = 0; j < NQ_FRAGS; ++j) k.f[i][j].v = load16<STREAM>(reinterpret_cast<const Vec *>(first + lane_offset + 64 * j));
+        for (int j = 0; j < NQ_FRAGS; ++j) k.f[i][j].v = load16<STREAM, Vec>(half, lane_offset + 64 * j);
     }
     // element e of half i: key 16 i + 4 (l / 16) + e, query l % 16
     static __device__ __forceinline__ f32x4 scores(const Keys &k, int i, const Queries &q)
@@ -110,10 +116,10 @@ template <int D> struct Step<float, D> {
         }
     }
     template <bool STREAM>
-    static __device__ __forceinline__ void load_keys(Keys &k, int i, const char *first, uint32_t lane_offset)
+    static __device__ __forceinline__ void load_keys(Keys &k, int i, __amdgpu_buffer_rsrc_t half, uint32_t lane_offset)
     {
 #pragma unroll
-        for (int j = 0; j < NQ_FRAGS; ++j) k.f[i][j] = load16<STREAM>(reinterpret_cast<const Vec *>(first + lane_offset + 64 * j));
+        for (int j = 0; j < NQ_FRAGS; ++j) k.f[i][j] = load16<STREAM, Vec>(half, lane_offset + 64 * j);
     }
     static __device__ __forceinline__ f32x4 scores(const Keys &k, int i, const Queries &q)
     {
@@ -261,12 +267,12 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
         Vec values[S::V_LOADS];
         bool ok[HALVES];                                // is there a page
         const auto load = [&](int j) __attribute__((always_inline)) {
-            if ((j >> a.pt.page_shift) - window_at >= 64) {
+            if ((j >> a.pt.page_shift) - window_at >= 64 && j < j_end) {
                 window_at += 64;
                 window = next_window;
                 next_window = numbers(window_at + 64);
             }
-            const char *k_row[HALVES], *v_row[HALVES];
+            __amdgpu_buffer_rsrc_t k_half[HALVES], v_half[HALVES];
 #pragma unroll
             for (int i = 0; i < HALVES; ++i) {
                 const int nth = (j + 16 * i) >> a.pt.page_shift;
@@ -275,43 +281,45 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
                 if (nth - window_at >= 64) page = __builtin_amdgcn_readlane(next_window, 0);
                 ok[i] = (uint32_t)page < (uint32_t)a.pt.n_pages && j + 16 * i < j_end;
                 const int64_t row = ((int64_t)(ok[i] ? page : 0) << a.pt.page_shift) + ((j + 16 * i) & ((1 << a.pt.page_shift) - 1));
-                k_row[i] = k_head + row * row_bytes;
-                v_row[i] = v_head_base + row * row_bytes;
+                const uint32_t bytes = ok[i] ? (uint32_t)(min(j_end - j - 16 * i, 16) - 1) * (uint32_t)row_bytes + D * (int)sizeof(T) : 0;
+                k_half[i] = buffer_of(k_head + row * row_bytes, bytes);
+                v_half[i] = buffer_of(v_head_base + row * row_bytes, bytes);
             }
 #pragma unroll
-            for (int i = 0; i < HALVES; ++i) S::template load_keys<STREAM>(keys, i, k_row[i], k_lane);
+            for (int i = 0; i < HALVES; ++i) S::template load_keys<STREAM>(keys, i, k_half[i], k_lane);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < S::V_LOADS; ++i) {
                 const int row = i * 64 / S::CHUNKS;        // (of lane 0)
-                values[i] = load16<STREAM>(reinterpret_cast<const Vec *>(v_row[row / 16] + (row & 15) * row_bytes + v_lane));
+                values[i] = load16<STREAM, Vec>(v_half[row / 16], v_lane + (uint32_t)(row & 15) * (uint32_t)row_bytes);
             }
+            __builtin_amdgcn_sched_barrier(0);
         };
-        if (j0 < j_end) load(j0);
-        for (; j0 < j_end; j0 += ROUND) {
-            f32x4 p[NQ][HALVES];
+        f32x4 p[NQ][HALVES];
+        // scores of a tile, its values to LDS ...
+        const auto scores = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < NQ; ++i)
 #pragma unroll
                 for (int hf = 0; hf < HALVES; ++hf) p[i][hf] = S::scores(keys, hf, qf[i]);
-            bool all_there = j0 + TILE <= j_end;
+            bool all_there = j + TILE <= j_end;
 #pragma unroll
             for (int hf = 0; hf < HALVES; ++hf) all_there = all_there && ok[hf];
             if (!all_there) {
-                // keys that are not there have weight 0, and their values, which may be anything, are taken as 0
+                // keys that are not there have weight 0 (and their values were loaded as 0)
 #pragma unroll
                 for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (!ok[hf] || j0 + 16 * hf + 4 * g + e >= j_end)
+                        if (!ok[hf] || j + 16 * hf + 4 * g + e >= j_end)
 #pragma unroll
                             for (int i = 0; i < NQ; ++i) p[i][hf][e] = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < S::V_LOADS; ++i)
-                    if (!ok[i * 64 / S::CHUNKS / 16] || j0 + (i * 64 + lane) / S::CHUNKS >= j_end) values[i] = Vec{};
             }
 #pragma unroll
             for (int i = 0; i < S::V_LOADS; ++i) S::store_value(mine, (i * 64 + lane) / S::CHUNKS, lane % S::CHUNKS, values[i]);
-            if (j0 + ROUND < j_end) load(j0 + ROUND);
+        };
+        // ... and their weights and sums
+        const auto sums_of = [&]() __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
                 float top = -INFINITY;
@@ -340,6 +348,12 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
                     }
             }
             S::template add_values<NQ>(mine, p, o, lane);
+        };
+        if (j0 < j_end) load(j0);
+        for (; j0 < j_end; j0 += ROUND) {
+            scores(j0);
+            if (j0 + ROUND < j_end) load(j0 + ROUND);
+            sums_of();
         }
         // the wavefronts' sums meet in LDS, in their order; 16 queries at a time
 #pragma unroll
@@ -449,20 +463,27 @@ __global__ __launch_bounds__(THREADS) void decode_merge_kernel(DecodeArgs a, con
     const auto part_of = [&](int i) { return i == 0 ? chain.w : (chain.w & ~1) + 2 * i; };
     const int grp = tid / LANES, col = tid % LANES * 4;
     for (int n = blockIdx.y; n < n_q; n += gridDim.y) {
-        float top = -INFINITY;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        float v_top = -INFINITY, v_sum = 0.f, top = -INFINITY;
+        if (grp < chain.count) {                        // (a thread's first part is on its way while the maximum is found)
+            v = *reinterpret_cast<const f32x4 *>(parts.values(part_of(grp), n) + col);
+            v_top = parts.sums(part_of(grp), n)[0];
+            v_sum = parts.sums(part_of(grp), n)[1];
+        }
         for (int i = lane; i < chain.count; i += 64) top = fmaxf(top, parts.sums(part_of(i), n)[0]);
         top = wave_max(top);
         const float top_use = top == -INFINITY ? 0.f : top;
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        float total = 0.f;
+        const float first = fast_exp2(v_top - top_use);
+        f32x4 sum = {first * v[0], first * v[1], first * v[2], first * v[3]};
+        float total = first * v_sum;
 #pragma unroll 4
-        for (int i = grp; i < chain.count; i += GROUPS) {
+        for (int i = grp + GROUPS; i < chain.count; i += GROUPS) {
             const int part = part_of(i);
             const float weight = fast_exp2(parts.sums(part, n)[0] - top_use);
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(parts.values(part, n) + col);
+            const f32x4 w = *reinterpret_cast<const f32x4 *>(parts.values(part, n) + col);
             total += weight * parts.sums(part, n)[1];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, v[e], sum[e]);
+            for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, w[e], sum[e]);
         }
         acc[grp][tid % LANES] = sum;
         if (tid % LANES == 0) totals[grp] = total;

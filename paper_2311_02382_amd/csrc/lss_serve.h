@@ -4,6 +4,8 @@
 #include "lss_common.h"
 #include "lss_kernels.h"
 
+#include <type_traits>
+
 namespace lss {
 
 // The sequence of packed row t: the last b in [0, B) with cu[b] <= t, if t < cu[b + 1] too, else -1.  By the whole wavefront, 64 starts at a
@@ -108,11 +110,19 @@ template <typename T> struct Vec16;
 template <> struct Vec16<bf16_t> { typedef bf16x8 type; };
 template <> struct Vec16<float> { typedef f32x4 type; };
 
-__device__ __forceinline__ float wave_max(float x)
+__device__ __forceinline__ float wave_max(float x)      // all lanes active
 {
-#pragma unroll
-    for (int sh = 32; sh >= 1; sh >>= 1) x = fmaxf(x, __shfl_xor(x, sh));
-    return x;
+    const auto step = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+        const int other = __builtin_amdgcn_update_dpp((int)0xff800000, __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+        x = fmaxf(x, __builtin_bit_cast(float, other));
+    };
+    step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 __device__ __forceinline__ float wave_total(float x)
 {
