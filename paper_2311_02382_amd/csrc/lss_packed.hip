@@ -5,45 +5,65 @@ namespace lss {
 
 namespace {
 
-// A wavefront per row and head: lse = log sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s, in the splits' order.  A row whose result is not finite is
-// done over, over the keys that it sees alone (packed_bf16_kernel).
+// D / 4 lanes per row and head, four columns each: lse = log sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s, in the splits' order (16 at most: a lane
+// of the row's each).  A row whose result is not finite is done over by the wavefront, over the keys that it sees alone (packed_bf16_kernel).  4155 rows of 8
+// heads of 64 in float, 2 splits, 25 MB: 8 us (a wavefront per row 14).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void packed_merge_kernel(PackedArgs a, PackedParts parts, const T *__restrict__ q, const T *__restrict__ k,
                                                            const T *__restrict__ v, T *__restrict__ out, float *__restrict__ lse)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (item >= (int64_t)a.rows_q * a.H) return;
-    const int t = (int)(item / a.H), h = (int)(item % a.H);
-    int begin, end;
-    const int b = find_sequence(a.cu_q, a.B, t, lane, begin, end);
-    if (b < 0) return;
-    const float mine = lane < parts.splits ? *parts.lse(a, lane, t, h) : -INFINITY, top = wave_max(mine), top_use = top == -INFINITY ? 0.f : top;
-    const float weight = fast_exp2((mine - top_use) * kLog2e), total = wave_total(lane < parts.splits ? weight : 0.f);
-    float sum[D / 64];
+    constexpr int LANES = D / 4, ROWS = 64 / LANES;
+    const int lane = threadIdx.x & 63, mine = lane % LANES;
+    const int items = a.rows_q * a.H, item = ((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6)) * ROWS + lane / LANES;     // (2^30 at most)
+    const int t = min(item, items - 1) / a.H, h = min(item, items - 1) - t * a.H;
+    // the row's sequence: a wavefront's rows are of one token or of neighbours
+    int b = -1, end = 0;
+    for (int i = 0; i < ROWS; ++i) {
+        const int ti = __builtin_amdgcn_readlane(t, i * LANES);
+        int begin_i, end_i;
+        const int bi = find_sequence(a.cu_q, a.B, ti, lane, begin_i, end_i);
+        for (; i < ROWS && __builtin_amdgcn_readlane(t, i * LANES) == ti; ++i)
+            if (lane / LANES == i) { b = bi; end = end_i; }
+        --i;
+    }
+    const bool there = item < items && b >= 0;
+    const float part_lse = there && mine < parts.splits ? *parts.lse(a, mine, t, h) : -INFINITY;
+    float top = part_lse;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) sum[i] = 0.f;
+    for (int sh = LANES / 2; sh >= 1; sh >>= 1) top = fmaxf(top, __shfl_xor(top, sh));
+    const float weight = fast_exp2((part_lse - (top == -INFINITY ? 0.f : top)) * kLog2e);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float total = 0.f;
+#pragma unroll 4
     for (int s = 0; s < parts.splits; ++s) {
-        const float *const from = parts.values(a, s, t, h);
-        const float w = __shfl(weight, s);
+        const float w = __shfl(weight, lane / LANES * LANES + s);
+        const f32x4 part = there ? *reinterpret_cast<const f32x4 *>(parts.values(a, s, t, h) + 4 * mine) : f32x4{0.f, 0.f, 0.f, 0.f};
+        total += w;
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) sum[i] = fmaf(w, from[lane + 64 * i], sum[i]);
+        for (int e = 0; e < 4; ++e) sum[e] = fmaf(w, part[e], sum[e]);
     }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
     bool finite = true;
-    T *const row = out + item * D;
+    if (there) {
+        T *const to = out + (int64_t)item * D + 4 * mine;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-        const float r = total == 0.f ? 0.f : sum[i] / total;
-        row[lane + 64 * i] = (T)r;
-        finite = finite && fabsf(r) < INFINITY;
+        for (int e = 0; e < 4; ++e) {
+            const float r = sum[e] * inv;
+            to[e] = (T)r;
+            finite = finite && fabsf(r) < INFINITY;
+        }
+        if (mine == 0) lse[(int64_t)h * a.rows_q + t] = total == 0.f ? -INFINITY : top + log2f(total) * kLn2;
     }
-    float *const to = lse + (int64_t)h * a.rows_q + t;
-    if (lane == 0) *to = total == 0.f ? -INFINITY : top + log2f(total) * kLn2;
-    if (__any(!finite)) {
-        const int h_kv = h / (a.H / a.H_kv), k_begin = max(0, min(a.cu_k[b], a.rows_k)), n_k = max(0, min(a.cu_k[b + 1], a.rows_k) - k_begin);
-        const int seen = a.causal ? max(0, min(n_k, n_k - (min(end, a.rows_q) - t) + 1)) : n_k;
-        row_attention<T, D>(q + t * a.q_stride + (int64_t)h * D, k + k_begin * a.k_stride + (int64_t)h_kv * D, a.k_stride,
-                            v + k_begin * a.v_stride + (int64_t)h_kv * D, a.v_stride, seen, lane, [](int j) { return (int64_t)j; }, row, to);
+    const uint64_t bad = __ballot(!finite);
+    for (int i = 0; i < ROWS; ++i) {
+        if ((bad >> (i * LANES) & ((uint64_t)1 << (LANES - 1) << 1) - 1) == 0) continue;
+        const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, i * LANES); };
+        const int ti = of(t), hi = of(h), bi = of(b), h_kv = hi / (a.H / a.H_kv);
+        const int k_begin = max(0, min(a.cu_k[bi], a.rows_k)), n_k = max(0, min(a.cu_k[bi + 1], a.rows_k) - k_begin);
+        const int seen = a.causal ? max(0, min(n_k, n_k - (min(of(end), a.rows_q) - ti) + 1)) : n_k;
+        row_attention<T, D>(q + ti * a.q_stride + (int64_t)hi * D, k + k_begin * a.k_stride + (int64_t)h_kv * D, a.k_stride,
+                            v + k_begin * a.v_stride + (int64_t)h_kv * D, a.v_stride, seen, lane, [](int j) { return (int64_t)j; },
+                            out + ((int64_t)ti * a.H + hi) * D, lse + (int64_t)hi * a.rows_q + ti);
     }
 }
 
@@ -58,7 +78,8 @@ hipError_t launch_packed(const PackedArgs &a, const T *q, const T *k, const T *v
     if constexpr (sizeof(T) == 2) e = launch_packed_bf16_main(a, plan, q, k, v, out, lse, parts, st);
     else e = launch_packed_f32_main(a, q, k, v, out, lse, parts, st);
     if (e != hipSuccess || plan.splits == 1) return e;
-    const dim3 grid((unsigned)(((int64_t)a.rows_q * a.H + 3) / 4)), block(256);
+    const int64_t rows_per_wg = 256 / (a.d / 4);
+    const dim3 grid((unsigned)(((int64_t)a.rows_q * a.H + rows_per_wg - 1) / rows_per_wg)), block(256);
     TimedLaunch tl(K_PACKED_MERGE, st);
     if (a.d == 64) hipLaunchKernelGGL((packed_merge_kernel<T, 64>), grid, block, 0, st, a, parts, q, k, v, out, lse);
     else hipLaunchKernelGGL((packed_merge_kernel<T, 128>), grid, block, 0, st, a, parts, q, k, v, out, lse);
