@@ -154,37 +154,19 @@ template <int D> struct Step<float, D> {
 // ---- which rounds a workgroup takes.  Sequence b has R_b = ceil(length / round) of them per virtual head (a head of keys and values and up to 16 NQ
 // query heads), at least one; the virtual heads of a sequence lie one behind the other, then the next sequence's.
 template <int ROUND>
-__device__ __forceinline__ int rounds_of(const DecodeArgs &a, int b)
-{
-    return (max(1, min(a.lengths[b], a.max_len)) + ROUND - 1) / ROUND;
-}
-// by whole wavefronts, 64 sequences at a time (a round is 64 tokens at least: 64 sequences have fewer than 2^31): rounds of all sequences, per virtual
-// head, ...
-template <int ROUND>
-__device__ __forceinline__ int64_t all_rounds(const DecodeArgs &a, int lane)
-{
-    int64_t sum = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64)
-        sum += __builtin_amdgcn_readlane(lane_sum_scan(b0 + lane < a.B ? rounds_of<ROUND>(a, b0 + lane) : 0), 63);
-    return sum;
-}
-// ... and the sequence that round `at` of those belongs to, with the rounds in front of it
-template <int ROUND>
-__device__ __forceinline__ int sequence_at(const DecodeArgs &a, int64_t at, int lane, int64_t &before)
-{
-    before = 0;
-    for (int b0 = 0;; b0 += 64) {
-        const int mine = b0 + lane < a.B ? rounds_of<ROUND>(a, b0 + lane) : 0, upto = lane_sum_scan(mine);
-        const uint64_t past = __ballot(before + upto > at);
-        if (past != 0) {
-            const int l = __ffsll((long long)past) - 1;
-            before += __builtin_amdgcn_readlane(upto - mine, l);
-            return b0 + l;
-        }
-        before += __builtin_amdgcn_readlane(upto, 63);
-        if (b0 + 64 >= a.B) return a.B - 1;
+__device__ __forceinline__ int rounds_of(const DecodeArgs &a, int length) { return (max(1, min(length, a.max_len)) + ROUND - 1) / ROUND; }
+// 64 sequences' rounds by a wavefront, a lane each, and the sums up to each (a round is 64 tokens at least: 64 sequences have fewer than 2^31)
+template <int ROUND> struct Rounds {
+    int length, mine, upto;
+    __device__ __forceinline__ Rounds(const DecodeArgs &a, int b0, int lane)
+    {
+        length = b0 + lane < a.B ? a.lengths[b0 + lane] : 0;
+        mine = b0 + lane < a.B ? rounds_of<ROUND>(a, length) : 0;
+        upto = lane_sum_scan(mine);
     }
-}
+    __device__ __forceinline__ int all() const { return __builtin_amdgcn_readlane(upto, 63); }
+};
+
 // Scratch memory.  What a part of a sequence leaves there for its query n of `rows`: sum of weight * value [d], maximum (log2 domain) and sum.  A
 // workgroup has room for two parts: 2 w for its first and, if it begins there, 2 w + 1 for its last.  And for the joining launch, the sequences that
 // more than one workgroup has: by sequence and virtual head where those are not more than the workgroups, else by the workgroup that one begins in (as
@@ -213,11 +195,11 @@ template <typename T, int D> struct Decode {
     static constexpr int REGION = TILE_BYTES > JOIN_BYTES ? TILE_BYTES : JOIN_BYTES;
 };
 
-// Rounds at .. end - 1, the first of which is of sequence b and virtual head v_head; `base`: the first of (b, virtual head 0).  WHOLE: all of (b, v_head).
+// Rounds at .. end - 1, the first of which is of sequence b, of `length` tokens, and virtual head v_head; `base`: the first of (b, virtual head 0).  WHOLE: all of (b, v_head).
 template <typename T, int D, int NQ, bool STREAM>
 __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, float (&sums)[kWaves][2][16], const T *__restrict__ q,
                                               const T *__restrict__ k_cache, const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,
-                                              float *__restrict__ scratch, bool whole, int64_t at, int64_t end, int64_t share, int64_t base, int b, int v_head)
+                                              float *__restrict__ scratch, bool whole, int64_t at, int64_t end, int64_t share, int64_t base, int b, int v_head, int length)
 {
     typedef Decode<T, D> C;
     typedef Step<T, D> S;
@@ -236,7 +218,7 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
     const float c = kLog2e / sqrtf((float)D);
     const int64_t start = at;
     while (at < end) {
-        const int n = max(0, min(a.lengths[b], a.max_len)), R = rounds_of<ROUND>(a, b);
+        const int R = rounds_of<ROUND>(a, length), n = max(0, min(length, a.max_len));
         const int64_t first = base + (int64_t)v_head * R;           // of this sequence and head
         const int r0 = whole ? 0 : (int)(at - first), r1 = whole ? R : (int)min<int64_t>(R, end - first);
         const int h_kv = v_head / groups, sub = v_head % groups, n_q = min(16 * NQ, G - sub * 16 * NQ), h0 = h_kv * G + sub * 16 * NQ;
@@ -407,6 +389,7 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
             base += (int64_t)R * v_heads;
             v_head = 0;
             ++b;
+            if (at < end) length = a.lengths[b];
         }
     }
 }
@@ -423,26 +406,41 @@ __global__ __launch_bounds__(64 * kWaves, parts_of(sizeof(T), D, NQ) / 256) void
     const int lane = threadIdx.x & 63;
     const int G = a.H / a.H_kv, groups = (G + 16 * NQ - 1) / (16 * NQ), v_heads = a.H_kv * groups;
     int64_t at = 0, end = 1, share = 0, base = 0, bytes;
-    int b, v_head;
+    int b, v_head, n;                                   // (n: of b's tokens)
     if (whole) {
         b = blockIdx.x / v_heads;
+        n = a.lengths[b];
         v_head = blockIdx.x % v_heads;
         bytes = (int64_t)a.B * a.max_len * a.H_kv * (2 * D * (int)sizeof(T));
     } else {
-        const int64_t rounds = all_rounds<C::ROUND>(a, lane), all = rounds * v_heads;
+        // rounds of all sequences, per virtual head
+        Rounds<C::ROUND> group(a, 0, lane);
+        int64_t rounds = group.all();
+        for (int b0 = 64; b0 < a.B; b0 += 64) rounds += Rounds<C::ROUND>(a, b0, lane).all();
+        const int64_t all = rounds * v_heads;
         bytes = rounds * a.H_kv * (C::ROUND * 2 * D * (int)sizeof(T));
         share = (all + PARTS - 1) / PARTS;
         at = blockIdx.x * share;
         end = min(at + share, all);
         if (threadIdx.x == 0 && (int64_t)a.B * v_heads > PARTS) Scratch{scratch, 0, D, PARTS}.chain(blockIdx.x)->b = -1;
         if (at >= end) return;
-        int64_t before;
-        b = sequence_at<C::ROUND>(a, divide(at, v_heads), lane, before);
-        base = before * v_heads;
-        v_head = (int)divide(at - base, rounds_of<C::ROUND>(a, b));
+        // the sequence that this workgroup's first round belongs to, and the rounds in front of it
+        const int64_t nth = divide(at, v_heads);
+        int64_t before = 0;
+        int b0 = 0;
+        while (before + group.all() <= nth) {           // (nth < rounds: some sequence has it)
+            before += group.all();
+            b0 += 64;
+            group = Rounds<C::ROUND>(a, b0, lane);
+        }
+        const int l = __ffsll((long long)__ballot(before + group.upto > nth)) - 1;
+        b = b0 + l;
+        n = __builtin_amdgcn_readlane(group.length, l);
+        base = (before + __builtin_amdgcn_readlane(group.upto - group.mine, l)) * v_heads;
+        v_head = (int)divide(at - base, rounds_of<C::ROUND>(a, n));
     }
-    if (bytes >= kStreamBytes) decode_rounds<T, D, NQ, true>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, whole, at, end, share, base, b, v_head);
-    else decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, whole, at, end, share, base, b, v_head);
+    if (bytes >= kStreamBytes) decode_rounds<T, D, NQ, true>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, whole, at, end, share, base, b, v_head, n);
+    else decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, whole, at, end, share, base, b, v_head, n);
 }
 
 // Joins the parts of the sequences that more than one workgroup had rounds of, in their order: workgroup x those of chain x, queries y, y + gridDim.y ..
