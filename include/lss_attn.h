@@ -422,7 +422,8 @@ int lss_gelu_bwd(const void *u, const void *dg, int64_t n, void *du, void *strea
  * follow.  Keys and values may have fewer heads than queries (H a multiple of H_kv; query head h reads head h / (H / H_kv)).
  * Rows of a tensor [rows, heads, d] lie `*_stride` elements apart (heads * d where it is contiguous, more for a slice of a wider product; a
  * multiple of 16 bytes, at most 2^23 elements), the heads of a row one behind the other.  elem_bytes 2: bf16, 4: float.  int32 arrays are DEVICE memory, read when the
- * kernels run: a captured call follows them.  Whatever they hold, nothing outside the tensors is read or written.
+ * kernels run: a captured call follows them.  Whatever they hold, nothing outside the tensors is read or written.  Outputs and workspace overlap no other
+ * operand but where it is said that they may (out between the first and the last byte of q: LSS_ERR_RANGE).
  *
  * The cache: k_cache, v_cache [n_pages, page_size, H_kv, d] contiguous; block_table [B, max_pages] int32: token p of sequence b lies in
  * page block_table[b, p / page_size], slot p % page_size.  Sequences may share pages.  A number outside [0, n_pages) is no page: nothing
@@ -440,7 +441,7 @@ int lss_gelu_bwd(const void *u, const void *dg, int64_t n, void *du, void *strea
  *   k_rot        NULL or [rows, H_kv, d] contiguous (written): the keys as they went into the cache; may be k where that is contiguous
  * The angle is taken in 64 bits, its cosine and sine and the products in 32, rounded to the tensors' type once.  Rows before cu_seqlens[0]
  * and from cu_seqlens[B] on are not touched.  A row whose position is negative or past its table goes into no cache.  Two rows that go to one place
- * (pages that are shared and written) leave either.  rows <= 2^24 (LSS_ERR_SHAPE otherwise).  Uses no workspace.
+ * (pages that are shared and written) leave parts of either.  rows <= 2^24 (LSS_ERR_SHAPE otherwise).  Uses no workspace.
  */
 int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
                      const int32_t *cu_seqlens, const int32_t *lengths, const int32_t *block_table,

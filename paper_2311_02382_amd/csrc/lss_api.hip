@@ -861,6 +861,15 @@ int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_s
     return LSS_OK;
 }
 
+// `out` [rows, heads, d] is written while other workgroups still read q
+static int check_apart(const char *what, const void *q, int64_t q_stride, const void *out, int64_t rows, int64_t heads, int64_t d, int elem_bytes)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(q), b = reinterpret_cast<uintptr_t>(out);
+    if (a < b + rows * heads * d * elem_bytes && b < a + ((rows - 1) * q_stride + heads * d) * elem_bytes)
+        return fail(LSS_ERR_RANGE, "%s: out lies over q", what);
+    return LSS_OK;
+}
+
 // The scratch of a call that needs `need` bytes: the caller's own (`*base`, `bytes`) if given, else the one registered for the current GPU
 static int get_scratch(const char *what, size_t need, void **base, size_t bytes)
 {
@@ -905,6 +914,7 @@ int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, 
     if (misaligned(workspace)) return fail(LSS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", what);
     if (int rc = check_arrays(what, {lengths, block_table, lse})) return rc;
     if (int rc = get_scratch(what, lss::paged_decode_workspace_bytes((int)H, (int)H_kv, (int)d, (int)max_len), &workspace, workspace_bytes)) return rc;
+    if (int rc = check_apart(what, q, q_stride, out, B, H, d, elem_bytes)) return rc;
     const lss::DecodeArgs a{pt, lengths, q_stride, (int)B, (int)H, (int)H_kv, (int)d, (int)max_len};
     const auto go = [&](auto zero) {
         typedef decltype(zero) T;
@@ -944,6 +954,7 @@ int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t 
     if (misaligned(workspace)) return fail(LSS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", what);
     if (int rc = check_arrays(what, {cu_q, cu_k, lse})) return rc;
     if (int rc = get_scratch(what, lss_packed_attn_workspace_bytes(rows_q, rows_k, B, H, H_kv, d, elem_bytes), &workspace, workspace_bytes)) return rc;
+    if (int rc = check_apart(what, q, q_stride, out, rows_q, H, d, elem_bytes)) return rc;
     const lss::PackedArgs a{cu_q, cu_k, q_stride, k_stride, v_stride, (int)rows_q, (int)rows_k, (int)B, (int)H, (int)H_kv, (int)d, causal ? 1 : 0};
     const auto go = [&](auto zero) {
         typedef decltype(zero) T;

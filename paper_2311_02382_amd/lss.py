@@ -327,7 +327,7 @@ def lss_paged_attn_decode(q, k_cache, v_cache, block_table, lengths, max_len=Non
     """Attention of one token per sequence, q [B, H, d], over the first lengths[b] tokens of its pages; H a multiple of H_kv.
 
     max_len: a bound on the lengths (a longer sequence counts as that long); None: what the tables hold.  workspace: a device tensor of
-    lss_paged_attn_workspace_bytes() bytes used by this call alone; None: the binding's buffer of that GPU.
+    lss_paged_attn_workspace_bytes() bytes used by this call alone; None: the binding's buffer of that GPU, for calls that do not overlap in time.
     Returns (out [B, H, d] in q's dtype, lse [B, H] float32)."""
     return (_native or _bind()).paged_attn_decode(q, k_cache, v_cache, block_table, lengths, max_len, out, lse, stream, workspace)
 
@@ -340,7 +340,7 @@ def lss_packed_attn_fwd(q, k, v, cu_q, cu_k=None, causal=True, out=None, lse=Non
     """Attention within each of the sequences that are packed one behind the other: q [rows, H, d] with starts cu_q int32 [B + 1],
     k, v [rows, H_kv, d] with starts cu_k (None: cu_q), H a multiple of H_kv.  With `causal` the rows of a sequence stand at the end of
     its keys: row r of n_q sees keys up to n_k - n_q + r.  workspace: a device tensor of lss_packed_attn_workspace_bytes() bytes used by this call
-    alone; None: the binding's buffer of that GPU.
+    alone; None: the binding's buffer of that GPU, for calls that do not overlap in time.
 
     Returns (out [rows, H, d] in q's dtype, lse [H, rows] float32)."""
     return (_native or _bind()).packed_attn_fwd(q, k, v, cu_q, cu_k, causal, out, lse, stream, workspace)

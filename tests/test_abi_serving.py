@@ -86,3 +86,12 @@ def test_scratch_of_packed_prompts(lib):
     for bad in ((0, 9000, 2, 4, 2, 64, 2), (60, -1, 2, 4, 2, 64, 2), (60, 9000, 0, 4, 2, 64, 2), (60, 9000, 2, 5, 2, 64, 2), (60, 9000, 2, 4, 2, 32, 2),
                 (60, 9000, 2, 4, 2, 64, 3)):
         assert need(*bad) == 0
+
+
+def test_out_over_q_is_refused(lib):
+    # decode: 2 rows of 4 heads of 64, 256 elements apart: 0x400 bytes from 0x1000; packed: 5 rows, 0xa00 bytes
+    for call, end in ((_decode, 0x1400), (_packed, 0x1a00)):
+        for out in (0x1000, 0x1010, end - 0x10, 0x1000 - (end - 0x1000) + 0x10):
+            assert call(lib, out=out) == -5 and "out lies over q" in lss.lss_last_error()
+    # rows further apart: 0x800 bytes from one to the next, the last one 0x200
+    assert _decode(lib, qs=1024, out=0x19f0) == -5 and _packed(lib, qs=1024, out=0x31f0) == -5

@@ -139,3 +139,57 @@ def test_starts_that_do_not_ascend_stay_within_the_tensors():
         torch.cuda.synchronize()
         assert bool((big_out[:32] == 7).all() and (big_out[32 + rows:] == 7).all() and (big_lse[:512] == 7).all() and (big_lse[512 + H * rows:] == 7).all())
         assert bool((k_cache[:5] == 7).all() and (k_cache[6:] == 7).all() and (v_cache[:5] == 7).all() and (v_cache[6:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype,rows,apart", [(torch.bfloat16, 700, 1 << 23), (torch.float32, 400, 1 << 23)])
+def test_rows_as_far_apart_as_they_may_be(dtype, rows, apart):
+    # every operand's rows lie 2^23 elements apart, past 2^32 elements; packed attention, append and attention of one token out of it
+    H, H_kv, d, page = 4, 2, 64, 16
+    wide = torch.empty(((rows - 1) * apart + 1024,), dtype=dtype, device="cuda")
+    q, k, v = (sv.normal(rows, h, d, seed=80 + i, dtype=dtype) for i, h in enumerate((H, H_kv, H_kv)))
+    views = []
+    for x, at in ((q, 0), (k, H * d), (v, H * d + H_kv * d)):
+        view = wide.as_strided(x.shape, (apart, d, 1), at)
+        view.copy_(x.cuda())
+        views.append(view)
+    counts = [rows - 150, 1, 149]
+    cu, lengths = sv.starts(counts).cuda(), torch.tensor(counts, dtype=torch.int32, device="cuda")
+    out, lse = lss.lss_packed_attn_fwd(*views, cu)
+    plain = lss.lss_packed_attn_fwd(q.cuda(), k.cuda(), v.cuda(), cu)
+    assert torch.equal(sv.bits(out), sv.bits(plain[0])) and torch.equal(sv.bits(lse), sv.bits(plain[1]))
+    table, n_pages = sv.tables(counts, page, 83)
+    k_cache, v_cache = (torch.empty(n_pages, page, H_kv, d, dtype=dtype, device="cuda") for _ in range(2))
+    q_rot, _ = lss.lss_paged_append(views[1], views[2], k_cache, v_cache, table.cuda(), lengths, cu_seqlens=cu, q=views[0])
+    assert torch.equal(q_rot.cpu(), q)
+    for b, n in enumerate(counts):
+        for cache, x in ((k_cache, k), (v_cache, v)):
+            got = cache[table[b, :-(-n // page)].long().cuda()].reshape(-1, H_kv, d)[:n]
+            assert torch.equal(got.cpu(), x[int(cu[b]):int(cu[b]) + n])
+    last = [int(cu[b + 1]) - 1 for b in range(3)]
+    far = wide.as_strided((3, H, d), (apart, d, 1), (rows - 3) * apart)
+    far.copy_(q[last].cuda())
+    got = lss.lss_paged_attn_decode(far, k_cache, v_cache, table.cuda(), lengths)
+    want = lss.lss_paged_attn_decode(q[last].cuda(), k_cache, v_cache, table.cuda(), lengths)
+    assert all(torch.equal(sv.bits(a), sv.bits(b)) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("n", [40, 1000])
+def test_prompts_whose_results_pass_32_bits(n):
+    # 2^26 rows of heads and more, over 2^32 elements: the first and the last two sequences hold numbers, zeros lie between them
+    H, H_kv, d = 64, 1, 64
+    B = (1 << 20) // n + 50
+    rows = B * n
+    q = torch.zeros(rows, H, d, dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.zeros(rows, H_kv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ends = [slice(0, n), slice(rows - 2 * n, rows - n), slice(rows - n, rows)]
+    for i, at in enumerate(ends):
+        for j, x in enumerate((q, k, v)):
+            x[at] = sv.normal(n, x.shape[1], d, seed=90 + 3 * i + j).cuda()
+    out, lse = lss.lss_packed_attn_fwd(q, k, v, sv.starts([n] * B).cuda())
+    for i, at in enumerate(ends):
+        for h in (0, 63):
+            some = torch.arange(0, n, 37)
+            want, want_lse, ob, lb = sv.attention(q[at][some, h].cpu(), k[at][:, 0].cpu(), v[at][:, 0].cpu(), some + 1, torch.bfloat16)
+            sv.check(out[at][some, h], want, ob, f"out of end {i}")
+            sv.check(lse[h, at][some], want_lse, lb, f"lse of end {i}")
+    assert not bool(out[n:rows - 2 * n].any())
