@@ -365,8 +365,9 @@ struct FwdView {
 };
 
 // Rows r0 .. r0 + 127: row_of(j) is where the result of row r0 + 32 (wavefront) + 16 j + lane % 16 goes, put(j, that, db, values) takes its columns 16 db +
-// 4 (lane / 16) .. + 3, normalised, put_lse(j, .) its lse.  `bh`: batch * head for the dropout's decisions.
-template <int D, bool DROP, typename RowOf, typename Put, typename PutLse>
+// 4 (lane / 16) .. + 3, normalised, put_lse(j, .) its lse.  `bh`: batch * head for the dropout's decisions.  PACKED: G heads of a token, perhaps more rows
+// than keys (a segment has none of that).
+template <int D, bool DROP, bool PACKED, typename RowOf, typename Put, typename PutLse>
 __device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const DropArgs &dr, int bh, int r0, int split, int n_splits, RowOf &&row_of,
                                              Put &&put, PutLse &&put_lse)
 {
@@ -381,7 +382,9 @@ __device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const
 
     // the keys any row of this tile sees, and this split's share of their tiles
     const int r_last = min(r0 + kRowsPerWg, s.l_s) - 1;
-    const int kv_end = s.causal ? (int)max<int64_t>(min<int64_t>(s.l_x, s.s0 + r_last / s.G + 1), 0) : s.l_x;
+    const int G = PACKED ? s.G : 1;
+    int kv_end = s.causal ? (int)min<int64_t>(s.l_x, s.s0 + r_last / G + 1) : s.l_x;
+    if (PACKED) kv_end = max(kv_end, 0);
     const int n_tiles = (kv_end + BC - 1) / BC, per = (n_tiles + n_splits - 1) / n_splits;
     const int t_begin = split * per, t_end = min(n_tiles, t_begin + per);
 
@@ -391,10 +394,12 @@ __device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const
     const float *const qp = s.q + g * 8;
     const auto row_at = [&](int j) {
         const int rr = min(r + 16 * j, s.l_s - 1);
-        return (int64_t)(rr / s.G) * s.q_ld + (rr % s.G) * D;
+        return (int64_t)(rr / G) * s.q_ld + (rr % G) * D;
     };
     const bool tiny = split_rows<D, 2>(qp, {row_at(0), row_at(1)}, qf);
-    const int position[2] = {(int)s.s0 + r / s.G, (int)s.s0 + (r + 16) / s.G}, first_position = (int)s.s0 + rw0 / s.G, last_position = (int)s.s0 + (rw0 + 31) / s.G;
+    // (a segment's positions are made from r again where they are wanted: kept, they cost d = 64 with dropout registers that it has not got)
+    const int kept[2] = {(int)s.s0 + r / G, (int)s.s0 + (r + 16) / G}, first_position = (int)s.s0 + rw0 / G, last_position = (int)s.s0 + (rw0 + 31) / G;
+    const auto position = [&](int j) { return PACKED ? kept[j] : (int)s.s0 + r + 16 * j; };
     if (tid == 0) *tiny_word = 0u;
     Sums<D, 2> o;
     o.clear();
@@ -404,7 +409,7 @@ __device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const
     if (DROP) {
         drop_cs = drop_col_seed(dr.seed_hi);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) drop_rk[j] = drop_row_key(dr.seed_lo, (uint32_t)bh, (uint32_t)position[j]);
+        for (int j = 0; j < 2; ++j) drop_rk[j] = drop_row_key(dr.seed_lo, (uint32_t)bh, (uint32_t)position(j));
     }
 
     int a_off[NS], t_off[D / 16];
@@ -431,7 +436,7 @@ __device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const
         if ((s.causal && jb + 31 > first_position) || jb + 32 > s.l_x) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int last = s.causal ? min(position[j], s.l_x - 1) : s.l_x - 1, rel = last - jb - 4 * g;
+                const int last = s.causal ? min(position(j), s.l_x - 1) : s.l_x - 1, rel = last - jb - 4 * g;
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     if (16 * (e >> 2) + (e & 3) > rel) sc.v[e >> 2][j][e & 3] = -INFINITY;
@@ -515,13 +520,13 @@ __device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const
         const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
         const float lse_nat = l_tot > 0.f ? (m[j] + log2f(l_tot)) * kLn2 : -INFINITY;
         if (r + 16 * j >= s.l_s) continue;
-        float *const to = row_of(j);
+        float *const to = row_of(r + 16 * j) + 4 * g;
 #pragma unroll
         for (int db = 0; db < D / 16; ++db) {
             const f32x4 a = o.v[db][j];
-            put(j, to, db, f32x4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv});
+            put(j, to + 16 * db, f32x4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv});
         }
-        if (g == 0) put_lse(j, lse_nat);
+        if (g == 0) put_lse(r + 16 * j, lse_nat);
     }
 }
 
@@ -540,17 +545,16 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void fwd_f32_kernel(SegShape 
     const int64_t ld = (int64_t)s.H * D, head = (int64_t)h * D;
     const FwdView view{q + (int64_t)b * s.l_s * ld + head, k + (int64_t)b * s.l_x * ld + head, v + (int64_t)b * s.l_x * ld + head, ld, ld, ld, s.s0, s.l_s,
                        s.l_x, s.causal, 1};
-    const int lane = threadIdx.x & 63, r = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32 + (lane & 15), g = lane >> 4;
-    const auto part_row = [&](int j) { return ((int64_t)split * bhs + bh) * s.l_s + r + 16 * j; };
-    fwd_f32_body<D, DROP>(
+    const auto part_row = [&](int row) { return ((int64_t)split * bhs + bh) * s.l_s + row; };
+    fwd_f32_body<D, DROP, false>(
         smem, view, dr, bh, r0, split, n_splits,
-        [&](int j) __attribute__((always_inline)) {
-            return n_splits == 1 ? out + ((int64_t)b * s.l_s + r + 16 * j) * ld + (int64_t)h * D : o_part + part_row(j) * D;
+        [&](int row) __attribute__((always_inline)) {
+            return n_splits == 1 ? out + ((int64_t)b * s.l_s + row) * ld + (int64_t)h * D : o_part + part_row(row) * D;
         },
-        [&](int, float *to, int db, const f32x4 &val) __attribute__((always_inline)) { *reinterpret_cast<f32x4 *>(to + db * 16 + 4 * g) = val; },
-        [&](int j, float v) __attribute__((always_inline)) {
-            if (n_splits == 1) lse[(int64_t)bh * s.l_s + r + 16 * j] = v;
-            else lse_part[part_row(j)] = v;
+        [&](int, float *to, const f32x4 &val) __attribute__((always_inline)) { *reinterpret_cast<f32x4 *>(to) = val; },
+        [&](int row, float v) __attribute__((always_inline)) {
+            if (n_splits == 1) lse[(int64_t)bh * s.l_s + row] = v;
+            else lse_part[part_row(row)] = v;
         });
 }
 
@@ -561,7 +565,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_f32_kernel(Packed
                                                                          PackedParts parts, int n_tiles)
 {
     __shared__ __attribute__((aligned(1024))) char smem[2 * PlaneTile<D>::BYTES + 16];
-    const int lane = threadIdx.x & 63, g = lane >> 4, G = a.H / a.H_kv;
+    const int lane = threadIdx.x & 63, G = a.H / a.H_kv;
     int h_kv, rank;
     if (!xcd_item(blockIdx.x, a.H_kv, SPLIT ? n_tiles * parts.splits : n_tiles, a.causal != 0, h_kv, rank)) return;
     const int split = SPLIT ? rank % parts.splits : 0;
@@ -570,20 +574,19 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_f32_kernel(Packed
     if (!packed_tile<kRowsPerWg>(a, G, rank, lane, t)) return;
     const FwdView view{q + (int64_t)t.q_begin * a.q_stride + (int64_t)h_kv * G * D, k + (int64_t)t.k_begin * a.k_stride + (int64_t)h_kv * D,
                        v + (int64_t)t.k_begin * a.v_stride + (int64_t)h_kv * D, a.q_stride, a.k_stride, a.v_stride, t.n_k - t.n_q, t.n_q * G, t.n_k, a.causal, G};
-    const int r0 = t.tile * kRowsPerWg, rw0 = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32, r = rw0 + (lane & 15);
+    const int r0 = t.tile * kRowsPerWg, rw0 = r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32;
     int token, head;
     bool finite[2] = {true, true};
-    fwd_f32_body<D, false>(
+    fwd_f32_body<D, false, true>(
         smem, view, DropArgs{}, 0, r0, split, parts.splits,      // (1 as a constant: 34 registers of d = 64 go to memory)
-        [&](int j) __attribute__((always_inline)) {
-            int row = r + 16 * j;
+        [&](int row) __attribute__((always_inline)) {
             asm volatile("" : "+v"(row));               // (so that its address is made here, not kept through the main loop)
             token = t.q_begin + row / G;
             head = h_kv * G + row % G;
             return SPLIT ? parts.values(a, split, token, head) : out + ((int64_t)token * a.H + head) * D;
         },
-        [&](int j, float *to, int db, const f32x4 &val) __attribute__((always_inline)) {
-            *reinterpret_cast<f32x4 *>(to + db * 16 + 4 * g) = val;
+        [&](int j, float *to, const f32x4 &val) __attribute__((always_inline)) {
+            *reinterpret_cast<f32x4 *>(to) = val;
             finite[j] = finite[j] && fabsf(val[0]) < INFINITY && fabsf(val[1]) < INFINITY && fabsf(val[2]) < INFINITY && fabsf(val[3]) < INFINITY;
         },
         [&](int, float v) __attribute__((always_inline)) {
