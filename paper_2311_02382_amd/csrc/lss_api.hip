@@ -1,6 +1,7 @@
 // C ABI of the segment-attention library: argument checks, workspace, dispatch.
 // Every entry point is documented in include/lss_attn.h.
 #include "lss_attn.h"
+#include "lss_cache_shape.h"
 #include "lss_common.h"
 #include "lss_kernels.h"
 #include "lss_plan.h"
@@ -817,10 +818,10 @@ static int check_cache(const char *what, int64_t B, int64_t H_kv, int64_t d, int
                        lss::PageTable *pt)
 {
     if (B < 0 || B > (int64_t)1 << 24) return fail(LSS_ERR_SHAPE, "%s: B = %lld (0 .. 2^24)", what, (long long)B);
-    if (page_size < 16 || page_size > 65536 || (page_size & (page_size - 1)) != 0)
+    if (!lss::cache_page_ok(page_size))
         return fail(LSS_ERR_SHAPE, "%s: page_size = %lld (a power of two from 16 to 65536)", what, (long long)page_size);
     if (n_pages < 1 || n_pages > INT32_MAX) return fail(LSS_ERR_SHAPE, "%s: n_pages = %lld (1 .. 2^31 - 1)", what, (long long)n_pages);
-    if (max_pages < 1 || max_pages * page_size > (int64_t)1 << 30 || max_pages > (int64_t)1 << 30)
+    if (!lss::cache_table_ok(max_pages, page_size))
         return fail(LSS_ERR_SHAPE, "%s: max_pages = %lld (at least 1, tables of at most 2^30 tokens)", what, (long long)max_pages);
     if (H_kv * d * page_size > (int64_t)1 << 29)
         return fail(LSS_ERR_SHAPE, "%s: pages of %lld elements (at most 2^29)", what, (long long)(H_kv * d * page_size));

@@ -590,7 +590,9 @@ PyObject *paged_attn_decode(PyObject *const *a)
     const Cache m = cache_of(kc, vc, table, lengths);
     const Rows rq = head_rows(q, "q");
     require(q.scalar_type() == m.dt && rq.rows == m.B && rq.d == m.d, "q must be [B, H, d] in the cache's dtype");
-    const int64_t max_len = none(a[5]) ? m.max_pages * m.page_size : integer(a[5]);
+    int64_t max_len;
+    if (!none(a[5])) max_len = integer(a[5]);
+    else if (__builtin_mul_overflow(m.max_pages, m.page_size, &max_len)) max_len = -1;      // (pages of no elements can be that long; refused as such)
     const at::Tensor out = output(a[6], q.sizes(), m.dt, q), lse = output(a[7], {m.B, rq.heads}, kF32, q);
     on_current_gpu({&q, &kc, &vc, &table, &lengths, &out, &lse});
     size_t wn = 0;
