@@ -2,6 +2,7 @@
 #include "lss_cache_shape.h"
 
 #include <cstdio>
+#include <initializer_list>
 
 int main()
 {
