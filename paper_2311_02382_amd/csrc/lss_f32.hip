@@ -518,7 +518,8 @@ __device__ __forceinline__ void fwd_f32_body(char *smem, const FwdView &s, const
         float l_tot = l[j] + __shfl_xor(l[j], 16);
         l_tot += __shfl_xor(l_tot, 32);
         const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-        const float lse_nat = l_tot > 0.f ? (m[j] + log2f(l_tot)) * kLn2 : -INFINITY;
+        const bool has_sum = PACKED ? l_tot != 0.f : l_tot > 0.f;       // (packed: a NaN among the scores is one in lse)
+        const float lse_nat = has_sum ? (m[j] + log2f(l_tot)) * kLn2 : -INFINITY;
         if (r + 16 * j >= s.l_s) continue;
         float *const to = row_of(r + 16 * j) + 4 * g;
 #pragma unroll
@@ -601,9 +602,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void packed_f32_kernel(Packed
         for (uint32_t rows = (uint32_t)(bad | bad >> 16 | bad >> 32 | bad >> 48) & 0xffffu; rows != 0; rows &= rows - 1) {
             const int again = rw0 + 16 * j + __builtin_ctz(rows), at = again / G, hd = h_kv * G + again % G;
             const int seen = a.causal ? max(0, min(t.n_k, t.n_k - t.n_q + at + 1)) : t.n_k;
-            row_attention<float, D>(view.q + (int64_t)at * a.q_stride + again % G * D, view.k, a.k_stride, view.v, a.v_stride, seen, lane,
-                                    [](int i) { return (int64_t)i; }, out + ((int64_t)(t.q_begin + at) * a.H + hd) * D,
-                                    lse + (int64_t)hd * a.rows_q + t.q_begin + at);
+            const float row_lse = lse[(int64_t)hd * a.rows_q + t.q_begin + at];
+            if (row_lse != row_lse) continue;
+            row_attention<float, D, 8>(view.q + (int64_t)at * a.q_stride + again % G * D, view.k, a.k_stride, view.v, a.v_stride, seen, row_lse, lane,
+                                    out + ((int64_t)(t.q_begin + at) * a.H + hd) * D);
         }
     }
 }

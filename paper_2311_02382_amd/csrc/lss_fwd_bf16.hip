@@ -402,10 +402,11 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
 
     const float l_own = l + __shfl_xor(l, 32);
     const float kept = DROP ? dr.scale : 1.f;           // of the kept weights: applied to their sum
+    const auto has_sum = [](float sum) { return PACKED ? sum != 0.f : sum > 0.f; };    // (packed: a NaN among the scores is one in lse)
     if constexpr (KG == 1) {
         const float inv = l_own > 0.f ? kept / l_own : 0.f;
         if (!row_ok) return;
-        if (hh == 0) put_lse(l_own > 0.f ? (m + log2f(l_own)) * kLn2 : -INFINITY);
+        if (hh == 0) put_lse(has_sum(l_own) ? (m + log2f(l_own)) * kLn2 : -INFINITY);
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
@@ -435,7 +436,7 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
             l_all += mg[g] * hand_ml(g)[1];
         }
         const float inv = l_all > 0.f ? kept / l_all : 0.f;
-        if (group == 0 && hh == 0) put_lse(l_all > 0.f ? (m_all + log2f(l_all)) * kLn2 : -INFINITY);
+        if (group == 0 && hh == 0) put_lse(has_sum(l_all) ? (m_all + log2f(l_all)) * kLn2 : -INFINITY);
         constexpr int PER = C::UNITS / KG;
         static_assert(C::UNITS % KG == 0, "");
 #pragma unroll
@@ -535,16 +536,17 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void packed_bf16_ker
             else lse[(int64_t)h * a.rows_q + token] = v;
         });
     // A key's weight is 0 for the rows of its block that do not see it, but 0 times a value that is not finite is NaN: rows with such a result are done over,
-    // over the keys that they see alone (of a tile whose keys are split: by packed_merge_kernel).
+    // over the keys that they see alone (of a tile whose keys are split: by packed_merge_kernel).  Not where lse is NaN: lse is made of the scores of seen keys alone.
     if (SPLIT) return;
     if (KG > 1) __syncthreads();                // (the groups have written parts of one row)
     const uint64_t bad = __ballot(!finite);
     for (uint32_t rows = (uint32_t)bad | (uint32_t)(bad >> 32); rows != 0; rows &= rows - 1) {
         const int again = rw0 + __builtin_ctz(rows), at = again / G, head = h_kv * G + again % G;
         const int seen = a.causal ? max(0, min(t.n_k, t.n_k - t.n_q + at + 1)) : t.n_k;
-        row_attention<bf16_t, D>(view.q + (int64_t)at * a.q_stride + again % G * D, view.k, a.k_stride, view.v, a.v_stride, seen, lane,
-                                 [](int j) { return (int64_t)j; }, out + ((int64_t)(t.q_begin + at) * a.H + head) * D,
-                                 lse + (int64_t)head * a.rows_q + t.q_begin + at);
+        const float row_lse = lse[(int64_t)head * a.rows_q + t.q_begin + at];
+        if (row_lse != row_lse) continue;
+        row_attention<bf16_t, D, 8>(view.q + (int64_t)at * a.q_stride + again % G * D, view.k, a.k_stride, view.v, a.v_stride, seen, row_lse, lane,
+                                 out + ((int64_t)(t.q_begin + at) * a.H + head) * D);
     }
 }
 

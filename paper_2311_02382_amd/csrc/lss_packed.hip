@@ -43,6 +43,7 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedArgs a, PackedP
         for (int e = 0; e < 4; ++e) sum[e] = fmaf(w, part[e], sum[e]);
     }
     const float inv = total == 0.f ? 0.f : 1.f / total;
+    const float row_lse = total == 0.f ? -INFINITY : top + log2f(total) * kLn2;
     bool finite = true;
     if (there) {
         T *const to = out + (int64_t)item * D + 4 * mine;
@@ -52,18 +53,18 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedArgs a, PackedP
             to[e] = (T)r;
             finite = finite && fabsf(r) < INFINITY;
         }
-        if (mine == 0) lse[(int64_t)h * a.rows_q + t] = total == 0.f ? -INFINITY : top + log2f(total) * kLn2;
+        if (mine == 0) lse[(int64_t)h * a.rows_q + t] = row_lse;
     }
-    const uint64_t bad = __ballot(!finite);
+    const uint64_t bad = __ballot(!finite && row_lse == row_lse);
     for (int i = 0; i < ROWS; ++i) {
         if ((bad >> (i * LANES) & ((uint64_t)1 << (LANES - 1) << 1) - 1) == 0) continue;
         const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, i * LANES); };
         const int ti = of(t), hi = of(h), bi = of(b), h_kv = hi / (a.H / a.H_kv);
         const int k_begin = max(0, min(a.cu_k[bi], a.rows_k)), n_k = max(0, min(a.cu_k[bi + 1], a.rows_k) - k_begin);
         const int seen = a.causal ? max(0, min(n_k, n_k - (min(of(end), a.rows_q) - ti) + 1)) : n_k;
-        row_attention<T, D>(q + ti * a.q_stride + (int64_t)hi * D, k + k_begin * a.k_stride + (int64_t)h_kv * D, a.k_stride,
-                            v + k_begin * a.v_stride + (int64_t)h_kv * D, a.v_stride, seen, lane, [](int j) { return (int64_t)j; },
-                            out + ((int64_t)ti * a.H + hi) * D, lse + (int64_t)hi * a.rows_q + ti);
+        row_attention<T, D, 2>(q + ti * a.q_stride + (int64_t)hi * D, k + k_begin * a.k_stride + (int64_t)h_kv * D, a.k_stride,
+                            v + k_begin * a.v_stride + (int64_t)h_kv * D, a.v_stride, seen, __builtin_bit_cast(float, of(__builtin_bit_cast(int, row_lse))), lane,
+                            out + ((int64_t)ti * a.H + hi) * D);
     }
 }
 

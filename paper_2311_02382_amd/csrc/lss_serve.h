@@ -131,50 +131,51 @@ __device__ __forceinline__ float wave_total(float x)
     return x;
 }
 
-// Attention of one query row against n_keys keys by one wavefront: lanes own keys for the scores and columns lane, lane + 64, ..
-// for the sum of the values, everything in fp32.  row_of(j): key j's row in k and v, or -1 for a key that is not there.  A
-// value is multiplied only where its key is seen, so that what lies in other rows cannot reach the result.
-template <typename T, int D, typename F>
-__device__ void row_attention(const T *q, const T *k, int64_t k_stride, const T *v, int64_t v_stride, int n_keys, int lane, F row_of, T *out,
-                              float *lse)
+// Attention of one query row against the first n_keys keys by one wavefront, everything in fp32, for rows whose log-sum-exp is known and whose result was spoilt by
+// a value that the row does not see: a value is multiplied only where its key is seen here.  64 keys at a time, a lane each for the scores; then each lane's 16 bytes
+// of every (64 / CHUNKS)th value, LOADS loads on their way at once.  The weights' own sum divides them, so that the log-sum-exp's rounding does not matter.
+// (Keys and values one by one, a broadcast each: 1000 cycles a key.)
+template <typename T, int D, int LOADS>
+__device__ __forceinline__ void row_attention(const T *q, const T *k, int64_t k_stride, const T *v, int64_t v_stride, int n_keys, float lse, int lane, T *out)
 {
     typedef typename Vec16<T>::type Vec;
-    constexpr int VEC = 16 / sizeof(T);
-    const float c = kLog2e / sqrtf((float)D);
-    float acc[D / 64], m = -INFINITY, l = 0.f;
+    constexpr int VEC = 16 / sizeof(T), CHUNKS = D / VEC, KEYS = 64 / CHUNKS;
+    const float c = kLog2e / sqrtf((float)D), top = lse * kLog2e;
+    if (lse == -INFINITY) n_keys = 0;                   // no key, or none with a weight: zeros
+    const int mine = lane / CHUNKS, column = lane % CHUNKS * VEC;
+    float acc[VEC], l = 0.f;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) acc[i] = 0.f;
+    for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
     for (int j0 = 0; j0 < n_keys; j0 += 64) {
-        const int64_t row = j0 + lane < n_keys ? row_of(j0 + lane) : -1;
-        float s = -INFINITY;
-        if (row >= 0) {
-            s = 0.f;
-#pragma unroll 2                                        // (its registers must not add to those of the kernels that fall back on it)
-            for (int i = 0; i < D; i += VEC) {
-                const Vec a = *reinterpret_cast<const Vec *>(q + i), b = *reinterpret_cast<const Vec *>(k + row * k_stride + i);
+        const T *const key = k + min(j0 + lane, n_keys - 1) * k_stride;
+        float s = 0.f;
+#pragma unroll (LOADS < 4 ? LOADS : 4)
+        for (int i = 0; i < D; i += VEC) {
+            const Vec a = *reinterpret_cast<const Vec *>(q + i), b = *reinterpret_cast<const Vec *>(key + i);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) s = fmaf((float)a[e], (float)b[e], s);
-            }
+            for (int e = 0; e < VEC; ++e) s = fmaf((float)a[e], (float)b[e], s);
         }
-        s *= c;
-        const float m_new = fmaxf(m, wave_max(s)), m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = fast_exp2(m - m_use), p = row >= 0 ? fast_exp2(s - m_use) : 0.f;
-        m = m_new;
-        l = l * alpha + wave_total(p);
+        const float p = j0 + lane < n_keys ? fast_exp2(s * c - top) : 0.f;
+        l += p;
+#pragma unroll LOADS
+        for (int i = 0; i < CHUNKS; ++i) {
+            const int at = j0 + i * KEYS + mine;
+            const Vec x = *reinterpret_cast<const Vec *>(v + min(at, n_keys - 1) * v_stride + column);
+            const float w = __shfl(p, i * KEYS + mine);
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) acc[i] *= alpha;
-        for (int j = 0; j < min(64, n_keys - j0); ++j) {
-            const int64_t at = __shfl(row, j);
-            const float w = __shfl(p, j);
-            if (at < 0) continue;
-#pragma unroll
-            for (int i = 0; i < D / 64; ++i) acc[i] = fmaf(w, (float)v[at * v_stride + lane + 64 * i], acc[i]);
+            for (int e = 0; e < VEC; ++e) acc[e] = fmaf(w, at < n_keys ? (float)x[e] : 0.f, acc[e]);
         }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;         // no key: zeros and -infinity
+    l = wave_total(l);
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    Vec r;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) out[lane + 64 * i] = (T)(acc[i] * inv);
-    if (lane == 0) *lse = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    for (int e = 0; e < VEC; ++e) {
+#pragma unroll
+        for (int sh = CHUNKS; sh < 64; sh *= 2) acc[e] += __shfl_xor(acc[e], sh);
+        r[e] = (T)(acc[e] * inv);
+    }
+    if (lane < CHUNKS) *reinterpret_cast<Vec *>(out + column) = r;
 }
 
 } // namespace lss
