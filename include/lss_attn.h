@@ -439,7 +439,7 @@ int lss_gelu_bwd(const void *u, const void *dg, int64_t n, void *du, void *strea
  *                as they are.  x_i, y_i: columns i and i + rot_dim / 2 of a head, with `interleaved` 2 i and 2 i + 1
  *   q, q_rot     [rows, H, d]; both or neither NULL.  q_rot contiguous (written), may be q where that is contiguous
  *   k_rot        NULL or [rows, H_kv, d] contiguous (written): the keys as they went into the cache; may be k where that is contiguous
- * The angle is taken in 64 bits, its cosine and sine and the products in 32, rounded to the tensors' type once.  Rows before cu_seqlens[0]
+ * The angle is taken in 64 bits to within half a turn, what is left of it, its cosine and sine and the products in 32, rounded to the tensors' type once.  Rows before cu_seqlens[0]
  * and from cu_seqlens[B] on are not touched.  A row whose position is negative or past its table goes into no cache.  Two rows that go to one place
  * (pages that are shared and written) leave parts of either.  rows <= 2^24 (LSS_ERR_SHAPE otherwise).  Uses no workspace.
  */
@@ -458,7 +458,7 @@ int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_s
  *   max_len  bound on the lengths, at most max_pages * page_size: a longer sequence counts as that long
  *   workspace  DEVICE buffer of lss_paged_attn_workspace_bytes(H, H_kv, d, max_len) bytes (0 where max_len is small), 16-byte aligned;
  *            NULL: the one registered with lss_set_workspace().  Calls that overlap in time on one GPU need a buffer each
- * B * H <= 2^23 (LSS_ERR_SHAPE otherwise).  Arithmetic and accumulation in fp32.  What lies in a page behind a sequence's last token does not reach the result.
+ * B * H <= 2^23 (LSS_ERR_SHAPE otherwise).  Scores, sums and lse in fp32; bf16: a weight multiplies values as two bf16 parts, off by 2^-16 of it at most, and the result is rounded once.  What lies in a page behind a sequence's last token does not reach the result.
  */
 size_t lss_paged_attn_workspace_bytes(int64_t H, int64_t H_kv, int64_t d, int64_t max_len);
 int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
@@ -478,6 +478,8 @@ int lss_paged_attn_decode(const void *q, int64_t q_stride, const void *k_cache, 
  * that row is computed a second time over the keys that it sees: a call all of whose rows see an infinite value takes 20 to 75 times as long.
  *   workspace  DEVICE buffer of lss_packed_attn_workspace_bytes(rows_q, rows_k, B, H, H_kv, d, elem_bytes) bytes (0 for many rows), 16-byte aligned;
  *         NULL: the one registered with lss_set_workspace().  Calls that overlap in time on one GPU need a buffer each
+ * Scores, sums and lse in fp32; bf16: weights are rounded to bf16 before they multiply values (off by 2^-8 of each at most), and the result is rounded once; float: products of
+ * three-part operands, as in lss_segment_attn_fwd.
  * rows_q * H <= 2^30, B * H_kv <= 2^22, rows_k <= 2^30 (LSS_ERR_SHAPE otherwise).
  */
 size_t lss_packed_attn_workspace_bytes(int64_t rows_q, int64_t rows_k, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes);

@@ -1,6 +1,6 @@
 // Attention of one token per sequence over a paged cache of keys and values.
 //
-// A sequence's keys and values are read once, by groups of up to 16 or 32 query heads that share their head: what bounds it is
+// A sequence's keys and values are read once by every group of up to 32 query heads that share their head (so once, but for more than 32 of them): what bounds it is
 // those bytes.  Work is counted in rounds of one tile per wavefront (4 x 32 keys in bf16, 4 x 16 in float); the
 // rounds of all sequences and heads, one behind the other, are dealt out in equal parts to as many workgroups as the chip holds at once, so that
 // sequences of any lengths fill it evenly.  A part that is not all of its sequence goes to scratch memory, two at most per
@@ -18,7 +18,8 @@
 // both are positive, so that an infinite value gives infinity as the definition has it, not the NaN of parts of either sign or of 0 times it.
 //
 // 128 sequences of 2048 to 6500 tokens, 8 heads of 128 for 32, 2.07 GB: 336 us, 6.2 TB/s (plain reads of as much: 7.06; with one head of keys, whose rows
-// lie one behind the other, 6.5); 76 MB in 24 ragged sequences 21.2 us, of which the first loads of a workgroup take 5 and the second launch 4.
+// lie one behind the other, 6.5); 76 MB in 24 ragged sequences 21.0 us, of which the first loads of a workgroup take 5 and the second launch 4,
+// and whole rounds: 1296 of them for 512 workgroups, 432 of which take three and 80 none.
 // Built, measured and longer: the heads of a sequence side by side in neighbouring workgroups (the same tokens at the same time: 357 us against
 // 338 for the large one); at d = 64 two tiles on their way and three workgroups a compute unit instead of four (98 sequences in float 172 us, 153); at d = 128 three
 // workgroups (registers to memory: 490) -- or two tiles on their way, likewise.

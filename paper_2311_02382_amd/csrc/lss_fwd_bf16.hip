@@ -498,7 +498,7 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void fwd_bf16_kernel
 // Packed sequences (lss_packed_attn_fwd).  A row of a workgroup is a query head of a token: the G heads that share a head of keys and values are
 // neighbours, so that a tile of keys serves 128 / G tokens of all of them, the causal diagonal crosses fewer of a wavefront's blocks,
 // and short prompts fill the rows.  Matrix and vector work bound it, as in a segment: 24,576 rows, 16 heads of 64, 4 of keys 1.21 ms (1020 TFLOP/s, matrix units
-// busy 60 % of the cycles, vector ALU 86 %); nine prompts of 205 to 4108 rows, 32 heads of 128, 8 of keys 249 us (910; 50 and 48 %: one in ten of a tile's
+// busy 60 % of the cycles, vector ALU 86 %); nine prompts of 205 to 4108 rows, 32 heads of 128, 8 of keys 248 us (911; 49 and 48 %: one in ten of a tile's
 // cycles is its start and end, and short prompts' last tiles of keys are half masked).  Weights are rounded to bf16 before they multiply the values (off by at most 2^-8
 // of each): two parts, as for single tokens, would be half as much matrix work again.
 template <int D, int RB, int KG, bool SPLIT>

@@ -13,7 +13,8 @@ namespace {
 constexpr int kAppendThreads = 256, kAppendRows = 2, kAppendUnits = 3;
 
 // ---- append.  Row t of the packed rows has position lengths[b] - (rows of b) + (t - cu[b]).  What bounds it is the bytes it moves, or in a step of single tokens
-// its launch and four dependent loads.  A workgroup takes two rows (one of few): one wavefront each finds the way from row to cache row; then one thread per angle
+// its launch and two loads that wait for one another, length and page number (of rows that are found in the starts, two more), and inv_freq's, which waits for nothing
+// but is issued behind the first barrier.  A workgroup takes two rows (one of few): one wavefront each finds the way from row to cache row; then one thread per angle
 // turns positions into cosines and sines, which serve all heads of a row through LDS; then 32 bytes per thread and unit are rotated and stored.  A thread's first
 // three units are loaded before all that: where they lie does not depend on it.  6904 rows of 32 + 8 + 8 heads of 128, keys also
 // to a tensor of their own, 184 MB: 32.7 us, 5.6 TB/s (a copy of as much: 29.4); loaded behind the angles, four rows, 46.6; with loads that stay in the caches 40.4.
