@@ -449,6 +449,13 @@ int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_s
                      int64_t n_pages, int64_t page_size, int64_t max_pages,
                      const double *inv_freq, int64_t rot_dim, int interleaved,
                      void *k_cache, void *v_cache, void *q_rot, void *k_rot, void *stream);
+/* lss_paged_append with `positions` [rows] int32: row t is rotated by positions[t] in place of p (the tokens of a drafted tree by their depth); NULL: by p. */
+int lss_paged_append_ex(const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride,
+                        const int32_t *cu_seqlens, const int32_t *lengths, const int32_t *block_table, const int32_t *positions,
+                        int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes,
+                        int64_t n_pages, int64_t page_size, int64_t max_pages,
+                        const double *inv_freq, int64_t rot_dim, int interleaved,
+                        void *k_cache, void *v_cache, void *q_rot, void *k_rot, void *stream);
 
 /*
  * Attention of one token per sequence over its pages:
@@ -487,6 +494,81 @@ int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t 
                         const int32_t *cu_q, const int32_t *cu_k, int64_t rows_q, int64_t rows_k,
                         int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes, int causal,
                         void *workspace, size_t workspace_bytes, void *out, float *lse, void *stream);
+
+/*
+ * Several continuations of a sequence over the cache: beams, and trees of drafted tokens.  A step of beam search is lss_beam_select, lss_paged_fork, lss_paged_append,
+ * lss_paged_attn_decode; a step with drafted tokens lss_paged_append_ex (positions: the tokens' depths), lss_paged_attn_tree, and when the model has answered
+ * lss_paged_compact.  As above, int32 arrays are DEVICE memory that a captured call follows, and whatever they hold, nothing outside the tensors is read or written.
+ *
+ * lss_paged_attn_tree: rows cu_q[b] .. cu_q[b + 1] - 1 of q are sequence b's n_b drafted tokens, the last of its L_b = min(lengths[b], max_len).  Row t sees key j if
+ *     j < L_b - n_b,  or drafted token c = j - (L_b - n_b) is named by bit c % 64 of tree[t, c / 64];  tree NULL: c <= t - cu_q[b]
+ *   q     [rows, H, d];  out [rows, H, d] contiguous (written);  lse [rows, H] float (written)
+ *   cu_q  [B + 1] int32, ascending
+ *   tree  [rows, words] int64 or NULL; a drafted token past its words is seen by nobody.  A row sees itself only where its own bit is set
+ *   workspace  DEVICE buffer of lss_paged_attn_tree_workspace_bytes() bytes, 16-byte aligned; NULL: the one registered with lss_set_workspace().  Calls that
+ *              overlap in time on one GPU need a buffer each
+ * A row that sees no key gives zeros and lse = -infinity; a key that a row does not see does not reach its result, whatever its value.  Rows of no sequence are
+ * not touched.  rows * H <= 2^24, words <= 1024 (LSS_ERR_SHAPE otherwise).
+ */
+size_t lss_paged_attn_tree_workspace_bytes(int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int64_t max_len, int elem_bytes);
+int lss_paged_attn_tree(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
+                        const int32_t *lengths, const int32_t *block_table, const int32_t *cu_q, const int64_t *tree, int64_t words,
+                        int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes,
+                        int64_t n_pages, int64_t page_size, int64_t max_pages, int64_t max_len,
+                        void *workspace, size_t workspace_bytes, void *out, float *lse, void *stream);
+
+/*
+ * lss_paged_fork: B_out sequences from B.  Sequence s has the lengths[p] tokens of its parent p = parents[s] and room for room[s] more:
+ *   * full pages are its parent's, shared by all that name them;
+ *   * a partly filled one, where it has room (so that it will be written into): the lowest sequence that writes into it keeps it if all that have it do and it is not
+ *     held, the others take a new page, into which the tokens of K and V in it are copied;
+ *   * new pages up to token lengths[p] + room[s]; entries behind them are -1.
+ * New pages are those that no sequence of the result has from its parent and that are not held, the lowest numbers first, in the order of (sequence, page).
+ *   lengths [B], block_table [B, max_pages]  the sequences before, only read.  A sequence that is nobody's parent leaves its pages free
+ *   parents [B_out]  a number outside [0, B): a sequence without tokens
+ *   room    [B_out], negative ones count as 0; NULL: 1 for each that has a parent
+ *   held    [n_pages] or NULL: not 0 where somebody else has the page
+ *   table_out [B_out, max_pages], lengths_out [B_out]: lengths[p] + room[s], at most what a table holds (written)
+ *   missing [1] (written): pages that there were too few of, or that the tables have no entry for; their entries are -1, a partly filled page's that could not be
+ *           copied too.  Nothing that the old table names has been written then, so the call can be made again from it
+ *   workspace  DEVICE buffer of lss_paged_fork_workspace_bytes() bytes, 16-byte aligned; NULL: the registered one
+ * An entry that names no page stays one that names none.  Outputs lie over no input (LSS_ERR_RANGE).  B, B_out <= 2^20 (LSS_ERR_SHAPE otherwise).
+ */
+size_t lss_paged_fork_workspace_bytes(int64_t n_pages, int64_t B_out);
+int lss_paged_fork(const int32_t *lengths, const int32_t *block_table, const int32_t *parents, const int32_t *room, const int32_t *held,
+                   int64_t B, int64_t B_out, int64_t H_kv, int64_t d, int elem_bytes,
+                   int64_t n_pages, int64_t page_size, int64_t max_pages, void *workspace, size_t workspace_bytes,
+                   void *k_cache, void *v_cache, int32_t *table_out, int32_t *lengths_out, int32_t *missing, void *stream);
+
+/*
+ * lss_paged_compact: of sequence b's n_b = cu_q[b + 1] - cu_q[b] last tokens (of lengths[b]) the kept ones move to their front:
+ *     token lengths[b] - n_b + i  becomes what token lengths[b] - n_b + kept[b, i] was,  i < m_b = min(n_kept[b], max_kept, n_b)
+ *   kept [B, max_kept], n_kept [B]: numbers below n_b, ascending; one that is not (or below its place i) leaves its place as it is, or with another's of the list
+ *   lengths_out [B] (written): lengths[b] - n_b + m_b.  It lies over no input (LSS_ERR_RANGE)
+ * Tokens without a page neither move nor are moved to.  Uses no workspace.  B <= 2^18 (LSS_ERR_SHAPE otherwise).
+ */
+int lss_paged_compact(const int32_t *lengths, const int32_t *block_table, const int32_t *cu_q, const int32_t *kept, const int32_t *n_kept,
+                      int64_t max_kept, int64_t B, int64_t H_kv, int64_t d, int elem_bytes,
+                      int64_t n_pages, int64_t page_size, int64_t max_pages, void *k_cache, void *v_cache, int32_t *lengths_out, void *stream);
+
+/*
+ * lss_beam_select: for each of B prompts the n_out best continuations (beam k < K, token v < V) by
+ *     total(k, v) = scores[b, k] + logits[b K + k, v] - log sum_u exp(logits[b K + k, u]),
+ * best first, of equal totals the lower k V + v.
+ *   logits    [B K, V], rows `stride` elements apart, elem_bytes 2 (bf16) or 4 (float), aligned to its elements
+ *   scores    [B, K] float
+ *   finished  [B, K] bytes or NULL: not 0 for beams that have ended, whose one continuation is (end_token, total scores[b, k])
+ *   end_token in [0, V); -1: none (finished and finished_out NULL)
+ *   scores_out, parents, tokens [B, n_out] (written): total, b K + k, v.  finished_out [B, n_out] bytes or NULL (written): 1 if the beam had ended or v is end_token
+ *   workspace DEVICE buffer of lss_beam_select_workspace_bytes() bytes (0 where V is small), 16-byte aligned; NULL: the registered one
+ * No continuation: of a beam whose score is not finite or whose row's log-sum-exp is not (a NaN or +infinity in it, nothing but -infinity); a logit of -infinity.
+ * Where there are fewer than n_out: -infinity, -1, -1 and 1.  Within a beam logits are compared as they are; totals are made and compared in 64 bits, of a
+ * log-sum-exp that is off by 2^-19 at most (alike for rows that are).  K, n_out <= 64, K V < 2^31, B K <= 2^20 (LSS_ERR_SHAPE otherwise).  Outputs lie over no input (LSS_ERR_RANGE).
+ */
+size_t lss_beam_select_workspace_bytes(int64_t B, int64_t K, int64_t V, int64_t n_out);
+int lss_beam_select(const void *logits, int64_t stride, const float *scores, const uint8_t *finished, int64_t end_token,
+                    int64_t B, int64_t K, int64_t V, int64_t n_out, int elem_bytes, void *workspace, size_t workspace_bytes,
+                    float *scores_out, int32_t *parents, int32_t *tokens, uint8_t *finished_out, void *stream);
 
 #ifdef __cplusplus
 }

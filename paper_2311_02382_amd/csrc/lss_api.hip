@@ -829,8 +829,8 @@ static int check_cache(const char *what, int64_t B, int64_t H_kv, int64_t d, int
     return LSS_OK;
 }
 
-int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride, const int32_t *cu_seqlens,
-                     const int32_t *lengths, const int32_t *block_table, int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes,
+int lss_paged_append_ex(const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride, const int32_t *cu_seqlens,
+                     const int32_t *lengths, const int32_t *block_table, const int32_t *positions, int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes,
                      int64_t n_pages, int64_t page_size, int64_t max_pages, const double *inv_freq, int64_t rot_dim, int interleaved, void *k_cache,
                      void *v_cache, void *q_rot, void *k_rot, void *stream)
 {
@@ -849,9 +849,9 @@ int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_s
         return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
     if (misaligned(k) || misaligned(v) || misaligned(q) || misaligned(k_cache) || misaligned(v_cache) || misaligned(q_rot) || misaligned(k_rot))
         return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
-    if (int rc = check_arrays(what, {cu_seqlens, lengths, block_table}, inv_freq)) return rc;
+    if (int rc = check_arrays(what, {cu_seqlens, lengths, block_table, positions}, inv_freq)) return rc;
     const lss::AppendArgs a{pt, cu_seqlens, lengths, inv_freq, k_stride, v_stride, q_stride, (int)rows, (int)B, (int)H, (int)H_kv, (int)d, (int)rot_dim,
-                            interleaved ? 1 : 0, 0, 0};
+                            interleaved ? 1 : 0, 0, 0, positions};
     const auto go = [&](auto zero) {
         typedef decltype(zero) T;
         return lss::launch_paged_append<T>(a, static_cast<const T *>(k), static_cast<const T *>(v), static_cast<const T *>(q), static_cast<T *>(k_cache),
@@ -860,6 +860,15 @@ int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_s
     const hipError_t e = elem_bytes == 2 ? go(lss::bf16_t{}) : go(float{});
     if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));
     return LSS_OK;
+}
+
+int lss_paged_append(const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *q, int64_t q_stride, const int32_t *cu_seqlens,
+                     const int32_t *lengths, const int32_t *block_table, int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes,
+                     int64_t n_pages, int64_t page_size, int64_t max_pages, const double *inv_freq, int64_t rot_dim, int interleaved, void *k_cache,
+                     void *v_cache, void *q_rot, void *k_rot, void *stream)
+{
+    return lss_paged_append_ex(k, k_stride, v, v_stride, q, q_stride, cu_seqlens, lengths, block_table, nullptr, rows, B, H, H_kv, d, elem_bytes, n_pages,
+                               page_size, max_pages, inv_freq, rot_dim, interleaved, k_cache, v_cache, q_rot, k_rot, stream);
 }
 
 // `out` [rows, heads, d] is written while other workgroups still read q
@@ -961,6 +970,159 @@ int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t 
         typedef decltype(zero) T;
         return lss::launch_packed<T>(a, static_cast<const T *>(q), static_cast<const T *>(k), static_cast<const T *>(v), static_cast<T *>(out), lse,
                                      static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
+    };
+    const hipError_t e = elem_bytes == 2 ? go(lss::bf16_t{}) : go(float{});
+    if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));
+    return LSS_OK;
+}
+
+// ---- several continuations of a sequence
+// [a, a + a_bytes) and [b, b + b_bytes) have a byte in common
+static bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && x < y + b_bytes && y < x + a_bytes;
+}
+
+size_t lss_paged_attn_tree_workspace_bytes(int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int64_t max_len, int elem_bytes)
+{
+    if (rows < 1 || B < 1 || B > (int64_t)1 << 24 || H < 1 || H > 65535 || H_kv < 1 || H % H_kv != 0 || (d != 64 && d != 128) || max_len < 0 || max_len > (int64_t)1 << 30 ||
+        (elem_bytes != 2 && elem_bytes != 4) || rows > (int64_t)1 << 24 || rows * H > (int64_t)1 << 24)
+        return 0;
+    return lss::paged_tree_workspace_bytes(rows, (int)B, (int)H, (int)H_kv, (int)d, (int)max_len, elem_bytes);
+}
+
+int lss_paged_attn_tree(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache, const int32_t *lengths, const int32_t *block_table,
+                        const int32_t *cu_q, const int64_t *tree, int64_t words, int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int elem_bytes,
+                        int64_t n_pages, int64_t page_size, int64_t max_pages, int64_t max_len, void *workspace, size_t workspace_bytes, void *out, float *lse,
+                        void *stream)
+{
+    const char *what = "paged_attn_tree";
+    lss::PageTable pt;
+    if (int rc = check_heads(what, H, H_kv, d, elem_bytes)) return rc;
+    if (int rc = check_groups(what, H, H_kv)) return rc;
+    if (int rc = check_cache(what, B, H_kv, d, n_pages, page_size, max_pages, block_table, &pt)) return rc;
+    if (int rc = check_rows(what, "q", rows, q_stride, H, d, elem_bytes)) return rc;
+    if (max_len < 0 || max_len > max_pages * page_size)
+        return fail(LSS_ERR_RANGE, "%s: max_len = %lld, the tables hold %lld tokens", what, (long long)max_len, (long long)(max_pages * page_size));
+    if (rows * H > (int64_t)1 << 24) return fail(LSS_ERR_SHAPE, "%s: rows*H = %lld exceeds 2^24", what, (long long)(rows * H));
+    if (tree && (words < 1 || words > 1024)) return fail(LSS_ERR_SHAPE, "%s: %lld words of tree a row (1 .. 1024)", what, (long long)words);
+    if (rows == 0 || B == 0) return LSS_OK;
+    if (!q || !k_cache || !v_cache || !lengths || !block_table || !cu_q || !out || !lse) return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
+    if (misaligned(q) || misaligned(k_cache) || misaligned(v_cache) || misaligned(out))
+        return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
+    if (misaligned(workspace)) return fail(LSS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", what);
+    if (off_by(tree, 8)) return fail(LSS_ERR_ALIGN, "%s: tree must be 8-byte aligned", what);
+    if (int rc = check_arrays(what, {lengths, block_table, cu_q, lse})) return rc;
+    if (int rc = get_scratch(what, lss::paged_tree_workspace_bytes(rows, (int)B, (int)H, (int)H_kv, (int)d, (int)max_len, elem_bytes), &workspace, workspace_bytes)) return rc;
+    if (int rc = check_apart(what, q, q_stride, out, rows, H, d, elem_bytes)) return rc;
+    const lss::TreeArgs a{pt, lengths, cu_q, reinterpret_cast<const uint64_t *>(tree), q_stride, (int)rows, tree ? (int)words : 0, (int)B, (int)H, (int)H_kv, (int)d, (int)max_len};
+    const auto go = [&](auto zero) {
+        typedef decltype(zero) T;
+        return lss::launch_paged_tree<T>(a, static_cast<const T *>(q), static_cast<const T *>(k_cache), static_cast<const T *>(v_cache), static_cast<T *>(out), lse,
+                                         static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
+    };
+    const hipError_t e = elem_bytes == 2 ? go(lss::bf16_t{}) : go(float{});
+    if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));
+    return LSS_OK;
+}
+
+size_t lss_paged_fork_workspace_bytes(int64_t n_pages, int64_t B_out)
+{
+    if (n_pages < 1 || n_pages > INT32_MAX || B_out < 0 || B_out > (int64_t)1 << 20) return 0;
+    return lss::paged_fork_workspace_bytes(n_pages, B_out);
+}
+
+int lss_paged_fork(const int32_t *lengths, const int32_t *block_table, const int32_t *parents, const int32_t *room, const int32_t *held, int64_t B, int64_t B_out,
+                   int64_t H_kv, int64_t d, int elem_bytes, int64_t n_pages, int64_t page_size, int64_t max_pages, void *workspace, size_t workspace_bytes, void *k_cache,
+                   void *v_cache, int32_t *table_out, int32_t *lengths_out, int32_t *missing, void *stream)
+{
+    const char *what = "paged_fork";
+    lss::PageTable pt;
+    if (int rc = check_heads(what, 1, H_kv, d, elem_bytes)) return rc;
+    if (int rc = check_cache(what, B, H_kv, d, n_pages, page_size, max_pages, block_table, &pt)) return rc;
+    if (B > (int64_t)1 << 20 || B_out < 0 || B_out > (int64_t)1 << 20)
+        return fail(LSS_ERR_SHAPE, "%s: %lld sequences from %lld (0 .. 2^20)", what, (long long)B_out, (long long)B);
+    if (!k_cache || !v_cache || !missing || (B > 0 && (!lengths || !block_table)) || (B_out > 0 && (!parents || !table_out || !lengths_out)))
+        return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
+    if (misaligned(k_cache) || misaligned(v_cache)) return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
+    if (misaligned(workspace)) return fail(LSS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", what);
+    if (int rc = check_arrays(what, {lengths, block_table, parents, room, held, table_out, lengths_out, missing})) return rc;
+    // what is written while other workgroups still read
+    const struct { const void *p; int64_t n; } in[] = {{lengths, B}, {block_table, B * max_pages}, {parents, B_out}, {room, B_out}, {held, n_pages}},
+                                               written[] = {{table_out, B_out * max_pages}, {lengths_out, B_out}, {missing, 1}};
+    for (const auto &w : written)
+        for (const auto &r : in)
+            if (overlap(w.p, (size_t)w.n * 4, r.p, (size_t)r.n * 4)) return fail(LSS_ERR_RANGE, "%s: an output lies over an input", what);
+    if (int rc = get_scratch(what, lss::paged_fork_workspace_bytes(n_pages, B_out), &workspace, workspace_bytes)) return rc;
+    const lss::ForkArgs a{pt, lengths, parents, room, held, (int)B, (int)B_out};
+    const hipError_t e = lss::launch_paged_fork(a, (int)(H_kv * d * elem_bytes), k_cache, v_cache, static_cast<int32_t *>(workspace), table_out, lengths_out, missing,
+                                                static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));
+    return LSS_OK;
+}
+
+int lss_paged_compact(const int32_t *lengths, const int32_t *block_table, const int32_t *cu_q, const int32_t *kept, const int32_t *n_kept, int64_t max_kept, int64_t B,
+                      int64_t H_kv, int64_t d, int elem_bytes, int64_t n_pages, int64_t page_size, int64_t max_pages, void *k_cache, void *v_cache, int32_t *lengths_out,
+                      void *stream)
+{
+    const char *what = "paged_compact";
+    lss::PageTable pt;
+    if (int rc = check_heads(what, 1, H_kv, d, elem_bytes)) return rc;
+    if (int rc = check_cache(what, B, H_kv, d, n_pages, page_size, max_pages, block_table, &pt)) return rc;
+    if (B > (int64_t)1 << 18) return fail(LSS_ERR_SHAPE, "%s: B = %lld exceeds 2^18", what, (long long)B);
+    if (max_kept < 0 || max_kept > (int64_t)1 << 24) return fail(LSS_ERR_SHAPE, "%s: lists of %lld (0 .. 2^24)", what, (long long)max_kept);
+    if (B == 0) return LSS_OK;
+    if (!k_cache || !v_cache || !lengths || !block_table || !cu_q || (max_kept > 0 && !kept) || !n_kept || !lengths_out) return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
+    if (misaligned(k_cache) || misaligned(v_cache)) return fail(LSS_ERR_ALIGN, "%s: tensor pointers must be 16-byte aligned", what);
+    if (int rc = check_arrays(what, {lengths, block_table, cu_q, kept, n_kept, lengths_out})) return rc;
+    const struct { const void *p; int64_t n; } in[] = {{lengths, B}, {block_table, B * max_pages}, {cu_q, B + 1}, {kept, B * max_kept}, {n_kept, B}};
+    for (const auto &r : in)
+        if (overlap(lengths_out, (size_t)B * 4, r.p, (size_t)r.n * 4)) return fail(LSS_ERR_RANGE, "%s: lengths_out lies over an input", what);
+    const lss::CompactArgs a{pt, lengths, cu_q, kept, n_kept, (int)B, (int)max_kept};
+    const hipError_t e = lss::launch_paged_compact(a, (int)(H_kv * d * elem_bytes), k_cache, v_cache, lengths_out, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));
+    return LSS_OK;
+}
+
+static bool beam_sizes_ok(int64_t B, int64_t K, int64_t V, int64_t N)
+{
+    return B >= 0 && K >= 1 && K <= 64 && V >= 1 && V <= INT32_MAX / K && N >= 1 && N <= 64 && B <= ((int64_t)1 << 20) / K;
+}
+
+size_t lss_beam_select_workspace_bytes(int64_t B, int64_t K, int64_t V, int64_t N)
+{
+    return B >= 1 && beam_sizes_ok(B, K, V, N) ? lss::beam_select_workspace_bytes((int)B, (int)K, (int)V, (int)N) : 0;
+}
+
+int lss_beam_select(const void *logits, int64_t stride, const float *scores, const uint8_t *finished, int64_t end_token, int64_t B, int64_t K, int64_t V, int64_t N,
+                    int elem_bytes, void *workspace, size_t workspace_bytes, float *scores_out, int32_t *parents, int32_t *tokens, uint8_t *finished_out, void *stream)
+{
+    const char *what = "beam_select";
+    if (elem_bytes != 2 && elem_bytes != 4) return fail(LSS_ERR_SHAPE, "%s: elem_bytes = %d: 2 (bf16) or 4 (float)", what, elem_bytes);
+    if (!beam_sizes_ok(B, K, V, N))
+        return fail(LSS_ERR_SHAPE, "%s: %lld prompts of %lld beams over %lld tokens, %lld chosen (1 .. 64 beams and chosen ones, K*V below 2^31, B*K up to 2^20)", what, (long long)B,
+                    (long long)K, (long long)V, (long long)N);
+    if (stride < V || stride > (int64_t)1 << 32) return fail(LSS_ERR_SHAPE, "%s: rows of logits are %lld elements apart (at least %lld, at most 2^32)", what, (long long)stride, (long long)V);
+    if (end_token < -1 || end_token >= V || (end_token < 0 && (finished || finished_out)))
+        return fail(LSS_ERR_RANGE, "%s: end_token = %lld, of %lld tokens (-1: none, and no beam has ended)", what, (long long)end_token, (long long)V);
+    if (B == 0) return LSS_OK;
+    if (!logits || !scores || !scores_out || !parents || !tokens) return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);
+    if (off_by(logits, (size_t)elem_bytes)) return fail(LSS_ERR_ALIGN, "%s: logits must be aligned to their elements", what);
+    if (misaligned(workspace)) return fail(LSS_ERR_ALIGN, "%s: workspace must be 16-byte aligned", what);
+    for (const void *p : {(const void *)scores, (const void *)scores_out, (const void *)parents, (const void *)tokens})
+        if (off_by(p, 4)) return fail(LSS_ERR_ALIGN, "%s: scores, parents and tokens must be 4-byte aligned", what);
+    const struct { const void *p; size_t n; } in[] = {{logits, ((size_t)(B * K - 1) * stride + V) * elem_bytes}, {scores, (size_t)(B * K) * 4}, {finished, (size_t)(B * K)}},
+                                              written[] = {{scores_out, (size_t)(B * N) * 4}, {parents, (size_t)(B * N) * 4}, {tokens, (size_t)(B * N) * 4},
+                                                           {finished_out, (size_t)(B * N)}};
+    for (const auto &w : written)
+        for (const auto &r : in)
+            if (overlap(w.p, w.n, r.p, r.n)) return fail(LSS_ERR_RANGE, "%s: an output lies over an input", what);
+    if (int rc = get_scratch(what, lss::beam_select_workspace_bytes((int)B, (int)K, (int)V, (int)N), &workspace, workspace_bytes)) return rc;
+    const auto go = [&](auto zero) {
+        typedef decltype(zero) T;
+        return lss::launch_beam_select<T>(static_cast<const T *>(logits), stride, scores, finished, (int)end_token, (int)B, (int)K, (int)V, (int)N, workspace, scores_out, parents,
+                                          tokens, finished_out, static_cast<hipStream_t>(stream));
     };
     const hipError_t e = elem_bytes == 2 ? go(lss::bf16_t{}) : go(float{});
     if (e != hipSuccess) return fail(LSS_ERR_LAUNCH, "%s launch failed: %s", what, hipGetErrorString(e));

@@ -111,7 +111,8 @@ hipError_t allow_lds(K kernel, int bytes, DeviceOnce &once)
 enum KernelId { K_FWD_F32 = 0, K_FWD_MERGE, K_ROWDOT, K_BWD_MAIN_F32, K_DQ_MERGE, K_REDUCE, K_BWD_MAIN_BF16, K_PROJ_FWD, K_PROJ_BWD,
                 K_PE_FWD, K_PE_BWD, K_LN_FWD, K_LN_BWD, K_LN_PARAMS, K_GELU_FWD, K_GELU_BWD, K_LINEAR_FWD, K_LINEAR_BWD, K_RESIDUAL, K_LINEAR_WGRAD,
                 K_FWD_BF16, K_BWD_PREP_BF16, K_BWD_SKINNY_BF16, K_LN_BWD_SHORT, K_PROJ_FWD_SMALL, K_PROJ_BWD_SMALL, K_LINEAR_FWD_SMALL,
-                K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_BF16, K_PACKED_F32, K_PACKED_MERGE, K_COUNT };
+                K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_BF16, K_PACKED_F32, K_PACKED_MERGE, K_PAGED_TREE, K_FORK_CLEAR,
+                K_FORK_TABLE, K_FORK_PLAN, K_FORK_COPY, K_PAGED_COMPACT, K_BEAM_ROWS, K_BEAM_SELECT, K_COUNT };
 void timing_begin(int id, hipStream_t st);
 void timing_end(int id, hipStream_t st);
 struct TimedLaunch {    // RAII bracket around one kernel launch
@@ -182,6 +183,7 @@ struct AppendArgs {
     const double *inv_freq;             // [rot / 2] radians per position
     int64_t k_stride, v_stride, q_stride;
     int rows, B, H, H_kv, d, rot, interleaved, rows_per_wg, unit_shift;
+    const int32_t *positions;           // [rows] that the rows are rotated by; null: their places
 };
 template <typename T>
 hipError_t launch_paged_append(const AppendArgs &a, const T *k, const T *v, const T *q, T *k_cache, T *v_cache, T *q_rot, T *k_rot, hipStream_t st);
@@ -194,6 +196,35 @@ struct DecodeArgs {
 size_t paged_decode_workspace_bytes(int H, int H_kv, int d, int max_len);
 template <typename T>
 hipError_t launch_paged_decode(const DecodeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st);
+// several continuations of a sequence (lss_tree.hip, lss_pages.hip, lss_beam.hip)
+struct TreeArgs {
+    PageTable pt;
+    const int32_t *lengths, *cu;        // cu [B + 1]
+    const uint64_t *tree;               // [rows, words] of bits; null: a drafted token sees those in front of it
+    int64_t q_stride;
+    int rows, words, B, H, H_kv, d, max_len;
+};
+size_t paged_tree_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem_bytes);
+template <typename T>
+hipError_t launch_paged_tree(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st);
+struct ForkArgs {
+    PageTable pt;                       // of the B sequences before
+    const int32_t *lengths, *parents, *room, *held;     // [B], [B_out], [B_out] or null, [n_pages] or null
+    int B, B_out;
+};
+size_t paged_fork_workspace_bytes(int64_t n_pages, int64_t B_out);
+hipError_t launch_paged_fork(const ForkArgs &a, int row_bytes, void *k_cache, void *v_cache, int32_t *scratch, int32_t *table_out, int32_t *lengths_out, int32_t *missing,
+                             hipStream_t st);
+struct CompactArgs {
+    PageTable pt;
+    const int32_t *lengths, *cu, *kept, *n_kept;        // [B], [B + 1], [B, max_kept], [B]
+    int B, max_kept;
+};
+hipError_t launch_paged_compact(const CompactArgs &a, int row_bytes, void *k_cache, void *v_cache, int32_t *lengths_out, hipStream_t st);
+size_t beam_select_workspace_bytes(int B, int K, int V, int N);
+template <typename T>
+hipError_t launch_beam_select(const T *logits, int64_t stride, const float *scores, const uint8_t *finished, int end_token, int B, int K, int V, int N, void *workspace,
+                              float *scores_out, int32_t *parents, int32_t *tokens, uint8_t *finished_out, hipStream_t st);
 struct PackedArgs {
     const int32_t *cu_q, *cu_k;         // [B + 1]
     int64_t q_stride, k_stride, v_stride;

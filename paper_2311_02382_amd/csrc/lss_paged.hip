@@ -4,15 +4,13 @@
 // [n_pages, page_size, H_kv, d] each.  A number outside [0, n_pages) is no page: nothing is written there and nobody sees its tokens.
 #include "lss_serve.h"
 
-#include <climits>
-
 namespace lss {
 
 namespace {
 
-constexpr int kAppendThreads = 256, kAppendRows = 2, kAppendUnits = 3;
+constexpr int kAppendThreads = 256, kAppendRows = 2, kAppendUnits = 3, kNoRow = -2;
 
-// ---- append.  Row t of the packed rows has position lengths[b] - (rows of b) + (t - cu[b]).  What bounds it is the bytes it moves, or in a step of single tokens
+// ---- append.  Row t of the packed rows has position lengths[b] - (rows of b) + (t - cu[b]), and is rotated by it or by positions[t].  What bounds it is the bytes it moves, or in a step of single tokens
 // its launch and two loads that wait for one another, length and page number (of rows that are found in the starts, two more), and inv_freq's, which waits for nothing
 // but is issued behind the first barrier.  A workgroup takes two rows (one of few): one wavefront each finds the way from row to cache row; then one thread per angle
 // turns positions into cosines and sines, which serve all heads of a row through LDS; then 32 bytes per thread and unit are rotated and stored.  A thread's first
@@ -29,8 +27,8 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(AppendArgs
 {
     typedef typename Vec16<T>::type Vec;
     constexpr int VEC = 16 / sizeof(T);
-    __shared__ int position[kAppendRows];                         // INT_MIN: no sequence's row, not touched at all
-    __shared__ int64_t target[kAppendRows];                       // cache row, -1: none
+    __shared__ int position[kAppendRows];                         // that the row is rotated by
+    __shared__ int64_t target[kAppendRows];                       // cache row, -1: none; kNoRow: no sequence's row, not touched at all
     __shared__ float turn[2][kAppendRows][64];                    // cosine, sine
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row0 = blockIdx.x * a.rows_per_wg, n_rows = min(a.rows_per_wg, a.rows - row0);
@@ -76,14 +74,14 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(AppendArgs
         const int p = b < 0 ? -1 : a.lengths[b] - (end - t);
         const int64_t at = b < 0 ? -1 : cache_row(a.pt, b, p);
         if (lane == 0) {
-            position[wave] = b < 0 ? INT_MIN : p;
-            target[wave] = at;
+            position[wave] = a.positions && b >= 0 ? a.positions[t] : p;
+            target[wave] = b < 0 ? kNoRow : at;
         }
     }
     __syncthreads();
     for (int i = tid; i < n_rows * half; i += kAppendThreads) {
         const int r = i / half, pair = i - r * half;
-        if (position[r] == INT_MIN) continue;
+        if (target[r] == kNoRow) continue;
         const double turns = (double)position[r] * (a.inv_freq[pair] * 0.15915494309189535);
         float sn, cs;
         sincospif((float)(2.0 * (turns - rint(turns))), &sn, &cs);
@@ -97,7 +95,7 @@ __global__ __launch_bounds__(kAppendThreads) void paged_append_kernel(AppendArgs
             const int item = item0 + i * slots;
             if (item >= n_items) continue;
             const Unit u = unit(item);
-            if (position[u.row] == INT_MIN) continue;
+            if (target[u.row] == kNoRow) continue;
             const float *const cosine = turn[0][u.row], *const sine = turn[1][u.row];
             if constexpr (INTERLEAVED) {
                 const auto rotate = [&](Vec &z, int first) __attribute__((always_inline)) {

@@ -91,7 +91,7 @@ bool shaped(const at::Tensor &t, std::initializer_list<int64_t> s) { return t.si
 void dev(const at::Tensor &t, at::ScalarType dt, const char *what)
 {
     if (!plain(t, dt))
-        throw ValueError(std::string(what) + " must be a contiguous " + (dt == kBf16 ? "torch.bfloat16" : dt == kF32 ? "torch.float32" : "torch.uint8") + " device tensor");
+        throw ValueError(std::string(what) + " must be a contiguous " + (dt == kBf16 ? "torch.bfloat16" : dt == kF32 ? "torch.float32" : dt == at::kInt ? "torch.int32" : dt == at::kBool ? "torch.bool" : "torch.uint8") + " device tensor");
 }
 
 at::Tensor fresh(at::IntArrayRef shape, at::ScalarType dt, const at::Tensor &like)
@@ -544,7 +544,7 @@ Cache cache_of(const at::Tensor &k, const at::Tensor &v, const at::Tensor &table
     require(lengths.size(0) == table.size(0), "lengths and block_table disagree on the number of sequences");
     return {k.size(0), k.size(1), k.size(2), k.size(3), table.size(0), table.size(1), k.scalar_type() == kF32 ? 4 : 2, k.scalar_type()};
 }
-// k v k_cache v_cache block_table lengths cu_seqlens q inv_freq interleaved q_rot k_rot stream
+// k v k_cache v_cache block_table lengths cu_seqlens q inv_freq interleaved q_rot k_rot stream positions
 PyObject *paged_append(PyObject *const *a)
 {
     const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &kc = tensor(a[2]), &vc = tensor(a[3]), &table = tensor(a[4]), &lengths = tensor(a[5]);
@@ -552,7 +552,7 @@ PyObject *paged_append(PyObject *const *a)
     const Rows rk = head_rows(k, "k"), rv = head_rows(v, "v");
     require(k.scalar_type() == m.dt && v.scalar_type() == m.dt && rk.heads == m.H_kv && rk.d == m.d && k.sizes() == v.sizes(),
             "k and v must be [rows, H_kv, d] in the cache's dtype");
-    at::Tensor cu, q, freq, q_rot, k_rot;
+    at::Tensor cu, q, freq, q_rot, k_rot, positions;
     if (none(a[6])) require(rk.rows == m.B, "without cu_seqlens there is one row for every sequence");
     else {
         cu = tensor(a[6]);
@@ -571,10 +571,15 @@ PyObject *paged_append(PyObject *const *a)
         require(freq.dim() == 1 && freq.scalar_type() == at::kDouble && on_gpu(freq), "inv_freq must be a contiguous torch.float64 device tensor of 1 dimension");
     }
     if (!none(a[11])) k_rot = output(a[11], k.sizes(), m.dt, k);
-    on_current_gpu({&k, &v, &kc, &vc, &table, &lengths, &cu, &q, &freq, &q_rot, &k_rot});
+    if (!none(a[13])) {
+        positions = tensor(a[13]);
+        int32_array(positions, 1, "positions");
+        require(positions.size(0) == rk.rows, "positions must have one entry for every row");
+    }
+    on_current_gpu({&k, &v, &kc, &vc, &table, &lengths, &cu, &q, &freq, &q_rot, &k_rot, &positions});
     const auto ints = [](const at::Tensor &t) { return t.defined() ? static_cast<const int32_t *>(t.data_ptr()) : nullptr; };
     const auto any = [](const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
-    invoke(lss_paged_append, ptr(k), rk.stride, ptr(v), rv.stride, any(q), rq.stride, ints(cu), ints(lengths), ints(table), rk.rows, m.B, rq.heads,
+    invoke(lss_paged_append_ex, ptr(k), rk.stride, ptr(v), rv.stride, any(q), rq.stride, ints(cu), ints(lengths), ints(table), ints(positions), rk.rows, m.B, rq.heads,
            m.H_kv, m.d, m.eb, m.n_pages, m.page_size, m.max_pages, freq.defined() ? static_cast<const double *>(freq.data_ptr()) : nullptr,
            freq.defined() ? 2 * freq.size(0) : 0, truth(a[9]), ptr(kc), ptr(vc), any(q_rot), any(k_rot), stream_of(a[12]));
     const auto result = [](PyObject *passed, const at::Tensor &t) -> PyObject * {
@@ -621,6 +626,106 @@ PyObject *packed_attn_fwd(PyObject *const *a)
            ptr(out), fptr(lse), stream_of(a[8]));
     return pack({give(a[6], out), give(a[7], lse)});
 }
+// ------------------------------------------------------------------------------------ several continuations of a sequence
+const int32_t *words_of(const at::Tensor &t) { return t.defined() ? static_cast<const int32_t *>(t.data_ptr()) : nullptr; }
+int32_t *written_words(const at::Tensor &t) { return static_cast<int32_t *>(t.data_ptr()); }
+// q k_cache v_cache block_table lengths cu_q tree max_len out lse stream workspace
+PyObject *paged_attn_tree(PyObject *const *a)
+{
+    const at::Tensor &q = tensor(a[0]), &kc = tensor(a[1]), &vc = tensor(a[2]), &table = tensor(a[3]), &lengths = tensor(a[4]), &cu = tensor(a[5]);
+    const Cache m = cache_of(kc, vc, table, lengths);
+    const Rows rq = head_rows(q, "q");
+    require(q.scalar_type() == m.dt && rq.d == m.d, "q must be [rows, H, d] in the cache's dtype");
+    int32_array(cu, 1, "cu_q");
+    require(cu.size(0) == m.B + 1, "cu_q must have one entry more than there are sequences");
+    at::Tensor tree;
+    if (!none(a[6])) {
+        tree = tensor(a[6]);
+        require(tree.dim() == 2 && tree.scalar_type() == at::kLong && on_gpu(tree) && tree.size(0) == rq.rows && tree.size(1) >= 1,
+                "tree must be a contiguous torch.int64 device tensor [rows, words]");
+    }
+    int64_t max_len;
+    if (!none(a[7])) max_len = integer(a[7]);
+    else if (__builtin_mul_overflow(m.max_pages, m.page_size, &max_len)) max_len = -1;
+    const at::Tensor out = output(a[8], q.sizes(), m.dt, q), lse = output(a[9], {rq.rows, rq.heads}, kF32, q);
+    on_current_gpu({&q, &kc, &vc, &table, &lengths, &cu, &tree, &out, &lse});
+    size_t wn = 0;
+    void *wp = call_scratch(a[11], lss_paged_attn_tree_workspace_bytes(rq.rows, m.B, rq.heads, m.H_kv, m.d, max_len, m.eb), q, wn);
+    invoke(lss_paged_attn_tree, ptr(q), rq.stride, ptr(kc), ptr(vc), words_of(lengths), words_of(table), words_of(cu),
+           tree.defined() ? static_cast<const int64_t *>(tree.data_ptr()) : nullptr, tree.defined() ? tree.size(1) : 0, rq.rows, m.B, rq.heads, m.H_kv, m.d, m.eb,
+           m.n_pages, m.page_size, m.max_pages, max_len, wp, wn, ptr(out), fptr(lse), stream_of(a[10]));
+    return pack({give(a[8], out), give(a[9], lse)});
+}
+// k_cache v_cache block_table lengths parents room held table_out lengths_out missing stream workspace
+PyObject *paged_fork(PyObject *const *a)
+{
+    const at::Tensor &kc = tensor(a[0]), &vc = tensor(a[1]), &table = tensor(a[2]), &lengths = tensor(a[3]), &parents = tensor(a[4]);
+    const Cache m = cache_of(kc, vc, table, lengths);
+    require(parents.scalar_type() == at::kInt && on_gpu(parents), "parents must be a contiguous torch.int32 device tensor");
+    const int64_t S = parents.numel();
+    at::Tensor room, held;
+    if (!none(a[5])) {
+        room = tensor(a[5]);
+        require(room.scalar_type() == at::kInt && on_gpu(room) && room.numel() == S, "room must be a contiguous torch.int32 device tensor, an entry for every parent");
+    }
+    if (!none(a[6])) {
+        held = tensor(a[6]);
+        int32_array(held, 1, "held");
+        require(held.size(0) == m.n_pages, "held must have one entry for every page");
+    }
+    const at::Tensor table_out = output(a[7], {S, m.max_pages}, at::kInt, table), lengths_out = output(a[8], {S}, at::kInt, table), missing = output(a[9], {1}, at::kInt, table);
+    on_current_gpu({&kc, &vc, &table, &lengths, &parents, &room, &held, &table_out, &lengths_out, &missing});
+    size_t wn = 0;
+    void *wp = call_scratch(a[11], lss_paged_fork_workspace_bytes(m.n_pages, S), kc, wn);
+    invoke(lss_paged_fork, words_of(lengths), words_of(table), words_of(parents), words_of(room), words_of(held), m.B, S, m.H_kv, m.d, m.eb, m.n_pages, m.page_size,
+           m.max_pages, wp, wn, ptr(kc), ptr(vc), written_words(table_out), written_words(lengths_out), written_words(missing), stream_of(a[10]));
+    return pack({give(a[7], table_out), give(a[8], lengths_out), give(a[9], missing)});
+}
+// k_cache v_cache block_table lengths cu_q kept n_kept lengths_out stream
+PyObject *paged_compact(PyObject *const *a)
+{
+    const at::Tensor &kc = tensor(a[0]), &vc = tensor(a[1]), &table = tensor(a[2]), &lengths = tensor(a[3]), &cu = tensor(a[4]), &kept = tensor(a[5]), &n_kept = tensor(a[6]);
+    const Cache m = cache_of(kc, vc, table, lengths);
+    int32_array(cu, 1, "cu_q");
+    require(cu.size(0) == m.B + 1, "cu_q must have one entry more than there are sequences");
+    int32_array(kept, 2, "kept");
+    int32_array(n_kept, 1, "n_kept");
+    require(kept.size(0) == m.B && n_kept.size(0) == m.B, "kept and n_kept must have a row for every sequence");
+    const at::Tensor lengths_out = output(a[7], {m.B}, at::kInt, table);
+    on_current_gpu({&kc, &vc, &table, &lengths, &cu, &kept, &n_kept, &lengths_out});
+    invoke(lss_paged_compact, words_of(lengths), words_of(table), words_of(cu), words_of(kept), words_of(n_kept), kept.size(1), m.B, m.H_kv, m.d, m.eb, m.n_pages,
+           m.page_size, m.max_pages, ptr(kc), ptr(vc), written_words(lengths_out), stream_of(a[8]));
+    return give(a[7], lengths_out);
+}
+// logits scores n_out finished end_token scores_out parents tokens finished_out stream workspace
+PyObject *beam_select(PyObject *const *a)
+{
+    const at::Tensor &logits = tensor(a[0]), &scores = tensor(a[1]);
+    require(scores.dim() == 2 && plain(scores, kF32), "scores must be a contiguous torch.float32 device tensor [B, K]");
+    const int64_t B = scores.size(0), K = scores.size(1), N = none(a[2]) ? K : integer(a[2]), end_token = integer(a[4]);
+    require(logits.dim() == 2 && logits.is_cuda() && (logits.scalar_type() == kBf16 || logits.scalar_type() == kF32) && logits.size(0) == B * K &&
+                (logits.size(1) <= 1 || logits.stride(1) == 1),
+            "logits must be a bfloat16 or float32 device tensor [B * K, V], the logits of a row one behind the other");
+    const int64_t V = logits.size(1), stride = logits.size(0) > 1 ? logits.stride(0) : V;
+    require(N >= 0, "n_out is negative");
+    at::Tensor finished, finished_out;
+    if (!none(a[3])) {
+        finished = tensor(a[3]);
+        require(finished.sizes() == scores.sizes() && plain(finished, at::kBool), "finished must be a contiguous torch.bool device tensor [B, K]");
+    }
+    const at::Tensor scores_out = output(a[5], {B, N}, kF32, scores), parents = output(a[6], {B, N}, at::kInt, scores), tokens = output(a[7], {B, N}, at::kInt, scores);
+    if (end_token >= 0 || !none(a[8])) finished_out = output(a[8], {B, N}, at::kBool, scores);
+    on_current_gpu({&logits, &scores, &finished, &scores_out, &parents, &tokens, &finished_out});
+    size_t wn = 0;
+    void *wp = call_scratch(a[10], lss_beam_select_workspace_bytes(B, K, V, N), logits, wn);
+    const auto bytes = [](const at::Tensor &t) { return t.defined() ? static_cast<uint8_t *>(t.data_ptr()) : nullptr; };
+    invoke(lss_beam_select, ptr(logits), stride, static_cast<const float *>(ptr(scores)), static_cast<const uint8_t *>(bytes(finished)), end_token, B, K, V, N,
+           logits.scalar_type() == kF32 ? 4 : 2, wp, wn, fptr(scores_out), written_words(parents), written_words(tokens), bytes(finished_out), stream_of(a[9]));
+    PyObject *ended = Py_None;
+    if (finished_out.defined()) ended = give(a[8], finished_out);
+    else Py_INCREF(ended);
+    return pack({give(a[5], scores_out), give(a[6], parents), give(a[7], tokens), ended});
+}
 PyObject *set_error_type(PyObject *const *p)
 {
     Py_INCREF(p[0]);
@@ -653,8 +758,9 @@ PyMethodDef g_methods[] = {
     LSS_FN(project_bwd, 10), LSS_FN(project_bwd_weight, 10), LSS_FN(embed_pe_fwd, 5), LSS_FN(embed_pe_bwd, 3),
     LSS_FN(residual_dropout_add, 7), LSS_FN(layernorm_fwd, 8), LSS_FN(layernorm_bwd, 10), LSS_FN(linear_fwd, 4),
     LSS_FN(linear_bwd_input, 4), LSS_FN(linear_bwd_weight, 5), LSS_FN(linear_gelu_fwd, 5), LSS_FN(linear_bwd_input_gelu, 5),
-    LSS_FN(gelu_fwd, 3), LSS_FN(gelu_bwd, 4), LSS_FN(paged_append, 13), LSS_FN(paged_attn_decode, 10),
-    LSS_FN(packed_attn_fwd, 10), LSS_FN(set_error_type, 1), {nullptr, nullptr, 0, nullptr}};
+    LSS_FN(gelu_fwd, 3), LSS_FN(gelu_bwd, 4), LSS_FN(paged_append, 14), LSS_FN(paged_attn_decode, 10),
+    LSS_FN(packed_attn_fwd, 10), LSS_FN(paged_attn_tree, 12), LSS_FN(paged_fork, 12), LSS_FN(paged_compact, 9), LSS_FN(beam_select, 11),
+    LSS_FN(set_error_type, 1), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_lss_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace

@@ -33,7 +33,8 @@ EXPORTS = ["lss_version", "lss_last_error", "lss_workspace_bytes", "lss_set_work
            "lss_layernorm_bwd", "lss_linear_fwd", "lss_linear_bwd_input", "lss_linear_bwd_weight_scratch_bytes", "lss_linear_bwd_weight",
            "lss_linear_gelu_fwd",
            "lss_linear_bwd_input_gelu", "lss_gelu_fwd", "lss_gelu_bwd", "lss_paged_append", "lss_paged_attn_workspace_bytes", "lss_paged_attn_decode",
-           "lss_packed_attn_workspace_bytes", "lss_packed_attn_fwd"]
+           "lss_packed_attn_workspace_bytes", "lss_packed_attn_fwd", "lss_paged_append_ex", "lss_paged_attn_tree_workspace_bytes", "lss_paged_attn_tree",
+           "lss_paged_fork_workspace_bytes", "lss_paged_fork", "lss_paged_compact", "lss_beam_select_workspace_bytes", "lss_beam_select"]
 
 LSS_FLAG_SKIP_MASKED_TAIL = 1
 
@@ -116,7 +117,19 @@ def load():
     lib.lss_packed_attn_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i64, i64, ci, ci, vp, sz, vp, vp, vp]
     lib.lss_packed_attn_workspace_bytes.argtypes = [i64, i64, i64, i64, i64, i64, ci]
     lib.lss_packed_attn_workspace_bytes.restype = sz
-    for name in ("lss_paged_append", "lss_paged_attn_decode", "lss_packed_attn_fwd"):
+    lib.lss_paged_append_ex.argtypes = [vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, i64, i64, i64, i64, ci, i64, i64, i64, vp, i64, ci, vp, vp, vp, vp, vp]
+    lib.lss_paged_attn_tree.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, ci, i64, i64, i64, i64, vp, sz, vp, vp, vp]
+    lib.lss_paged_attn_tree_workspace_bytes.argtypes = [i64, i64, i64, i64, i64, i64, ci]
+    lib.lss_paged_attn_tree_workspace_bytes.restype = sz
+    lib.lss_paged_fork.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, i64, i64, i64, vp, sz, vp, vp, vp, vp, vp, vp]
+    lib.lss_paged_fork_workspace_bytes.argtypes = [i64, i64]
+    lib.lss_paged_fork_workspace_bytes.restype = sz
+    lib.lss_paged_compact.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, i64, i64, i64, vp, vp, vp, vp]
+    lib.lss_beam_select.argtypes = [vp, i64, vp, vp, i64, i64, i64, i64, i64, ci, vp, sz, vp, vp, vp, vp, vp]
+    lib.lss_beam_select_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.lss_beam_select_workspace_bytes.restype = sz
+    for name in ("lss_paged_append", "lss_paged_attn_decode", "lss_packed_attn_fwd", "lss_paged_append_ex", "lss_paged_attn_tree", "lss_paged_fork", "lss_paged_compact",
+                 "lss_beam_select"):
         getattr(lib, name).restype = ci
     for name in ("lss_embed_pe_fwd", "lss_embed_pe_bwd", "lss_residual_dropout_add", "lss_layernorm_fwd", "lss_layernorm_bwd", "lss_linear_fwd",
                  "lss_linear_bwd_input", "lss_linear_gelu_fwd", "lss_linear_bwd_input_gelu", "lss_gelu_fwd", "lss_gelu_bwd"):
@@ -306,17 +319,18 @@ def lss_gelu_bwd(u, dg, du=None, stream=None):
 
 
 def lss_paged_append(k, v, k_cache, v_cache, block_table, lengths, cu_seqlens=None, q=None, inv_freq=None, interleaved=False,
-                     q_rot=None, k_rot=None, stream=None):
+                     q_rot=None, k_rot=None, stream=None, positions=None):
     """New tokens into a paged cache, keys (and queries) rotated by their positions on the way.
 
     k, v [rows, H_kv, d]: rows cu_seqlens[b] .. cu_seqlens[b + 1] are the last tokens of sequence b, which has lengths[b] with
     them (without cu_seqlens: row b is the last token of sequence b).  Caches [n_pages, page_size, H_kv, d], block_table
     int32 [B, max_pages].  inv_freq float64 [rot_dim / 2]: radians per position of the pairs (i, i + rot_dim / 2), or with
     `interleaved` (2 i, 2 i + 1), of every head of k and q; None: no rotation.  Rows may lie apart (stride of the first dimension).
+    positions int32 [rows]: what each row is rotated by, where that is not its place (the tokens of a drafted tree: by their depth).
 
     Returns (q_rot, k_rot): the rotated q [rows, H, d] if q was given, and k_rot if it was passed (the keys as they went into the cache), else None.
     """
-    return (_native or _bind()).paged_append(k, v, k_cache, v_cache, block_table, lengths, cu_seqlens, q, inv_freq, interleaved, q_rot, k_rot, stream)
+    return (_native or _bind()).paged_append(k, v, k_cache, v_cache, block_table, lengths, cu_seqlens, q, inv_freq, interleaved, q_rot, k_rot, stream, positions)
 
 
 def lss_paged_attn_workspace_bytes(H, H_kv, d, max_len) -> int:
@@ -344,3 +358,53 @@ def lss_packed_attn_fwd(q, k, v, cu_q, cu_k=None, causal=True, out=None, lse=Non
 
     Returns (out [rows, H, d] in q's dtype, lse [H, rows] float32)."""
     return (_native or _bind()).packed_attn_fwd(q, k, v, cu_q, cu_k, causal, out, lse, stream, workspace)
+
+
+def lss_paged_attn_tree_workspace_bytes(rows, B, H, H_kv, d, max_len, elem_bytes=2) -> int:
+    return int(load().lss_paged_attn_tree_workspace_bytes(*map(int, (rows, B, H, H_kv, d, max_len, elem_bytes))))
+
+
+def lss_paged_attn_tree(q, k_cache, v_cache, block_table, lengths, cu_q, tree=None, max_len=None, out=None, lse=None, stream=None, workspace=None):
+    """Attention of drafted tokens over a paged cache: rows cu_q[b] .. cu_q[b + 1] of q [rows, H, d] are the last n_b of sequence b's lengths[b] tokens.
+
+    Every row sees the tokens in front of the drafted ones, and of those the ones that its bits name: tree int64 [rows, words], bit j % 64 of word j / 64 of a
+    row for drafted token j of its sequence (its own bit too, if it is to see itself).  tree=None: a drafted token sees those up to itself (a chain of them, or
+    the next piece of a long prompt).  max_len, workspace: as for lss_paged_attn_decode, of lss_paged_attn_tree_workspace_bytes() bytes.
+    Returns (out [rows, H, d] in q's dtype, lse [rows, H] float32)."""
+    return (_native or _bind()).paged_attn_tree(q, k_cache, v_cache, block_table, lengths, cu_q, tree, max_len, out, lse, stream, workspace)
+
+
+def lss_paged_fork_workspace_bytes(n_pages, B_out) -> int:
+    return int(load().lss_paged_fork_workspace_bytes(int(n_pages), int(B_out)))
+
+
+def lss_paged_fork(k_cache, v_cache, block_table, lengths, parents, room=None, held=None, table_out=None, lengths_out=None, missing=None, stream=None,
+                   workspace=None):
+    """The sequences of the next step: sequence s takes on the tokens of sequence parents[s] and has room for room[s] more (None: for one; none without a parent).
+
+    block_table int32 [B, max_pages], lengths int32 [B]: the sequences before; parents, room int32, S entries.  Full pages are shared; a partly filled one that
+    more than one sequence writes into, or that somebody else reads, is copied; pages that no sequence of the result names are free, unless held[page] (int32
+    [n_pages]) is not 0.  A parent outside [0, B): a sequence without tokens.
+
+    Returns (table_out [S, max_pages], lengths_out [S]: with the room, missing [1]: pages that there were too few; the old table is as it was)."""
+    return (_native or _bind()).paged_fork(k_cache, v_cache, block_table, lengths, parents, room, held, table_out, lengths_out, missing, stream, workspace)
+
+
+def lss_paged_compact(k_cache, v_cache, block_table, lengths, cu_q, kept, n_kept, lengths_out=None, stream=None):
+    """The drafted tokens that are kept move to the front of them: of sequence b's n_b = cu_q[b + 1] - cu_q[b] last tokens the numbers kept[b, :n_kept[b]]
+    (int32 [B, most], ascending) become the first n_kept[b].  Returns lengths_out int32 [B]: the lengths without those that are not kept."""
+    return (_native or _bind()).paged_compact(k_cache, v_cache, block_table, lengths, cu_q, kept, n_kept, lengths_out, stream)
+
+
+def lss_beam_select_workspace_bytes(B, K, V, n_out) -> int:
+    return int(load().lss_beam_select_workspace_bytes(*map(int, (B, K, V, n_out))))
+
+
+def lss_beam_select(logits, scores, n_out=None, finished=None, end_token=-1, scores_out=None, parents=None, tokens=None, finished_out=None, stream=None,
+                    workspace=None):
+    """Beam search's choice: of the continuations (beam k of prompt b, token v) the n_out (None: K) with the largest scores[b, k] + log softmax(logits[b K + k])[v],
+    best first, of equal ones the lower (k, v).  logits [B * K, V] bfloat16 or float32, scores float32 [B, K].
+
+    finished bool [B, K]: beams that have ended go on with end_token alone, their score as it is.  Returns (scores_out, parents, tokens, finished_out), [B, n_out]
+    each: parents int32, rows of logits, as lss_paged_fork takes them; finished_out None without an end_token.  Where there are too few: -infinity, -1, -1, True."""
+    return (_native or _bind()).beam_select(logits, scores, n_out, finished, end_token, scores_out, parents, tokens, finished_out, stream, workspace)
