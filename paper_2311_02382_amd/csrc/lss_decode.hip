@@ -85,6 +85,11 @@ template <int D> struct Step<bf16_t, D> {
     {
         *reinterpret_cast<Vec *>(tile + DirectTile<D, 64>::chunk_offset(row, chunk)) = v;
     }
+    static __device__ __forceinline__ f32x4 values4(const char *tile, int row, int column)     // four neighbouring columns
+    {
+        const bf16x4 v = *reinterpret_cast<const bf16x4 *>(tile + DirectTile<D, 64>::chunk_offset(row, column / 8) + column % 8 * 2);
+        return f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+    }
     // o[n][db] += V^T P^T, element v of o[n][db]: column 16 db + 4 (l / 16) + v of query l % 16
     template <int NQ>
     static __device__ __forceinline__ void add_values(const char *tile, const f32x4 (&p)[NQ][2], f32x4 (&o)[NQ][D / 16], int lane)
@@ -145,6 +150,7 @@ template <int D> struct Step<float, D> {
     {
         *reinterpret_cast<Vec *>(tile + at(row, 4 * chunk)) = v;
     }
+    static __device__ __forceinline__ f32x4 values4(const char *tile, int row, int column) { return *reinterpret_cast<const f32x4 *>(tile + at(row, column)); }
     template <int NQ>
     static __device__ __forceinline__ void add_values(const char *tile, const f32x4 (&p)[NQ][1], f32x4 (&o)[NQ][D / 16], int lane)
     {
@@ -160,10 +166,26 @@ template <int D> struct Step<float, D> {
     }
 };
 
+template <typename Vec> __device__ __forceinline__ bool all_finite(const Vec &v)
+{
+    bool all = true;
+#pragma unroll
+    for (int e = 0; e < (int)(16 / sizeof(v[0])); ++e) all = all && fabsf((float)v[e]) < INFINITY;
+    return all;
+}
+// v with 0 in the place of the elements that are finite, or of those that are not
+template <typename Vec> __device__ __forceinline__ Vec without(Vec v, bool finite)
+{
+#pragma unroll
+    for (int e = 0; e < (int)(16 / sizeof(v[0])); ++e)
+        if ((fabsf((float)v[e]) < INFINITY) == finite) v[e] = 0.f;
+    return v;
+}
+
 // ---- which rounds a workgroup takes.  Sequence b has R_b = ceil(length / round) of them per virtual head (a head of keys and values and up to 16 NQ
 // query heads), at least one; the virtual heads of a sequence lie one behind the other, then the next sequence's.
-template <int ROUND>
-__device__ __forceinline__ int rounds_of(const DecodeArgs &a, int length) { return (max(1, min(length, a.max_len)) + ROUND - 1) / ROUND; }
+template <int ROUND, typename Args>
+__device__ __forceinline__ int rounds_of(const Args &a, int length) { return (max(1, min(length, a.max_len)) + ROUND - 1) / ROUND; }
 // 64 sequences' rounds by a wavefront, a lane each, and the sums up to each (a round is 64 tokens at least: 64 sequences have fewer than 2^31)
 template <int ROUND> struct Rounds {
     int length, mine, upto;
@@ -175,6 +197,55 @@ template <int ROUND> struct Rounds {
     }
     __device__ __forceinline__ int all() const { return __builtin_amdgcn_readlane(upto, 63); }
 };
+
+// ---- drafted tokens (lss_paged_attn_tree).  Sequence b has n_b G rows per head of keys and values, row r of them query head r % G of its drafted token r / G: tiles
+// of 16 NQ rows take the place of a head's query heads, and a sequence without rows has no rounds.
+__device__ __forceinline__ void rows_of(const TreeArgs &a, int b, int &begin, int &n)
+{
+    begin = max(0, min(a.cu[b], a.rows));
+    n = max(0, min(a.cu[b + 1], a.rows) - begin);
+}
+template <int ROUND, int NQ> struct TreeRounds {
+    int length, begin, n;
+    int64_t mine, upto;         // rounds per head of keys and values; whole: tiles
+    __device__ __forceinline__ TreeRounds(const TreeArgs &a, int b0, int lane, bool whole)
+    {
+        length = begin = n = 0;
+        if (b0 + lane < a.B) {
+            length = a.lengths[b0 + lane];
+            rows_of(a, b0 + lane, begin, n);
+        }
+        const int64_t tiles = ((int64_t)n * (a.H / a.H_kv) + 16 * NQ - 1) / (16 * NQ);
+        mine = whole ? tiles : tiles * rounds_of<ROUND>(a, length);
+        upto = mine;
+#pragma unroll
+        for (int sh = 1; sh < 64; sh *= 2) {
+            const int64_t below = __shfl_up(upto, sh);
+            if (lane >= sh) upto += below;
+        }
+    }
+    __device__ __forceinline__ int64_t all() const { return of(upto, 63); }
+    static __device__ __forceinline__ int64_t of(int64_t x, int lane)
+    {
+        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32);
+    }
+};
+// Which of the 32 keys from drafted number c0 on (below 0: the tokens in front of them) drafted token i of its sequence sees; `bits`: its words
+__device__ __forceinline__ uint32_t keys_seen(const TreeArgs &a, const uint64_t *bits, int i, int c0)
+{
+    if (a.tree == nullptr) {
+        const int last = i - c0;
+        return last < 0 ? 0u : last >= 31 ? ~0u : (2u << last) - 1;
+    }
+    if (c0 <= -32) return ~0u;
+    const int from = max(c0, 0), word = from >> 6, sh = from & 63;
+    uint64_t seen = word < a.words ? bits[word] >> sh : 0;
+    if (sh > 32 && word + 1 < a.words) seen |= bits[word + 1] << (64 - sh);
+    return c0 >= 0 ? (uint32_t)seen : (uint32_t)seen << -c0 | ((1u << -c0) - 1);
+}
+
+// row of out and lse of row r of a sequence that begins with drafted token `begin`
+__device__ __forceinline__ int64_t tree_row(const TreeArgs &a, int begin, int G, int h_kv, int r) { return (int64_t)(begin + r / G) * a.H + h_kv * G + r % G; }
 
 // Scratch memory.  What a part of a sequence leaves there for its query n of `rows`: sum of weight * value [d], maximum (log2 domain) and sum.  A
 // workgroup has room for two parts: 2 w for its first and, if it begins there, 2 w + 1 for its last.  And for the joining launch, the sequences that
@@ -205,8 +276,9 @@ template <typename T, int D> struct Decode {
 };
 
 // Rounds at .. end - 1, the first of which is of sequence b, of `length` tokens, and virtual head v_head; `base`: the first of (b, virtual head 0).  WHOLE: all of (b, v_head).
-template <typename T, int D, int NQ, bool STREAM>
-__device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, float (&sums)[kWaves][2][16], const T *__restrict__ q,
+// Args: DecodeArgs, or TreeArgs where the queries are drafted tokens' and every row sees keys of its own among the last n_b.
+template <typename T, int D, int NQ, bool STREAM, typename Args>
+__device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (&sums)[kWaves][2][16], const T *__restrict__ q,
                                               const T *__restrict__ k_cache, const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,
                                               float *__restrict__ scratch, bool whole, int64_t at, int64_t end, int64_t share, int64_t base, int b, int v_head, int length)
 {
@@ -217,10 +289,17 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
     const int tid = threadIdx.x, lane = tid & 63, lq = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     char *const mine = smem + wave * REGION;
-    const int G = a.H / a.H_kv, groups = (G + 16 * NQ - 1) / (16 * NQ), v_heads = a.H_kv * groups;
+    constexpr bool TREE = std::is_same<Args, TreeArgs>::value;
+    const int G = a.H / a.H_kv;
+    int begin = 0, n_rows = G;                          // drafted tokens: the sequence's first row, and how many (times G)
+    if constexpr (TREE) {
+        rows_of(a, b, begin, n_rows);
+        n_rows *= G;
+    }
+    int groups = (n_rows + 16 * NQ - 1) / (16 * NQ), v_heads = a.H_kv * groups;
     constexpr int PARTS = parts_of(sizeof(T), D, NQ);
-    const Scratch parts{scratch, min(G, 16 * NQ), D, PARTS};
-    const bool by_item = (int64_t)a.B * v_heads <= PARTS;
+    const Scratch parts{scratch, TREE ? 16 * NQ : min(G, 16 * NQ), D, PARTS};
+    const bool by_item = !TREE && (int64_t)a.B * v_heads <= PARTS;
     // (a page is at most 2^29 elements: what lies within 16 rows of one is 32 bits away)
     const int64_t row_bytes = (int64_t)a.H_kv * D * (int)sizeof(T);
     const uint32_t k_lane = (uint32_t)lq * (uint32_t)row_bytes + 16 * g, v_lane = (uint32_t)(lane / S::CHUNKS) * (uint32_t)row_bytes + lane % S::CHUNKS * 16;
@@ -230,12 +309,18 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
         const int R = rounds_of<ROUND>(a, length), n = max(0, min(length, a.max_len));
         const int64_t first = base + (int64_t)v_head * R;           // of this sequence and head
         const int r0 = whole ? 0 : (int)(at - first), r1 = whole ? R : (int)min<int64_t>(R, end - first);
-        const int h_kv = v_head / groups, sub = v_head % groups, n_q = min(16 * NQ, G - sub * 16 * NQ), h0 = h_kv * G + sub * 16 * NQ;
+        const int h_kv = v_head / groups, sub = v_head % groups, n_q = min(16 * NQ, n_rows - sub * 16 * NQ), h0 = h_kv * G + sub * 16 * NQ;
 
         typename S::Queries qf[NQ];
 #pragma unroll
-        for (int i = 0; i < NQ; ++i)
-            S::load_query(qf[i], q + b * a.q_stride + (int64_t)(h0 + min(16 * i + lq, n_q - 1)) * D, g, 16 * i + lq < n_q);
+        for (int i = 0; i < NQ; ++i) {
+            if constexpr (TREE) {
+                const int r = sub * 16 * NQ + min(16 * i + lq, n_q - 1), token = r / G;
+                S::load_query(qf[i], q + (int64_t)(begin + token) * a.q_stride + (int64_t)(h_kv * G + r - token * G) * D, g, 16 * i + lq < n_q);
+            } else {
+                S::load_query(qf[i], q + b * a.q_stride + (int64_t)(h0 + min(16 * i + lq, n_q - 1)) * D, g, 16 * i + lq < n_q);
+            }
+        }
         f32x4 o[NQ][D / 16];
         float m[NQ], l[NQ];
 #pragma unroll
@@ -310,7 +395,7 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
             for (int i = 0; i < S::V_LOADS; ++i) S::store_value(mine, (i * 64 + lane) / S::CHUNKS, lane % S::CHUNKS, values[i]);
         };
         // ... and their weights and sums
-        const auto sums_of = [&]() __attribute__((always_inline)) {
+        const auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
                 float top = -INFINITY;
@@ -338,14 +423,73 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
                         l[i] += p[i][hf][e];
                     }
             }
-            S::template add_values<NQ>(mine, p, o, lane);
         };
         if (j0 < j_end) load(j0);
-        for (; j0 < j_end; j0 += ROUND) {
+        const int first_drafted = TREE ? n - n_rows / G : n;      // its key; tiles that it or a later one is in come last
+        for (; j0 < j_end && (!TREE || j0 + TILE <= first_drafted); j0 += ROUND) {
             scores(j0);
             if (j0 + ROUND < j_end) load(j0 + ROUND);
-            sums_of();
+            weights();
+            S::template add_values<NQ>(mine, p, o, lane);
         }
+        if constexpr (TREE)
+            for (; j0 < j_end; j0 += ROUND) {            // (the next tile's loads wait for this one's end: registers)
+                uint32_t seen[NQ];
+#pragma unroll
+                for (int i = 0; i < NQ; ++i) {
+                    const int token = (sub * 16 * NQ + min(16 * i + lq, n_q - 1)) / G;
+                    seen[i] = keys_seen(a, a.tree + (int64_t)(begin + token) * a.words, token, j0 - first_drafted);
+                }
+                scores(j0);
+                bool finite = true;
+                uint32_t there = 0;                     // keys
+#pragma unroll
+                for (int i = 0; i < S::V_LOADS; ++i) finite = finite && all_finite(values[i]);
+#pragma unroll
+                for (int hf = 0; hf < HALVES; ++hf)
+                    if (ok[hf]) there |= (min(j_end - j0 - 16 * hf, 16) >= 16 ? 0xffffu : (1u << max(j_end - j0 - 16 * hf, 0)) - 1) << 16 * hf;
+#pragma unroll
+                for (int i = 0; i < NQ; ++i)
+#pragma unroll
+                    for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!(seen[i] >> (16 * hf + 4 * g + e) & 1)) p[i][hf][e] = -INFINITY;
+                weights();
+                // 0 times a value that is not finite is NaN: such values are taken out of the tile, and added by themselves where their key is seen, with a weight
+                // that is not 0 then
+                const bool plain = !__any(!finite);
+                const auto values_to_lds = [&](bool finite_out) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int i = 0; i < S::V_LOADS; ++i) S::store_value(mine, (i * 64 + lane) / S::CHUNKS, lane % S::CHUNKS, without(values[i], finite_out));
+                };
+                if (!plain) values_to_lds(false);
+                S::template add_values<NQ>(mine, p, o, lane);
+                if (!plain) values_to_lds(true);
+                const float smallest = 0x1p-126f;
+#pragma unroll 1
+                for (int key = plain ? TILE : 0; key < TILE; ++key) {
+                    if (!(there >> key & 1)) continue;
+#pragma unroll
+                    for (int i = 0; i < NQ; ++i) {
+                        float w = 0.f;
+#pragma unroll
+                        for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (key >> 4 == hf && (key & 3) == e) w = p[i][hf][e];
+                        w = fmaxf(__shfl(w, 16 * (key >> 2 & 3) + lq), smallest);
+                        if (seen[i] >> key & 1)
+#pragma unroll
+                            for (int db = 0; db < D / 16; ++db) {
+                                const f32x4 x = S::values4(mine, key, 16 * db + 4 * g);
+#pragma unroll
+                                for (int v = 0; v < 4; ++v) o[i][db][v] = fmaf(w, x[v], o[i][db][v]);
+                            }
+                    }
+                }
+                if (j0 + ROUND < j_end) load(j0 + ROUND);
+            }
         // the wavefronts' sums meet in LDS, in their order; 16 queries at a time
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
@@ -376,10 +520,12 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
                         r[e] = fmaf(weight[w], *reinterpret_cast<const float *>(smem + w * REGION + (row * ROW_STRIDE + col + e) * 4), r[e]);
                 if (r0 == 0 && r1 == R) {
                     const float inv = total == 0.f ? 0.f : 1.f / total;
-                    T *dst = out + ((int64_t)b * a.H + h0 + nth) * D + col;
+                    int64_t row_out = (int64_t)b * a.H + h0 + nth;
+                    if constexpr (TREE) row_out = tree_row(a, begin, G, h_kv, sub * 16 * NQ + nth);
+                    T *dst = out + row_out * D + col;
 #pragma unroll
                     for (int e = 0; e < D / 16; ++e) dst[e] = (T)(r[e] * inv);
-                    if (col == 0) lse[(int64_t)b * a.H + h0 + nth] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
+                    if (col == 0) lse[row_out] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
                 } else {
                     const int part = 2 * blockIdx.x + (at == start ? 0 : 1);
 #pragma unroll
@@ -398,6 +544,24 @@ __device__ __forceinline__ void decode_rounds(const DecodeArgs &a, char *smem, f
             base += (int64_t)R * v_heads;
             v_head = 0;
             ++b;
+            if constexpr (TREE) {
+                if (at >= end) return;
+                // the next sequence with rows (there is one: rounds are left), 64 at a time
+                for (n_rows = 0; b < a.B; b += 64) {
+                    int some = 0, mine_begin = 0;
+                    if (b + lane < a.B) rows_of(a, b + lane, mine_begin, some);
+                    const uint64_t who = __ballot(some > 0);
+                    if (who == 0) continue;
+                    const int l = __ffsll((long long)who) - 1;
+                    begin = __builtin_amdgcn_readlane(mine_begin, l);
+                    n_rows = __builtin_amdgcn_readlane(some, l) * G;
+                    b += l;
+                    break;
+                }
+                if (n_rows == 0) return;
+                groups = (n_rows + 16 * NQ - 1) / (16 * NQ);
+                v_heads = a.H_kv * groups;
+            }
             if (at < end) length = a.lengths[b];
         }
     }
@@ -452,21 +616,60 @@ __global__ __launch_bounds__(64 * kWaves, parts_of(sizeof(T), D, NQ) / 256) void
     else decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, whole, at, end, share, base, b, v_head, n);
 }
 
+// Drafted tokens: the same rounds; whole: a workgroup per head of keys and values and tile of rows, some of which there are not
+template <typename T, int D, int NQ>
+__global__ __launch_bounds__(64 * kWaves, parts_of(sizeof(T), D, NQ) / 256) void paged_tree_kernel(TreeArgs a, const T *__restrict__ q, const T *__restrict__ k_cache,
+                                                                    const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,
+                                                                    float *__restrict__ scratch, int whole)
+{
+    typedef Decode<T, D> C;
+    typedef TreeRounds<C::ROUND, NQ> Some;
+    constexpr int PARTS = parts_of(sizeof(T), D, NQ);
+    __shared__ __attribute__((aligned(1024))) char smem[kWaves * C::REGION];
+    __shared__ float sums[kWaves][2][16];
+    const int lane = threadIdx.x & 63;
+    Some group(a, 0, lane, whole);
+    int64_t rounds = group.all();
+    for (int b0 = 64; b0 < a.B; b0 += 64) rounds += Some(a, b0, lane, whole).all();
+    const int64_t all = rounds * a.H_kv, share = whole ? 1 : (all + PARTS - 1) / PARTS, at = blockIdx.x * share, end = min(at + share, all);
+    if (!whole && threadIdx.x == 0) Scratch{scratch, 0, D, PARTS}.chain(blockIdx.x)->b = -1;
+    if (at >= end) return;
+    const int64_t nth = divide(at, a.H_kv);
+    int64_t before = 0;
+    int b0 = 0;
+    while (before + group.all() <= nth) {
+        before += group.all();
+        b0 += 64;
+        group = Some(a, b0, lane, whole);
+    }
+    const int l = __ffsll((long long)__ballot(before + group.upto > nth)) - 1, length = __builtin_amdgcn_readlane(group.length, l);
+    const int64_t base = (before + Some::of(group.upto - group.mine, l)) * a.H_kv;
+    const int v_head = (int)divide(at - base, whole ? 1 : rounds_of<C::ROUND>(a, length));
+    decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, whole, at, end, share, base, b0 + l, v_head, length);
+}
+
 // Joins the parts of the sequences that more than one workgroup had rounds of, in their order: workgroup x those of chain x, queries y, y + gridDim.y ..
 // Thread: four columns of every (THREADS / (D / 4))th part.
-template <typename T, int D, int THREADS>
-__global__ __launch_bounds__(THREADS) void decode_merge_kernel(DecodeArgs a, const float *__restrict__ scratch, int nq, int n_parts, T *__restrict__ out,
+template <typename T, int D, int THREADS, typename Args>
+__global__ __launch_bounds__(THREADS) void decode_merge_kernel(Args a, const float *__restrict__ scratch, int nq, int n_parts, T *__restrict__ out,
                                                                float *__restrict__ lse)
 {
     constexpr int LANES = D / 4, GROUPS = THREADS / LANES;
     __shared__ f32x4 acc[GROUPS][LANES];
     __shared__ float totals[GROUPS];
     const int tid = threadIdx.x, lane = tid & 63;
-    const int G = a.H / a.H_kv, groups = (G + 16 * nq - 1) / (16 * nq);
-    const Scratch parts{const_cast<float *>(scratch), min(G, 16 * nq), D, n_parts};
+    constexpr bool TREE = std::is_same<Args, TreeArgs>::value;
+    const int G = a.H / a.H_kv;
+    const Scratch parts{const_cast<float *>(scratch), TREE ? 16 * nq : min(G, 16 * nq), D, n_parts};
     const Chain chain = *parts.chain(blockIdx.x);
     if (chain.b < 0) return;
-    const int sub = chain.v_head % groups, n_q = min(16 * nq, G - sub * 16 * nq), h0 = chain.v_head / groups * G + sub * 16 * nq;
+    int begin = 0, n_rows = G;
+    if constexpr (TREE) {
+        rows_of(a, chain.b, begin, n_rows);
+        n_rows *= G;
+    }
+    const int groups = (n_rows + 16 * nq - 1) / (16 * nq);
+    const int sub = chain.v_head % groups, n_q = min(16 * nq, n_rows - sub * 16 * nq), h0 = chain.v_head / groups * G + sub * 16 * nq;
     const auto part_of = [&](int i) { return i == 0 ? chain.w : (chain.w & ~1) + 2 * i; };
     const int grp = tid / LANES, col = tid % LANES * 4;
     for (int n = blockIdx.y; n < n_q; n += gridDim.y) {
@@ -496,7 +699,8 @@ __global__ __launch_bounds__(THREADS) void decode_merge_kernel(DecodeArgs a, con
         if (tid % LANES == 0) totals[grp] = total;
         __syncthreads();
         if (tid < D) {
-            const int64_t row = (int64_t)chain.b * a.H + h0 + n;
+            int64_t row = (int64_t)chain.b * a.H + h0 + n;
+            if constexpr (TREE) row = tree_row(a, begin, G, chain.v_head / groups, sub * 16 * nq + n);
             float value = 0.f;
             total = 0.f;
 #pragma unroll
@@ -509,6 +713,25 @@ __global__ __launch_bounds__(THREADS) void decode_merge_kernel(DecodeArgs a, con
         }
         __syncthreads();
     }
+}
+
+template <typename T, int D, int NQ>
+hipError_t launch_tree(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st)
+{
+    const int G = a.H / a.H_kv;
+    const bool whole = a.max_len <= kWholeLen;
+    constexpr int parts = parts_of(sizeof(T), D, NQ);
+    {
+        // (every sequence's last tile may be partly filled)
+        const int64_t tiles = (int64_t)a.rows * G / (16 * NQ) + std::min(a.rows, a.B);
+        TimedLaunch tl(K_PAGED_TREE, st);
+        hipLaunchKernelGGL((paged_tree_kernel<T, D, NQ>), dim3((unsigned)(whole ? tiles * a.H_kv : parts)), dim3(64 * kWaves), 0, st, a, q, k_cache, v_cache, out, lse,
+                           scratch, whole ? 1 : 0);
+    }
+    if (whole) return hipGetLastError();
+    TimedLaunch tl(K_DECODE_MERGE, st);
+    hipLaunchKernelGGL((decode_merge_kernel<T, D, 256, TreeArgs>), dim3((unsigned)parts, 8u), dim3(256), 0, st, a, scratch, NQ, parts, out, lse);
+    return hipGetLastError();
 }
 
 int queries_per_wave(int H, int H_kv) { return H / H_kv > 16 ? 2 : 1; }       // in sixteens
@@ -528,8 +751,8 @@ hipError_t launch(const DecodeArgs &a, const T *q, const T *k_cache, const T *v_
     // (few chains may be long: more threads each)
     const int chains = (int)std::min<int64_t>((int64_t)a.B * v_heads, parts), y = std::min(G, 8);
     TimedLaunch tl(K_DECODE_MERGE, st);
-    if (chains * y <= 256) hipLaunchKernelGGL((decode_merge_kernel<T, D, 1024>), dim3((unsigned)chains, (unsigned)y), dim3(1024), 0, st, a, scratch, NQ, parts, out, lse);
-    else hipLaunchKernelGGL((decode_merge_kernel<T, D, 256>), dim3((unsigned)chains, (unsigned)y), dim3(256), 0, st, a, scratch, NQ, parts, out, lse);
+    if (chains * y <= 256) hipLaunchKernelGGL((decode_merge_kernel<T, D, 1024, DecodeArgs>), dim3((unsigned)chains, (unsigned)y), dim3(1024), 0, st, a, scratch, NQ, parts, out, lse);
+    else hipLaunchKernelGGL((decode_merge_kernel<T, D, 256, DecodeArgs>), dim3((unsigned)chains, (unsigned)y), dim3(256), 0, st, a, scratch, NQ, parts, out, lse);
     return hipGetLastError();
 }
 
@@ -549,6 +772,27 @@ hipError_t launch_paged_decode(const DecodeArgs &a, const T *q, const T *k_cache
     if (a.d == 64) return two ? launch<T, 64, 2>(a, q, k_cache, v_cache, out, lse, scratch, st) : launch<T, 64, 1>(a, q, k_cache, v_cache, out, lse, scratch, st);
     return two ? launch<T, 128, 2>(a, q, k_cache, v_cache, out, lse, scratch, st) : launch<T, 128, 1>(a, q, k_cache, v_cache, out, lse, scratch, st);
 }
+
+// Rows of an average sequence per head of keys and values decide how many a wavefront takes, in sixteens
+static int tree_rows_per_wave(int64_t rows, int B, int H, int H_kv) { return rows * (H / H_kv) > (int64_t)16 * B ? 2 : 1; }
+
+size_t tree_narrow_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len)
+{
+    if (max_len <= kWholeLen) return 0;
+    const int nq = tree_rows_per_wave(rows, B, H, H_kv);
+    return scratch_bytes(16 * nq, d, parts_of(2, d, nq));
+}
+
+template <typename T>
+hipError_t launch_tree_narrow(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st)
+{
+    const bool two = tree_rows_per_wave(a.rows, a.B, a.H, a.H_kv) == 2;
+    if (a.d == 64) return two ? launch_tree<T, 64, 2>(a, q, k_cache, v_cache, out, lse, scratch, st) : launch_tree<T, 64, 1>(a, q, k_cache, v_cache, out, lse, scratch, st);
+    return two ? launch_tree<T, 128, 2>(a, q, k_cache, v_cache, out, lse, scratch, st) : launch_tree<T, 128, 1>(a, q, k_cache, v_cache, out, lse, scratch, st);
+}
+
+template hipError_t launch_tree_narrow<bf16_t>(const TreeArgs &, const bf16_t *, const bf16_t *, const bf16_t *, bf16_t *, float *, float *, hipStream_t);
+template hipError_t launch_tree_narrow<float>(const TreeArgs &, const float *, const float *, const float *, float *, float *, float *, hipStream_t);
 
 template hipError_t launch_paged_decode<bf16_t>(const DecodeArgs &, const bf16_t *, const bf16_t *, const bf16_t *, bf16_t *, float *, float *, hipStream_t);
 template hipError_t launch_paged_decode<float>(const DecodeArgs &, const float *, const float *, const float *, float *, float *, float *, hipStream_t);

@@ -207,6 +207,10 @@ struct TreeArgs {
 size_t paged_tree_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem_bytes);
 template <typename T>
 hipError_t launch_paged_tree(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st);
+// ... by the kernel of the attention of one token (lss_decode.hip)
+size_t tree_narrow_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len);
+template <typename T>
+hipError_t launch_tree_narrow(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st);
 struct ForkArgs {
     PageTable pt;                       // of the B sequences before
     const int32_t *lengths, *parents, *room, *held;     // [B], [B_out], [B_out] or null, [n_pages] or null
