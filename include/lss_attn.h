@@ -508,7 +508,7 @@ int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t 
  *   workspace  DEVICE buffer of lss_paged_attn_tree_workspace_bytes() bytes, 16-byte aligned; NULL: the one registered with lss_set_workspace().  Calls that
  *              overlap in time on one GPU need a buffer each
  * A row that sees no key gives zeros and lse = -infinity; a key that a row does not see does not reach its result, whatever its value.  Rows of no sequence are
- * not touched.  rows * H <= 2^24, words <= 1024 (LSS_ERR_SHAPE otherwise).
+ * not touched.  rows * H <= 2^24, B * H_kv <= 2^22, words <= 1024 (LSS_ERR_SHAPE otherwise).
  */
 size_t lss_paged_attn_tree_workspace_bytes(int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int64_t max_len, int elem_bytes);
 int lss_paged_attn_tree(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,

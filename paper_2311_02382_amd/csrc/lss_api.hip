@@ -987,7 +987,7 @@ static bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes
 size_t lss_paged_attn_tree_workspace_bytes(int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int64_t max_len, int elem_bytes)
 {
     if (rows < 1 || B < 1 || B > (int64_t)1 << 24 || H < 1 || H > 65535 || H_kv < 1 || H % H_kv != 0 || (d != 64 && d != 128) || max_len < 0 || max_len > (int64_t)1 << 30 ||
-        (elem_bytes != 2 && elem_bytes != 4) || rows > (int64_t)1 << 24 || rows * H > (int64_t)1 << 24)
+        (elem_bytes != 2 && elem_bytes != 4) || rows > (int64_t)1 << 24 || rows * H > (int64_t)1 << 24 || B * H_kv > (int64_t)1 << 22)
         return 0;
     return lss::paged_tree_workspace_bytes(rows, (int)B, (int)H, (int)H_kv, (int)d, (int)max_len, elem_bytes);
 }
@@ -1005,7 +1005,8 @@ int lss_paged_attn_tree(const void *q, int64_t q_stride, const void *k_cache, co
     if (int rc = check_rows(what, "q", rows, q_stride, H, d, elem_bytes)) return rc;
     if (max_len < 0 || max_len > max_pages * page_size)
         return fail(LSS_ERR_RANGE, "%s: max_len = %lld, the tables hold %lld tokens", what, (long long)max_len, (long long)(max_pages * page_size));
-    if (rows * H > (int64_t)1 << 24) return fail(LSS_ERR_SHAPE, "%s: rows*H = %lld exceeds 2^24", what, (long long)(rows * H));
+    if (rows * H > (int64_t)1 << 24 || B * H_kv > (int64_t)1 << 22)      // (a launch has fewer than 2^32 threads)
+        return fail(LSS_ERR_SHAPE, "%s: %lld rows of %lld heads in %lld sequences are too many", what, (long long)rows, (long long)H, (long long)B);
     if (tree && (words < 1 || words > 1024)) return fail(LSS_ERR_SHAPE, "%s: %lld words of tree a row (1 .. 1024)", what, (long long)words);
     if (rows == 0 || B == 0) return LSS_OK;
     if (!q || !k_cache || !v_cache || !lengths || !block_table || !cu_q || !out || !lse) return fail(LSS_ERR_NULL, "%s: NULL tensor pointer", what);

@@ -157,6 +157,35 @@ struct DirectTile {
                              : "memory", "m0");
         }
     }
+    // The same from pages: a wavefront's rows of either tile come from one 16-row part of a page, a buffer that begins with the part's first row and ends with the last one
+    // that is to be seen: lanes past it load zeros, and so do all where there is no page (an empty buffer).  `off`: page_offsets().  The buffers' words may have come out of
+    // vector registers (page numbers do): five wait states ahead of the first load.
+    static __device__ __forceinline__ void page_offsets(uint32_t (&off)[NI], uint32_t row_bytes, int wave, int lane)
+    {
+        static_assert(NI * RPI <= 16 && 16 % (NI * RPI) == 0, "a wavefront's rows are of one part");
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+            const int row = (wave * NI + i) * RPI + lane / CPR, chunk = (lane % CPR) ^ tile_swizzle<D>(row);
+            // (the instruction's own offset is taken off again: row RPI i begins 1024 i bytes from the part's first at least)
+            off[i] = (uint32_t)(row % 16) * row_bytes + (uint32_t)chunk * 16u - (uint32_t)i * 1024u;
+        }
+    }
+    static __device__ __forceinline__ void issue_pages(const u32x4 &k_uniform, const u32x4 &v_uniform, const uint32_t (&off)[NI], char *lds_tile, int wave)
+    {
+        static_assert(NI == 2 || NI == 4, "");
+        const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)(lds_tile + wave * (NI * 1024));
+        const uint32_t lds1 = lds0 + BYTES;
+        if constexpr (NI == 2)
+            asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %4, 0 offen lds\n\tbuffer_load_dwordx4 %3, %4, 0 offen offset:1024 lds\n\t"
+                         "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, 0 offen lds\n\tbuffer_load_dwordx4 %3, %5, 0 offen offset:1024 lds"
+                         : : "s"(lds0), "s"(lds1), "v"(off[0]), "v"(off[1]), "s"(k_uniform), "s"(v_uniform) : "memory", "m0");
+        else
+            asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %6, 0 offen lds\n\tbuffer_load_dwordx4 %3, %6, 0 offen offset:1024 lds\n\t"
+                         "buffer_load_dwordx4 %4, %6, 0 offen offset:2048 lds\n\tbuffer_load_dwordx4 %5, %6, 0 offen offset:3072 lds\n\t"
+                         "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %7, 0 offen lds\n\tbuffer_load_dwordx4 %3, %7, 0 offen offset:1024 lds\n\t"
+                         "buffer_load_dwordx4 %4, %7, 0 offen offset:2048 lds\n\tbuffer_load_dwordx4 %5, %7, 0 offen offset:3072 lds"
+                         : : "s"(lds0), "s"(lds1), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(k_uniform), "s"(v_uniform) : "memory", "m0");
+    }
     // byte offset inside the tile of the 16-byte chunk c of row r
     static __device__ __forceinline__ int chunk_offset(int r, int c) { return r * (D * 2) + ((c ^ tile_swizzle<D>(r)) * 16); }
 };

@@ -198,55 +198,6 @@ template <int ROUND> struct Rounds {
     __device__ __forceinline__ int all() const { return __builtin_amdgcn_readlane(upto, 63); }
 };
 
-// ---- drafted tokens (lss_paged_attn_tree).  Sequence b has n_b G rows per head of keys and values, row r of them query head r % G of its drafted token r / G: tiles
-// of 16 NQ rows take the place of a head's query heads, and a sequence without rows has no rounds.
-__device__ __forceinline__ void rows_of(const TreeArgs &a, int b, int &begin, int &n)
-{
-    begin = max(0, min(a.cu[b], a.rows));
-    n = max(0, min(a.cu[b + 1], a.rows) - begin);
-}
-template <int ROUND, int NQ> struct TreeRounds {
-    int length, begin, n;
-    int64_t mine, upto;         // rounds per head of keys and values; whole: tiles
-    __device__ __forceinline__ TreeRounds(const TreeArgs &a, int b0, int lane, bool whole)
-    {
-        length = begin = n = 0;
-        if (b0 + lane < a.B) {
-            length = a.lengths[b0 + lane];
-            rows_of(a, b0 + lane, begin, n);
-        }
-        const int64_t tiles = ((int64_t)n * (a.H / a.H_kv) + 16 * NQ - 1) / (16 * NQ);
-        mine = whole ? tiles : tiles * rounds_of<ROUND>(a, length);
-        upto = mine;
-#pragma unroll
-        for (int sh = 1; sh < 64; sh *= 2) {
-            const int64_t below = __shfl_up(upto, sh);
-            if (lane >= sh) upto += below;
-        }
-    }
-    __device__ __forceinline__ int64_t all() const { return of(upto, 63); }
-    static __device__ __forceinline__ int64_t of(int64_t x, int lane)
-    {
-        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32);
-    }
-};
-// Which of the 32 keys from drafted number c0 on (below 0: the tokens in front of them) drafted token i of its sequence sees; `bits`: its words
-__device__ __forceinline__ uint32_t keys_seen(const TreeArgs &a, const uint64_t *bits, int i, int c0)
-{
-    if (a.tree == nullptr) {
-        const int last = i - c0;
-        return last < 0 ? 0u : last >= 31 ? ~0u : (2u << last) - 1;
-    }
-    if (c0 <= -32) return ~0u;
-    const int from = max(c0, 0), word = from >> 6, sh = from & 63;
-    uint64_t seen = word < a.words ? bits[word] >> sh : 0;
-    if (sh > 32 && word + 1 < a.words) seen |= bits[word + 1] << (64 - sh);
-    return c0 >= 0 ? (uint32_t)seen : (uint32_t)seen << -c0 | ((1u << -c0) - 1);
-}
-
-// row of out and lse of row r of a sequence that begins with drafted token `begin`
-__device__ __forceinline__ int64_t tree_row(const TreeArgs &a, int begin, int G, int h_kv, int r) { return (int64_t)(begin + r / G) * a.H + h_kv * G + r % G; }
-
 // Scratch memory.  What a part of a sequence leaves there for its query n of `rows`: sum of weight * value [d], maximum (log2 domain) and sum.  A
 // workgroup has room for two parts: 2 w for its first and, if it begins there, 2 w + 1 for its last.  And for the joining launch, the sequences that
 // more than one workgroup has: by sequence and virtual head where those are not more than the workgroups, else by the workgroup that one begins in (as
@@ -261,14 +212,10 @@ struct Scratch {
 };
 size_t scratch_bytes(int rows, int d, int parts) { return sizeof(float) * (4 * parts + (size_t)2 * parts * rows * (d + 2)); }
 
-// a / b in 32 bits where both fit (a fifth of the instructions); wavefront-uniform
-__device__ __forceinline__ int64_t divide(int64_t a, int64_t b)
-{
-    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
-}
-
 // workgroups that share the rounds: as many as there is room for at once
 constexpr int parts_of(int elem_bytes, int d, int nq) { return 256 * (d == 64 ? (nq == 1 ? 4 : 3) : nq == 1 || elem_bytes == 2 ? 2 : 1); }
+// (drafted tokens' rows in two sixteens: a workgroup less, or registers would go to scratch memory)
+constexpr int tree_per_cu(int elem_bytes, int d, int nq) { return d == 64 ? (nq == 1 ? 3 : 2) : elem_bytes == 2 && nq == 1 ? 2 : 1; }
 template <typename T, int D> struct Decode {
     static constexpr int ROUND = kWaves * Step<T, D>::TILE, ROW_STRIDE = D + 4;       // (16 bytes more: rows of the joining start in other banks)
     static constexpr int TILE_BYTES = Step<T, D>::TILE * D * (int)sizeof(T), JOIN_BYTES = 16 * ROW_STRIDE * 4;
@@ -276,11 +223,12 @@ template <typename T, int D> struct Decode {
 };
 
 // Rounds at .. end - 1, the first of which is of sequence b, of `length` tokens, and virtual head v_head; `base`: the first of (b, virtual head 0).  WHOLE: all of (b, v_head).
-// Args: DecodeArgs, or TreeArgs where the queries are drafted tokens' and every row sees keys of its own among the last n_b.
+// Args: DecodeArgs, or TreeArgs where the queries are drafted tokens' and every row sees keys of its own among the last n_b: then a part of one tile of rows, `tp`, only.
 template <typename T, int D, int NQ, bool STREAM, typename Args>
 __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (&sums)[kWaves][2][16], const T *__restrict__ q,
                                               const T *__restrict__ k_cache, const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,
-                                              float *__restrict__ scratch, bool whole, int64_t at, int64_t end, int64_t share, int64_t base, int b, int v_head, int length)
+                                              float *__restrict__ scratch, bool whole, int64_t at, int64_t end, int64_t share, int64_t base, int b, int v_head, int length,
+                                              const TreePart &tp = TreePart{}, int slots = 0)
 {
     typedef Decode<T, D> C;
     typedef Step<T, D> S;
@@ -290,16 +238,11 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     char *const mine = smem + wave * REGION;
     constexpr bool TREE = std::is_same<Args, TreeArgs>::value;
-    const int G = a.H / a.H_kv;
-    int begin = 0, n_rows = G;                          // drafted tokens: the sequence's first row, and how many (times G)
-    if constexpr (TREE) {
-        rows_of(a, b, begin, n_rows);
-        n_rows *= G;
-    }
-    int groups = (n_rows + 16 * NQ - 1) / (16 * NQ), v_heads = a.H_kv * groups;
+    const int G = a.H / a.H_kv, n_rows = TREE ? tp.n * G : G, groups = TREE ? tp.tiles : (G + 16 * NQ - 1) / (16 * NQ), v_heads = a.H_kv * groups;
     constexpr int PARTS = parts_of(sizeof(T), D, NQ);
-    const Scratch parts{scratch, TREE ? 16 * NQ : min(G, 16 * NQ), D, PARTS};
-    const bool by_item = !TREE && (int64_t)a.B * v_heads <= PARTS;
+    const Scratch parts{scratch, min(G, 16 * NQ), D, PARTS};
+    const TreeScratch tree_parts{scratch, 16 * NQ, D, slots};
+    const bool by_item = (int64_t)a.B * v_heads <= PARTS;
     // (a page is at most 2^29 elements: what lies within 16 rows of one is 32 bits away)
     const int64_t row_bytes = (int64_t)a.H_kv * D * (int)sizeof(T);
     const uint32_t k_lane = (uint32_t)lq * (uint32_t)row_bytes + 16 * g, v_lane = (uint32_t)(lane / S::CHUNKS) * (uint32_t)row_bytes + lane % S::CHUNKS * 16;
@@ -308,15 +251,15 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
     while (at < end) {
         const int R = rounds_of<ROUND>(a, length), n = max(0, min(length, a.max_len));
         const int64_t first = base + (int64_t)v_head * R;           // of this sequence and head
-        const int r0 = whole ? 0 : (int)(at - first), r1 = whole ? R : (int)min<int64_t>(R, end - first);
-        const int h_kv = v_head / groups, sub = v_head % groups, n_q = min(16 * NQ, n_rows - sub * 16 * NQ), h0 = h_kv * G + sub * 16 * NQ;
+        const int r0 = TREE ? tp.r0 : whole ? 0 : (int)(at - first), r1 = TREE ? tp.r1 : whole ? R : (int)min<int64_t>(R, end - first);
+        const int h_kv = TREE ? tp.h_kv : v_head / groups, sub = TREE ? tp.tile : v_head % groups, n_q = min(16 * NQ, n_rows - sub * 16 * NQ), h0 = h_kv * G + sub * 16 * NQ;
 
         typename S::Queries qf[NQ];
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
             if constexpr (TREE) {
                 const int r = sub * 16 * NQ + min(16 * i + lq, n_q - 1), token = r / G;
-                S::load_query(qf[i], q + (int64_t)(begin + token) * a.q_stride + (int64_t)(h_kv * G + r - token * G) * D, g, 16 * i + lq < n_q);
+                S::load_query(qf[i], q + (int64_t)(tp.begin + token) * a.q_stride + (int64_t)(h_kv * G + r - token * G) * D, g, 16 * i + lq < n_q);
             } else {
                 S::load_query(qf[i], q + b * a.q_stride + (int64_t)(h0 + min(16 * i + lq, n_q - 1)) * D, g, 16 * i + lq < n_q);
             }
@@ -438,7 +381,7 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
 #pragma unroll
                 for (int i = 0; i < NQ; ++i) {
                     const int token = (sub * 16 * NQ + min(16 * i + lq, n_q - 1)) / G;
-                    seen[i] = keys_seen(a, a.tree + (int64_t)(begin + token) * a.words, token, j0 - first_drafted);
+                    seen[i] = keys_seen(a, a.tree + (int64_t)(tp.begin + token) * a.words, token, j0 - first_drafted);
                 }
                 scores(j0);
                 bool finite = true;
@@ -518,14 +461,18 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
 #pragma unroll
                     for (int e = 0; e < D / 16; ++e)
                         r[e] = fmaf(weight[w], *reinterpret_cast<const float *>(smem + w * REGION + (row * ROW_STRIDE + col + e) * 4), r[e]);
-                if (r0 == 0 && r1 == R) {
+                if (TREE ? tp.count == 1 : r0 == 0 && r1 == R) {
                     const float inv = total == 0.f ? 0.f : 1.f / total;
                     int64_t row_out = (int64_t)b * a.H + h0 + nth;
-                    if constexpr (TREE) row_out = tree_row(a, begin, G, h_kv, sub * 16 * NQ + nth);
+                    if constexpr (TREE) row_out = tree_row(a, tp.begin, G, h_kv, sub * 16 * NQ + nth);
                     T *dst = out + row_out * D + col;
 #pragma unroll
                     for (int e = 0; e < D / 16; ++e) dst[e] = (T)(r[e] * inv);
                     if (col == 0) lse[row_out] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
+                } else if constexpr (TREE) {
+#pragma unroll
+                    for (int e = 0; e < D / 16; e += 4) *reinterpret_cast<f32x4 *>(tree_parts.values(tp.slot, nth) + col + e) = f32x4{r[e], r[e + 1], r[e + 2], r[e + 3]};
+                    if (col == 0) { tree_parts.sums(tp.slot, nth)[0] = top; tree_parts.sums(tp.slot, nth)[1] = total; }
                 } else {
                     const int part = 2 * blockIdx.x + (at == start ? 0 : 1);
 #pragma unroll
@@ -535,7 +482,7 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
             }
             __syncthreads();
         }
-        if (whole) return;
+        if (TREE || whole) return;
         if (r0 == 0 && tid == 0 && (by_item || r1 < R))
             *parts.chain(by_item ? b * v_heads + v_head : blockIdx.x) = {r1 < R ? b : -1, v_head, 2 * (int)blockIdx.x + (at == start ? 0 : 1),
                                                                          1 + (int)divide(R - r1 + share - 1, share)};
@@ -544,24 +491,6 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
             base += (int64_t)R * v_heads;
             v_head = 0;
             ++b;
-            if constexpr (TREE) {
-                if (at >= end) return;
-                // the next sequence with rows (there is one: rounds are left), 64 at a time
-                for (n_rows = 0; b < a.B; b += 64) {
-                    int some = 0, mine_begin = 0;
-                    if (b + lane < a.B) rows_of(a, b + lane, mine_begin, some);
-                    const uint64_t who = __ballot(some > 0);
-                    if (who == 0) continue;
-                    const int l = __ffsll((long long)who) - 1;
-                    begin = __builtin_amdgcn_readlane(mine_begin, l);
-                    n_rows = __builtin_amdgcn_readlane(some, l) * G;
-                    b += l;
-                    break;
-                }
-                if (n_rows == 0) return;
-                groups = (n_rows + 16 * NQ - 1) / (16 * NQ);
-                v_heads = a.H_kv * groups;
-            }
             if (at < end) length = a.lengths[b];
         }
     }
@@ -616,60 +545,37 @@ __global__ __launch_bounds__(64 * kWaves, parts_of(sizeof(T), D, NQ) / 256) void
     else decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, whole, at, end, share, base, b, v_head, n);
 }
 
-// Drafted tokens: the same rounds; whole: a workgroup per head of keys and values and tile of rows, some of which there are not
+// Drafted tokens: the same rounds of a part of a tile of rows (tree_part); slots = 0: of all of it
 template <typename T, int D, int NQ>
-__global__ __launch_bounds__(64 * kWaves, parts_of(sizeof(T), D, NQ) / 256) void paged_tree_kernel(TreeArgs a, const T *__restrict__ q, const T *__restrict__ k_cache,
+__global__ __launch_bounds__(64 * kWaves, tree_per_cu(sizeof(T), D, NQ)) void paged_tree_kernel(TreeArgs a, const T *__restrict__ q, const T *__restrict__ k_cache,
                                                                     const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,
-                                                                    float *__restrict__ scratch, int whole)
+                                                                    float *__restrict__ scratch, int target, int slots)
 {
     typedef Decode<T, D> C;
-    typedef TreeRounds<C::ROUND, NQ> Some;
-    constexpr int PARTS = parts_of(sizeof(T), D, NQ);
     __shared__ __attribute__((aligned(1024))) char smem[kWaves * C::REGION];
     __shared__ float sums[kWaves][2][16];
-    const int lane = threadIdx.x & 63;
-    Some group(a, 0, lane, whole);
-    int64_t rounds = group.all();
-    for (int b0 = 64; b0 < a.B; b0 += 64) rounds += Some(a, b0, lane, whole).all();
-    const int64_t all = rounds * a.H_kv, share = whole ? 1 : (all + PARTS - 1) / PARTS, at = blockIdx.x * share, end = min(at + share, all);
-    if (!whole && threadIdx.x == 0) Scratch{scratch, 0, D, PARTS}.chain(blockIdx.x)->b = -1;
-    if (at >= end) return;
-    const int64_t nth = divide(at, a.H_kv);
-    int64_t before = 0;
-    int b0 = 0;
-    while (before + group.all() <= nth) {
-        before += group.all();
-        b0 += 64;
-        group = Some(a, b0, lane, whole);
-    }
-    const int l = __ffsll((long long)__ballot(before + group.upto > nth)) - 1, length = __builtin_amdgcn_readlane(group.length, l);
-    const int64_t base = (before + Some::of(group.upto - group.mine, l)) * a.H_kv;
-    const int v_head = (int)divide(at - base, whole ? 1 : rounds_of<C::ROUND>(a, length));
-    decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, whole, at, end, share, base, b0 + l, v_head, length);
+    TreePart p;
+    const bool some = tree_part<C::ROUND, 16 * NQ, 1>(a, threadIdx.x & 63, blockIdx.x, slots ? target : 1, slots ? slots : gridDim.x, p);
+    if (slots && threadIdx.x == 0) TreeScratch{scratch, 16 * NQ, D, slots}.enter(p, some);
+    if (!some) return;
+    decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, true, 0, 1, 0, 0, p.b, 0, p.length, p, slots);
 }
 
 // Joins the parts of the sequences that more than one workgroup had rounds of, in their order: workgroup x those of chain x, queries y, y + gridDim.y ..
 // Thread: four columns of every (THREADS / (D / 4))th part.
-template <typename T, int D, int THREADS, typename Args>
-__global__ __launch_bounds__(THREADS) void decode_merge_kernel(Args a, const float *__restrict__ scratch, int nq, int n_parts, T *__restrict__ out,
+template <typename T, int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void decode_merge_kernel(DecodeArgs a, const float *__restrict__ scratch, int nq, int n_parts, T *__restrict__ out,
                                                                float *__restrict__ lse)
 {
     constexpr int LANES = D / 4, GROUPS = THREADS / LANES;
     __shared__ f32x4 acc[GROUPS][LANES];
     __shared__ float totals[GROUPS];
     const int tid = threadIdx.x, lane = tid & 63;
-    constexpr bool TREE = std::is_same<Args, TreeArgs>::value;
-    const int G = a.H / a.H_kv;
-    const Scratch parts{const_cast<float *>(scratch), TREE ? 16 * nq : min(G, 16 * nq), D, n_parts};
+    const int G = a.H / a.H_kv, groups = (G + 16 * nq - 1) / (16 * nq);
+    const Scratch parts{const_cast<float *>(scratch), min(G, 16 * nq), D, n_parts};
     const Chain chain = *parts.chain(blockIdx.x);
     if (chain.b < 0) return;
-    int begin = 0, n_rows = G;
-    if constexpr (TREE) {
-        rows_of(a, chain.b, begin, n_rows);
-        n_rows *= G;
-    }
-    const int groups = (n_rows + 16 * nq - 1) / (16 * nq);
-    const int sub = chain.v_head % groups, n_q = min(16 * nq, n_rows - sub * 16 * nq), h0 = chain.v_head / groups * G + sub * 16 * nq;
+    const int sub = chain.v_head % groups, n_q = min(16 * nq, G - sub * 16 * nq), h0 = chain.v_head / groups * G + sub * 16 * nq;
     const auto part_of = [&](int i) { return i == 0 ? chain.w : (chain.w & ~1) + 2 * i; };
     const int grp = tid / LANES, col = tid % LANES * 4;
     for (int n = blockIdx.y; n < n_q; n += gridDim.y) {
@@ -699,8 +605,7 @@ __global__ __launch_bounds__(THREADS) void decode_merge_kernel(Args a, const flo
         if (tid % LANES == 0) totals[grp] = total;
         __syncthreads();
         if (tid < D) {
-            int64_t row = (int64_t)chain.b * a.H + h0 + n;
-            if constexpr (TREE) row = tree_row(a, begin, G, chain.v_head / groups, sub * 16 * nq + n);
+            const int64_t row = (int64_t)chain.b * a.H + h0 + n;
             float value = 0.f;
             total = 0.f;
 #pragma unroll
@@ -713,25 +618,6 @@ __global__ __launch_bounds__(THREADS) void decode_merge_kernel(Args a, const flo
         }
         __syncthreads();
     }
-}
-
-template <typename T, int D, int NQ>
-hipError_t launch_tree(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st)
-{
-    const int G = a.H / a.H_kv;
-    const bool whole = a.max_len <= kWholeLen;
-    constexpr int parts = parts_of(sizeof(T), D, NQ);
-    {
-        // (every sequence's last tile may be partly filled)
-        const int64_t tiles = (int64_t)a.rows * G / (16 * NQ) + std::min(a.rows, a.B);
-        TimedLaunch tl(K_PAGED_TREE, st);
-        hipLaunchKernelGGL((paged_tree_kernel<T, D, NQ>), dim3((unsigned)(whole ? tiles * a.H_kv : parts)), dim3(64 * kWaves), 0, st, a, q, k_cache, v_cache, out, lse,
-                           scratch, whole ? 1 : 0);
-    }
-    if (whole) return hipGetLastError();
-    TimedLaunch tl(K_DECODE_MERGE, st);
-    hipLaunchKernelGGL((decode_merge_kernel<T, D, 256, TreeArgs>), dim3((unsigned)parts, 8u), dim3(256), 0, st, a, scratch, NQ, parts, out, lse);
-    return hipGetLastError();
 }
 
 int queries_per_wave(int H, int H_kv) { return H / H_kv > 16 ? 2 : 1; }       // in sixteens
@@ -751,8 +637,8 @@ hipError_t launch(const DecodeArgs &a, const T *q, const T *k_cache, const T *v_
     // (few chains may be long: more threads each)
     const int chains = (int)std::min<int64_t>((int64_t)a.B * v_heads, parts), y = std::min(G, 8);
     TimedLaunch tl(K_DECODE_MERGE, st);
-    if (chains * y <= 256) hipLaunchKernelGGL((decode_merge_kernel<T, D, 1024, DecodeArgs>), dim3((unsigned)chains, (unsigned)y), dim3(1024), 0, st, a, scratch, NQ, parts, out, lse);
-    else hipLaunchKernelGGL((decode_merge_kernel<T, D, 256, DecodeArgs>), dim3((unsigned)chains, (unsigned)y), dim3(256), 0, st, a, scratch, NQ, parts, out, lse);
+    if (chains * y <= 256) hipLaunchKernelGGL((decode_merge_kernel<T, D, 1024>), dim3((unsigned)chains, (unsigned)y), dim3(1024), 0, st, a, scratch, NQ, parts, out, lse);
+    else hipLaunchKernelGGL((decode_merge_kernel<T, D, 256>), dim3((unsigned)chains, (unsigned)y), dim3(256), 0, st, a, scratch, NQ, parts, out, lse);
     return hipGetLastError();
 }
 
@@ -773,26 +659,20 @@ hipError_t launch_paged_decode(const DecodeArgs &a, const T *q, const T *k_cache
     return two ? launch<T, 128, 2>(a, q, k_cache, v_cache, out, lse, scratch, st) : launch<T, 128, 1>(a, q, k_cache, v_cache, out, lse, scratch, st);
 }
 
-// Rows of an average sequence per head of keys and values decide how many a wavefront takes, in sixteens
-static int tree_rows_per_wave(int64_t rows, int B, int H, int H_kv) { return rows * (H / H_kv) > (int64_t)16 * B ? 2 : 1; }
-
-size_t tree_narrow_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len)
-{
-    if (max_len <= kWholeLen) return 0;
-    const int nq = tree_rows_per_wave(rows, B, H, H_kv);
-    return scratch_bytes(16 * nq, d, parts_of(2, d, nq));
-}
-
 template <typename T>
-hipError_t launch_tree_narrow(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st)
+hipError_t launch_tree_narrow(const TreeArgs &a, const TreePlan &p, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st)
 {
-    const bool two = tree_rows_per_wave(a.rows, a.B, a.H, a.H_kv) == 2;
-    if (a.d == 64) return two ? launch_tree<T, 64, 2>(a, q, k_cache, v_cache, out, lse, scratch, st) : launch_tree<T, 64, 1>(a, q, k_cache, v_cache, out, lse, scratch, st);
-    return two ? launch_tree<T, 128, 2>(a, q, k_cache, v_cache, out, lse, scratch, st) : launch_tree<T, 128, 1>(a, q, k_cache, v_cache, out, lse, scratch, st);
+    const int64_t tiles = ((int64_t)a.rows * (a.H / a.H_kv) / p.rows + std::min(a.rows, a.B)) * a.H_kv;
+    const dim3 grid((unsigned)(((p.slots ? p.slots : tiles) + 7) / 8 * 8)), block(64 * kWaves);
+    TimedLaunch tl(K_PAGED_TREE, st);
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, q, k_cache, v_cache, out, lse, scratch, p.target, p.slots); };
+    if (a.d == 64) p.rows == 16 ? go(paged_tree_kernel<T, 64, 1>) : go(paged_tree_kernel<T, 64, 2>);
+    else p.rows == 16 ? go(paged_tree_kernel<T, 128, 1>) : go(paged_tree_kernel<T, 128, 2>);
+    return hipGetLastError();
 }
 
-template hipError_t launch_tree_narrow<bf16_t>(const TreeArgs &, const bf16_t *, const bf16_t *, const bf16_t *, bf16_t *, float *, float *, hipStream_t);
-template hipError_t launch_tree_narrow<float>(const TreeArgs &, const float *, const float *, const float *, float *, float *, float *, hipStream_t);
+template hipError_t launch_tree_narrow<bf16_t>(const TreeArgs &, const TreePlan &, const bf16_t *, const bf16_t *, const bf16_t *, bf16_t *, float *, float *, hipStream_t);
+template hipError_t launch_tree_narrow<float>(const TreeArgs &, const TreePlan &, const float *, const float *, const float *, float *, float *, float *, hipStream_t);
 
 template hipError_t launch_paged_decode<bf16_t>(const DecodeArgs &, const bf16_t *, const bf16_t *, const bf16_t *, bf16_t *, float *, float *, hipStream_t);
 template hipError_t launch_paged_decode<float>(const DecodeArgs &, const float *, const float *, const float *, float *, float *, float *, hipStream_t);

@@ -57,19 +57,39 @@ struct FwdView {
     int l_s, l_x, causal, G;    // rows, keys
 };
 
+// ... and drafted tokens over a paged cache (FwdView's k, v and their distances are not used; s0 and causal where there is no tree): tiles t0 .. t1 - 1 of the sequence's keys
+struct PagedView : FwdView {
+    const TreeArgs *a;
+    const int32_t *table;       // the sequence's
+    const char *k_head, *v_head;        // of the head, page 0
+    const uint64_t *bits;       // of the sequence's first row
+    int first, t0, t1;          // key of the first drafted token
+    int *spoilt;                // LDS, 0: has some value among the drafted ones' been found that is not finite
+};
+// v with 0 in the place of what is not finite
+__device__ __forceinline__ bf16x8 finite_part(bf16x8 v)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (!(fabsf((float)v[e]) < INFINITY)) v[e] = (bf16_t)0.f;
+    return v;
+}
+
 // DROP: dropout on the weights (Section 2.2): the weight that multiplies V is dropped or (the finished sum) scaled by
 // 1 / (1 - p) according to drop_keep() of (seed, batch*head, global row, key); row sum and lse are
 // those of the softmax.
 // The rows r0 .. of a workgroup: put(u, values) takes columns 8 u + 4 (lane / 32) .. + 3 of row r0 + 32 (wavefront) + lane % 32, normalised,
 // put_lse its lse.  `bh`: batch * head for the dropout's decisions.  PACKED: G heads of a token, K's and V's rows each with a distance of their own,
 // perhaps more rows than keys (a segment has none of that, and what is not there costs its kernels nothing: 1.2 % of lx24k's last segment).
-template <int D, bool DROP, int RB, int KG, bool PACKED, typename Put, typename PutLse>
-__device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, const DropArgs &dr, int bh, int r0, int split, int n_splits, Put &&put,
+template <int D, bool DROP, int RB, int KG, bool PACKED, typename View, typename Put, typename PutLse>
+__device__ __forceinline__ void fwd_bf16_body(char *smem, const View &s, const DropArgs &dr, int bh, int r0, int split, int n_splits, Put &&put,
                                               PutLse &&put_lse)
 {
     using C = FwdBf16Cfg<D, RB, KG>;
     using Tile = typename C::Tile;
     constexpr int NU = C::NU;
+    constexpr bool PAGED = std::is_same<View, PagedView>::value;
+    static_assert(!PAGED || (PACKED && KG == 1), "");
 
     const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, hh = lane >> 5;
     const int all_waves = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -83,7 +103,8 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
     if (PACKED) kv_end = max(kv_end, 0);                // (more rows than keys: the first ones see none)
     const int n_tiles = (kv_end + C::BC - 1) / C::BC;
     const int per = (n_tiles + n_splits - 1) / n_splits;
-    const int s_begin = split * per, s_tiles = max(min(n_tiles, s_begin + per) - s_begin, 0);
+    int s_begin = split * per, s_tiles = max(min(n_tiles, s_begin + per) - s_begin, 0);
+    if constexpr (PAGED) s_begin = s.t0, s_tiles = max(min(n_tiles, s.t1) - s.t0, 0);
     // this group's tiles; the first group has `iters` of them, the last ones fewer or none
     const int iters = KG > 1 ? (s_tiles + KG - 1) / KG : s_tiles;
     const int t_begin = s_begin + group * iters, T = KG > 1 ? max(min(s_tiles - group * iters, iters), 0) : s_tiles;
@@ -147,18 +168,75 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
         };
         to_part(k_tile_next, offK, false);
         to_part(v_tile_next, offV, true);
+        // Pages: this lane's place in a part of 16 rows; buffers of the next K tile's part and, one tile behind, of V's; 64 pages' numbers, a lane each, and the 64 behind
+        // them (page numbers wait for nothing when a tile's turn comes).  `holes`: some number so far was none
+        uint32_t off_page[PAGED ? Tile::NI : 1];
+        u32x4 k_buffer, v_buffer;
+        int window = 0, window_behind = 0, window_at = 0, row_bytes = 0;
+        bool holes = false;
+        int64_t k_row = 0;              // bytes from page 0, and how many
+        uint32_t k_ok = 0;
+        const auto numbers = [&](int from) {
+            if constexpr (PAGED) return s.table[min(from + lane, s.a->pt.max_pages - 1)];
+            else return 0;
+        };
+        const auto look_for_holes = [&] {
+            if constexpr (PAGED) holes = holes || __any(((window_at + lane) << s.a->pt.page_shift) < s.l_x && (uint32_t)window >= (uint32_t)s.a->pt.n_pages);
+        };
+        const auto find_page = [&](int t) __attribute__((always_inline)) {
+            if constexpr (PAGED) {
+                const int key = t * C::BC + wave * 16 / (RB / 4) / 16 * 16, shift = s.a->pt.page_shift;
+                if ((key >> shift) - window_at >= 64) {
+                    window_at += 64;
+                    window = window_behind;
+                    window_behind = numbers(window_at + 64);
+                    look_for_holes();
+                }
+                const int page = __builtin_amdgcn_readlane(window, (key >> shift) - window_at & 63);
+                const bool there = (uint32_t)page < (uint32_t)s.a->pt.n_pages && key < s.l_x;
+                k_row = (((int64_t)(there ? page : 0) << shift) + (key & ((1 << shift) - 1))) * row_bytes;
+                k_ok = there ? (uint32_t)(min(s.l_x - key, 16) - 1) * (uint32_t)row_bytes + D * 2 : 0;
+            }
+        };
+        const auto buffer_of = [&](const char *head) __attribute__((always_inline)) {
+            const uint64_t p = (uint64_t)(head + k_row);
+            const auto uniform = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+            return u32x4{uniform((uint32_t)p), uniform((uint32_t)(p >> 32) & 0xffffu), uniform(k_ok), 0x00020000u};
+        };
+        if constexpr (PAGED) {
+            static_assert(RB == 4 || RB == 8, "");
+            row_bytes = s.a->H_kv * D * 2;
+            Tile::page_offsets(off_page, (uint32_t)row_bytes, wave, lane);
+            window_at = t_begin * C::BC >> s.a->pt.page_shift;
+            window = numbers(window_at);
+            window_behind = numbers(window_at + 64);
+            look_for_holes();
+            find_page(t_begin);
+            k_buffer = buffer_of(s.k_head);
+            v_buffer = buffer_of(s.v_head);
+        }
         auto advance_k = [&] {
+            if constexpr (PAGED) {
+                // (V's next tile is the one that was K's)
+                v_buffer = buffer_of(s.v_head);
+                if (k_tile_next < t_last) {
+                    find_page(++k_tile_next);
+                    k_buffer = buffer_of(s.k_head);
+                }
+                return;
+            }
             if (k_tile_next < t_last) { ++k_tile_next; k_next += k_bytes; to_part(k_tile_next, offK, false); }
         };
         auto advance_v = [&] {
-            if (v_tile_next < t_last) { ++v_tile_next; v_next += v_bytes; to_part(v_tile_next, offV, true); }
+            if (!PAGED && v_tile_next < t_last) { ++v_tile_next; v_next += v_bytes; to_part(v_tile_next, offV, true); }
         };
         // Iteration t's loads, behind its barrier: K of tile t + 2 in the place of tile t's, whose last rows have been read
         // by then, and V of tile t + 1 in the place of tile t - 1's.  (Past the end a tile is loaded once more: K where it
         // lies already or where nobody reads any more, V where nobody reads any more.)
         auto issue_next = [&](char *pair_slot) __attribute__((always_inline)) {
             static_assert(C::OFF_V == Tile::BYTES, "V tile follows K tile");
-            Tile::issue_pair(k_next, v_next, offK, offV, pair_slot, wave);
+            if constexpr (PAGED) Tile::issue_pages(k_buffer, v_buffer, off_page, pair_slot, wave);
+            else Tile::issue_pair(k_next, v_next, offK, offV, pair_slot, wave);
             if (DROP && wave == 0)
                 reinterpret_cast<uint32_t *>(ck_ring)[(k_tile_next & 3) * C::BC + lane] = drop_col_key(drop_cs, (uint32_t)(k_tile_next * C::BC + lane));
         };
@@ -190,8 +268,26 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
         // 0: keys after the lane's row, and keys past the sequence (whose loads re-read its last
         // row).  C-tile element e of this lane is key 8*(e/4) + 4*hh + e%4 of the block.
         // (positions are below 2^30, checked on the host: one 32-bit scalar compare, no vector work per step)
-        const int last_whole = min(s.causal ? (int)s.s0 + rw0 / G - 31 : s.l_x, s.l_x - 32);       // blocks from here on need no mask
+        int last_whole = min(s.causal ? (int)s.s0 + rw0 / G - 31 : s.l_x, s.l_x - 32);       // blocks from here on need no mask
+        if constexpr (PAGED)
+            if (!s.causal) last_whole = min(last_whole, s.first - 32);
         auto mask_s = [&](int jb, f32x16 &sc) __attribute__((always_inline)) {
+            if constexpr (PAGED) {
+                if (jb > last_whole || holes) {
+                    const int token = min(r, s.l_s - 1) / G, left = s.l_x - jb;
+                    uint32_t seen = keys_seen(*s.a, s.bits + (int64_t)token * s.a->words, token, jb - s.first);
+                    if (left < 32) seen &= left <= 0 ? 0u : (1u << left) - 1;
+                    if (holes)
+                        for (int i = 0; i < 2; ++i) {
+                            const int nth = (jb + 16 * i) >> s.a->pt.page_shift;
+                            if (jb + 16 * i < s.l_x && (uint32_t)s.table[nth] >= (uint32_t)s.a->pt.n_pages) seen &= ~(0xffffu << 16 * i);
+                        }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (!(seen >> (8 * (e >> 2) + 4 * hh + (e & 3)) & 1)) sc[e] = -INFINITY;
+                }
+                return;
+            }
             if (jb > last_whole) {
                 const int last = s.causal ? min(position, s.l_x - 1) : s.l_x - 1;
                 const int rel = max(min(last - jb - 4 * hh, 64), -1);
@@ -277,6 +373,24 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
         // (ak[0], cv[0] on entry), and this step leaves there those of the next step: halves kb2_an and kb2_cn.  `mid` runs
         // before those last reads: the even steps put the loop's barrier there, because the next step's blocks may lie in the
         // tile that the barrier publishes, and move the addresses on.
+        // Pages: V of a tile that drafted tokens are in, once it has landed and ahead of the barrier that shows it to the others: 0 in the place of values that are not
+        // finite, of the rows that this wavefront loaded.  0 times such a value is NaN, and not all rows see it; those that do get it at the end.
+        const auto clean = [&](char *pair_slot, int t) __attribute__((always_inline)) {
+            if constexpr (PAGED) {
+                if ((t + 1) * C::BC <= s.first) return;
+                bool some = false;
+#pragma unroll
+                for (int i = 0; i < Tile::NI; ++i) {
+                    bf16x8 *const at = reinterpret_cast<bf16x8 *>(pair_slot + C::OFF_V + (wave * Tile::NI + i) * 1024 + lane * 16);
+                    const bf16x8 v = *at, kept = finite_part(v);
+                    const u32x4 x = __builtin_bit_cast(u32x4, v), y = __builtin_bit_cast(u32x4, kept);
+                    some = some || x[0] != y[0] || x[1] != y[1] || x[2] != y[2] || x[3] != y[3];
+                    *at = kept;
+                }
+                if (__any(some) && lane == 0) *s.spoilt = 1;
+                wait_lds_reads();
+            }
+        };
         Frag<bf16_t> ak[2], cv[2];
         auto step = [&](auto has_a, auto has_b, auto has_c, int kb2_a, f32x16 &sc_a, f32x16 &sc_b,
                         int jb_b, Frag<bf16_t> (&pf_b)[2], int kb2_c, Frag<bf16_t> (&pf_c)[2], int kb2_an, int kb2_cn, auto &&mid)
@@ -349,6 +463,7 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
             // tiles and meeting the loop's barriers.
             for (int t = 0; t < T; ++t) {
                 wait_vmem_all();
+                clean(ring + ((t & 1) ^ 1) * C::PAIR, t_begin + t);
                 __syncthreads();
                 issue_next(ring + (t & 1) * C::PAIR);
                 advance_k();
@@ -377,6 +492,7 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
                 // requested its last operands from K of tile t and V of tile t-1.
                 step(true_type{}, true_type{}, true_type{}, 1, sc1, sc0, j0, pf0, 1, pf1, 0, 0, [&] {
                     wait_vmem_all();
+                    clean(ring + slot + other, t_begin + t);
                     __syncthreads();
                     issue_next(ring + slot);
 #pragma unroll
@@ -384,6 +500,10 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
 #pragma unroll
                     for (int db = 0; db < D / 32; ++db) { t_at[db][0] += other; t_at[db][1] += other; }
                 });
+                if constexpr (PAGED)                    // (zeros times a first value that is not finite)
+                    if (t == 0)
+#pragma unroll
+                        for (int db = 0; db < D / 32; ++db) o[db] = zero16;
                 // odd step g = 2t+1: A(2t+2) [tile t+1, first half; past the end of whatever its slot holds, result unused],
                 // B(2t+1), C(2t) [tile t, first half]
                 step(true_type{}, true_type{}, true_type{}, 0, sc0, sc1, j0 + 32, pf1, 0, pf0, 1, 1, nothing);
@@ -398,6 +518,28 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const FwdView &s, cons
         if (KG > 1)
             for (int t = T; t < iters; ++t) __syncthreads();           // the barriers of the groups that have more tiles
         wait_vmem_all();                                // the last, redundant prefetches must land before the workgroup's LDS is given away
+    }
+    if constexpr (PAGED) {
+        // values that are not finite in the tiles that drafted tokens are in, to the rows that see them: their weights are above 0, whatever they are
+        if (s_tiles > 0 && *s.spoilt && rw0 < s.l_s) {
+            const int token = min(r, s.l_s - 1) / G;
+            for (int key = max(max(s.first, 0) / C::BC, s_begin) * C::BC; key < min(s.l_x, (s_begin + s_tiles) * C::BC); ++key) {
+                const uint32_t page = (uint32_t)s.table[key >> s.a->pt.page_shift];
+                const bool sees = page < (uint32_t)s.a->pt.n_pages && (keys_seen(*s.a, s.bits + (int64_t)token * s.a->words, token, key - s.first) & 1);
+                if (!sees) continue;
+                const int64_t row = ((int64_t)page << s.a->pt.page_shift) + (key & ((1 << s.a->pt.page_shift) - 1));
+                const bf16_t *const value = reinterpret_cast<const bf16_t *>(s.v_head + row * (s.a->H_kv * D * 2)) + 4 * hh;
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                    for (int e4 = 0; e4 < 4; ++e4) {
+                        const bf16x4 x = *reinterpret_cast<const bf16x4 *>(value + 32 * db + 8 * e4);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!(fabsf((float)x[e]) < INFINITY)) o[db][4 * e4 + e] += (float)x[e];
+                    }
+            }
+        }
     }
 
     const float l_own = l + __shfl_xor(l, 32);
@@ -548,6 +690,81 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void packed_bf16_ker
         row_attention<bf16_t, D, 8>(view.q + (int64_t)at * a.q_stride + again % G * D, view.k, a.k_stride, view.v, a.v_stride, seen, row_lse, lane,
                                  out + ((int64_t)(t.q_begin + at) * a.H + head) * D);
     }
+}
+
+// Drafted tokens over a paged cache (lss_paged_attn_tree): rows as above, keys and values from pages.
+// WHOLE: a workgroup per tile of 128 rows, those with the most keys first; else per part of a tile's keys (tree_part), joined by a second launch.
+template <int D, bool WHOLE>
+__global__ __launch_bounds__(256, 2) void tree_bf16_kernel(TreeArgs a, const bf16_t *__restrict__ q, const bf16_t *__restrict__ k_cache,
+                                                          const bf16_t *__restrict__ v_cache, bf16_t *__restrict__ out, float *__restrict__ lse,
+                                                          float *__restrict__ scratch, int n_tiles, int target, int slots)
+{
+    using C = FwdBf16Cfg<D, 4, 1>;
+    __shared__ __attribute__((aligned(1024))) char smem[C::lds(false)];
+    __shared__ int spoilt;
+    const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5, G = a.H / a.H_kv;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const TreeScratch parts{scratch, C::BR, D, slots};
+    TreePart p;
+    if constexpr (WHOLE) {
+        int rank;
+        if (!xcd_item(blockIdx.x, a.H_kv, n_tiles, true, p.h_kv, rank)) return;
+        PackedTile t;
+        if (!packed_tile<C::BR>(a, G, rank, lane, t)) return;
+        p.b = t.b, p.tile = t.tile, p.begin = t.q_begin, p.n = t.n_q, p.length = t.n_k, p.r0 = 0, p.r1 = (t.n_k + C::BC - 1) / C::BC, p.count = 1, p.slot = 0;
+    } else {
+        const bool some = tree_part<C::BC, C::BR, 4>(a, lane, blockIdx.x, target, slots, p);
+        if (threadIdx.x == 0) parts.enter(p, some);
+        if (!some) return;
+    }
+    if (threadIdx.x == 0) spoilt = 0;
+    __syncthreads();
+    PagedView view;
+    view.q = q + (int64_t)p.begin * a.q_stride + (int64_t)p.h_kv * G * D;
+    view.q_ld = a.q_stride;
+    view.k = view.v = nullptr;
+    view.k_ld = view.v_ld = 0;
+    view.s0 = view.first = p.length - p.n;
+    view.l_s = p.n * G;
+    view.l_x = p.length;
+    view.causal = a.tree == nullptr;
+    view.G = G;
+    view.a = &a;
+    view.table = a.pt.table + (int64_t)p.b * a.pt.max_pages;
+    view.k_head = reinterpret_cast<const char *>(k_cache + (int64_t)p.h_kv * D);
+    view.v_head = reinterpret_cast<const char *>(v_cache + (int64_t)p.h_kv * D);
+    view.bits = a.tree + (int64_t)p.begin * a.words;
+    view.t0 = p.r0;
+    view.t1 = p.r1;
+    view.spoilt = &spoilt;
+    const int in_tile = wave * C::RW + lq, r = p.tile * C::BR + in_tile, token = p.begin + r / G, h = p.h_kv * G + r % G;
+    const bool all = WHOLE || p.count == 1;
+    fwd_bf16_body<D, false, 4, 1, true>(
+        smem, view, DropArgs{}, 0, p.tile * C::BR, 0, 1,
+        [&](int u, const f32x4 &val) __attribute__((always_inline)) {
+            if (all) *reinterpret_cast<bf16x4 *>(out + ((int64_t)token * a.H + h) * D + 8 * u + 4 * hh) = pack4(val[0], val[1], val[2], val[3]);
+            else *reinterpret_cast<f32x4 *>(parts.values(p.slot, in_tile) + 8 * u + 4 * hh) = val;
+        },
+        [&](float v) {
+            if (all) {
+                lse[(int64_t)token * a.H + h] = v;
+                return;
+            }
+            parts.sums(p.slot, in_tile)[0] = v * kLog2e;
+            parts.sums(p.slot, in_tile)[1] = v == -INFINITY ? 0.f : 1.f;
+        });
+}
+
+hipError_t launch_tree_bf16_main(const TreeArgs &a, const TreePlan &p, const bf16_t *q, const bf16_t *k_cache, const bf16_t *v_cache, bf16_t *out, float *lse, float *scratch,
+                                 hipStream_t st)
+{
+    const int n_tiles = (int)((int64_t)a.rows * (a.H / a.H_kv) / 128) + (a.B <= 64 && a.rows < a.B ? a.rows : a.B);
+    TimedLaunch tl(K_TREE_BF16, st);
+    const dim3 grid((unsigned)(p.slots == 0 ? xcd_grid(a.H_kv, n_tiles) : (p.slots + 7) / 8 * 8)), block(256);
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, q, k_cache, v_cache, out, lse, scratch, n_tiles, p.target, p.slots); };
+    if (a.d == 64) p.slots == 0 ? go(tree_bf16_kernel<64, true>) : go(tree_bf16_kernel<64, false>);
+    else p.slots == 0 ? go(tree_bf16_kernel<128, true>) : go(tree_bf16_kernel<128, false>);
+    return hipGetLastError();
 }
 
 int fwd_bf16_rows_per_workgroup(int d) { return d == 64 ? 128 : 256; }

@@ -112,7 +112,7 @@ enum KernelId { K_FWD_F32 = 0, K_FWD_MERGE, K_ROWDOT, K_BWD_MAIN_F32, K_DQ_MERGE
                 K_PE_FWD, K_PE_BWD, K_LN_FWD, K_LN_BWD, K_LN_PARAMS, K_GELU_FWD, K_GELU_BWD, K_LINEAR_FWD, K_LINEAR_BWD, K_RESIDUAL, K_LINEAR_WGRAD,
                 K_FWD_BF16, K_BWD_PREP_BF16, K_BWD_SKINNY_BF16, K_LN_BWD_SHORT, K_PROJ_FWD_SMALL, K_PROJ_BWD_SMALL, K_LINEAR_FWD_SMALL,
                 K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_BF16, K_PACKED_F32, K_PACKED_MERGE, K_PAGED_TREE, K_FORK_CLEAR,
-                K_FORK_TABLE, K_FORK_PLAN, K_FORK_COPY, K_PAGED_COMPACT, K_BEAM_ROWS, K_BEAM_SELECT, K_COUNT };
+                K_FORK_TABLE, K_FORK_PLAN, K_FORK_COPY, K_PAGED_COMPACT, K_BEAM_ROWS, K_BEAM_SELECT, K_TREE_BF16, K_TREE_MERGE, K_COUNT };
 void timing_begin(int id, hipStream_t st);
 void timing_end(int id, hipStream_t st);
 struct TimedLaunch {    // RAII bracket around one kernel launch
@@ -207,10 +207,16 @@ struct TreeArgs {
 size_t paged_tree_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem_bytes);
 template <typename T>
 hipError_t launch_paged_tree(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st);
-// ... by the kernel of the attention of one token (lss_decode.hip)
-size_t tree_narrow_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len);
+// How a call is run.  wide (bf16): workgroups of 128 rows by the packed forward's body (lss_fwd_bf16.hip), else of `rows` by the attention of one token's
+// (lss_decode.hip).  slots: parts that there are room for, about `target` of them where the sequences are long; 0: a workgroup per tile of rows
+struct TreePlan {
+    bool wide;
+    int rows, target, slots;
+};
+hipError_t launch_tree_bf16_main(const TreeArgs &a, const TreePlan &p, const bf16_t *q, const bf16_t *k_cache, const bf16_t *v_cache, bf16_t *out, float *lse, float *scratch,
+                                 hipStream_t st);
 template <typename T>
-hipError_t launch_tree_narrow(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st);
+hipError_t launch_tree_narrow(const TreeArgs &a, const TreePlan &p, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st);
 struct ForkArgs {
     PageTable pt;                       // of the B sequences before
     const int32_t *lengths, *parents, *room, *held;     // [B], [B_out], [B_out] or null, [n_pages] or null

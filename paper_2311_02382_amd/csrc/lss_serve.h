@@ -48,22 +48,34 @@ __device__ __forceinline__ int lane_sum_scan(int x)     // inclusive over the wa
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
     return x;
 }
-struct PackedTile { int q_begin, n_q, k_begin, n_k, tile; };
+struct PackedTile { int q_begin, n_q, k_begin, n_k, tile, b; };
 // Tile `rank` of a head of keys and values; false: there are fewer.  Up to 64 sequences, a lane each: tiles in the order of the keys they see (in
 // steps of 64), most first, so that no long one starts last.  More sequences: in the sequences' order, sequence b's tiles from number
 // floor(cu[b] G / BR) + b on -- room for all of them, one at most too much --, which is found like a row's sequence.
-template <int BR>
-__device__ __forceinline__ bool packed_tile(const PackedArgs &a, int G, int rank, int lane, PackedTile &t)
+__device__ __forceinline__ void sequence_rows(const int32_t *cu, int b, int rows, int &begin, int &n)
 {
-    const auto ends = [](const int32_t *cu, int b, int rows, int &begin, int &n) {
-        begin = max(0, min(cu[b], rows));
-        n = max(0, min(cu[b + 1], rows) - begin);
-    };
+    begin = max(0, min(cu[b], rows));
+    n = max(0, min(cu[b + 1], rows) - begin);
+}
+__device__ __forceinline__ void queries_of(const PackedArgs &a, int b, int &begin, int &n) { sequence_rows(a.cu_q, b, a.rows_q, begin, n); }
+__device__ __forceinline__ void keys_of(const PackedArgs &a, int b, int &begin, int &n) { sequence_rows(a.cu_k, b, a.rows_k, begin, n); }
+__device__ __forceinline__ int first_query(const PackedArgs &a, int b) { return max(0, min(a.cu_q[b], a.rows_q)); }
+__device__ __forceinline__ int most_keys(const PackedArgs &a) { return a.rows_k; }
+__device__ __forceinline__ bool is_causal(const PackedArgs &a) { return a.causal; }
+// ... of drafted tokens, whose keys are in the cache (their number; they begin nowhere)
+__device__ __forceinline__ void queries_of(const TreeArgs &a, int b, int &begin, int &n) { sequence_rows(a.cu, b, a.rows, begin, n); }
+__device__ __forceinline__ void keys_of(const TreeArgs &a, int b, int &begin, int &n) { begin = 0, n = max(0, min(a.lengths[b], a.max_len)); }
+__device__ __forceinline__ int first_query(const TreeArgs &a, int b) { return max(0, min(a.cu[b], a.rows)); }
+__device__ __forceinline__ int most_keys(const TreeArgs &a) { return a.max_len; }
+__device__ __forceinline__ bool is_causal(const TreeArgs &a) { return a.tree == nullptr; }
+template <int BR, typename Args>
+__device__ __forceinline__ bool packed_tile(const Args &a, int G, int rank, int lane, PackedTile &t)
+{
     int b, begin = 0, n_q = 0, k_begin = 0, n_k = 0, tile;
     if (a.B <= 64) {
         if (lane < a.B) {
-            ends(a.cu_q, lane, a.rows_q, begin, n_q);
-            ends(a.cu_k, lane, a.rows_k, k_begin, n_k);
+            queries_of(a, lane, begin, n_q);
+            keys_of(a, lane, k_begin, n_k);
         }
         const int tiles = (n_q * G + BR - 1) / BR;
         // its tiles that see keys from number 64 (x - 1) on: tile j's last row is of token ((j + 1) BR - 1) / G
@@ -71,10 +83,10 @@ __device__ __forceinline__ bool packed_tile(const PackedArgs &a, int G, int rank
             if (x <= 1) return tiles;
             const int last = 64 * (x - 1);              // some row's position must reach it
             if (last >= n_k) return 0;
-            return a.causal ? max(0, tiles - max(0, last - (n_k - n_q)) * G / BR) : tiles;
+            return is_causal(a) ? max(0, tiles - max(0, last - (n_k - n_q)) * G / BR) : tiles;
         };
         const auto total = [&](int x) { return __builtin_amdgcn_readlane(lane_sum_scan(count(x)), 63); };
-        int lo = 1, hi = (a.rows_k + 63) / 64 + 1;      // total(lo) > rank >= total(hi)
+        int lo = 1, hi = (most_keys(a) + 63) / 64 + 1;      // total(lo) > rank >= total(hi)
         if (rank >= total(1)) return false;
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
@@ -85,10 +97,10 @@ __device__ __forceinline__ bool packed_tile(const PackedArgs &a, int G, int rank
         b = __ffsll((long long)__ballot(scan > in)) - 1;
         tile = tiles - count(lo) + in - (scan - mine);
         const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, b); };
-        t = {of(begin), of(n_q), of(k_begin), of(n_k), of(tile)};
+        t = {of(begin), of(n_q), of(k_begin), of(n_k), of(tile), b};
         return true;
     }
-    const auto first = [&](int i) { return (int)((int64_t)max(0, min(a.cu_q[i], a.rows_q)) * G / BR) + i; };
+    const auto first = [&](int i) { return (int)((int64_t)first_query(a, i) * G / BR) + i; };
     int lo = 0, n = a.B;
     while (n > 1) {
         const int step = (n + 63) / 64, at = lane * step;
@@ -99,10 +111,10 @@ __device__ __forceinline__ bool packed_tile(const PackedArgs &a, int G, int rank
         n = min(step, n - last * step);
     }
     b = __builtin_amdgcn_readfirstlane(lo);
-    ends(a.cu_q, b, a.rows_q, begin, n_q);
-    ends(a.cu_k, b, a.rows_k, k_begin, n_k);
+    queries_of(a, b, begin, n_q);
+    keys_of(a, b, k_begin, n_k);
     t = {__builtin_amdgcn_readfirstlane(begin), __builtin_amdgcn_readfirstlane(n_q), __builtin_amdgcn_readfirstlane(k_begin),
-         __builtin_amdgcn_readfirstlane(n_k), __builtin_amdgcn_readfirstlane(rank - first(b))};
+         __builtin_amdgcn_readfirstlane(n_k), __builtin_amdgcn_readfirstlane(rank - first(b)), b};
     return t.tile >= 0 && t.tile < (t.n_q * G + BR - 1) / BR;
 }
 
@@ -176,6 +188,120 @@ __device__ __forceinline__ void row_attention(const T *q, const T *k, int64_t k_
         r[e] = (T)(acc[e] * inv);
     }
     if (lane < CHUNKS) *reinterpret_cast<Vec *>(out + column) = r;
+}
+
+// a / b in 32 bits where both fit (a fifth of the instructions); wavefront-uniform
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b)
+{
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// ---- drafted tokens (lss_paged_attn_tree).  Sequence b has n_b G rows per head of keys and values, row r of them query head r % G of its drafted token r / G: tiles
+// of BR rows.  The rounds of a tile (ROUND keys each) are cut into parts of as many as it takes to have about `target` of all sequences together, at least LEAST; a
+// workgroup has one.
+struct TreePart {
+    int b, h_kv, tile, tiles, begin, n, length;         // n: drafted tokens, from row `begin` on
+    int r0, r1, count, slot;                            // rounds; parts of the tile of rows, whose numbers are `tiles` apart; this one's
+    int parts;                                          // of the launch (set in any case)
+};
+__device__ __forceinline__ int64_t lane64(int64_t x, int lane)        // of that lane, wavefront-uniform
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32);
+}
+__device__ __forceinline__ int64_t lanes_upto(int64_t x, int lane)    // inclusive sum
+{
+#pragma unroll
+    for (int sh = 1; sh < 64; sh *= 2) {
+        const int64_t below = __shfl_up(x, sh);
+        if (lane >= sh) x += below;
+    }
+    return x;
+}
+// Workgroup `id`'s part; false: there is none.  Parts are numbered by sequence, head, part of the keys and tile of rows, and each XCD (workgroups go to them in turn) has a run
+// of them: tiles of rows that read the same keys do so at the same time from one L2.  All lanes active; wavefront-uniform.
+template <int ROUND, int BR, int LEAST>
+__device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, int target, int slots, TreePart &p)
+{
+    const int G = a.H / a.H_kv;
+    struct Some { int length, begin, n, tiles, R; };
+    const auto load = [&](int b0) {
+        Some s{0, 0, 0, 0, 0};
+        if (b0 + lane < a.B) {
+            s.length = max(0, min(a.lengths[b0 + lane], a.max_len));
+            queries_of(a, b0 + lane, s.begin, s.n);
+        }
+        s.tiles = (s.n * G + BR - 1) / BR;              // (rows * H <= 2^24)
+        s.R = (max(1, s.length) + ROUND - 1) / ROUND;
+        return s;
+    };
+    Some s = load(0);
+    int64_t rounds = lane64(lanes_upto((int64_t)s.tiles * s.R, lane), 63);
+    for (int b0 = 64; b0 < a.B; b0 += 64) {
+        const Some t = load(b0);
+        rounds += lane64(lanes_upto((int64_t)t.tiles * t.R, lane), 63);
+    }
+    const int64_t wanted = divide(rounds * a.H_kv + target - 1, target);
+    const int S = (int)min(max(wanted, (int64_t)LEAST), (int64_t)1 << 30);
+    const auto parts = [&](const Some &t) { return (int64_t)t.tiles * ((t.R + S - 1) / S); };
+    int64_t mine = parts(s), upto = lanes_upto(mine, lane), all = lane64(upto, 63);
+    for (int b0 = 64; b0 < a.B; b0 += 64) all += lane64(lanes_upto(parts(load(b0)), lane), 63);
+    // (`slots`: how many there can be where cu ascends)
+    all = min(all * a.H_kv, (int64_t)slots);
+    p.parts = (int)all;
+    const int64_t per_xcd = (all + 7) / 8, at = id % 8 * per_xcd + id / 8;
+    if (id / 8 >= per_xcd || at >= all) return false;
+    const int64_t nth = divide(at, a.H_kv);             // (some sequence has it)
+    int64_t before = 0;
+    int b0 = 0;
+    while (before + lane64(upto, 63) <= nth) {
+        before += lane64(upto, 63);
+        b0 += 64;
+        if (b0 >= a.B) return false;
+        s = load(b0);
+        mine = parts(s);
+        upto = lanes_upto(mine, lane);
+    }
+    const int l = __ffsll((long long)__ballot(before + upto > nth)) - 1;
+    const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+    const int R = of(s.R), tiles = of(s.tiles), c = (R + S - 1) / S, within = (int)(at - (before + lane64(upto - mine, l)) * a.H_kv), rest = within % (tiles * c);
+    p.b = b0 + l, p.begin = of(s.begin), p.n = of(s.n), p.length = of(s.length);
+    p.h_kv = within / (tiles * c), p.tiles = tiles, p.tile = rest % tiles;
+    p.count = c, p.r0 = rest / tiles * S, p.r1 = min(R, p.r0 + S);
+    p.slot = (int)at;
+    return true;
+}
+// row of out and lse of row r of a sequence that begins with drafted token `begin`
+__device__ __forceinline__ int64_t tree_row(const TreeArgs &a, int begin, int G, int h_kv, int r) { return (int64_t)(begin + r / G) * a.H + h_kv * G + r % G; }
+// Scratch memory of `slots` parts, for those of tiles that have several: of each row sum of weight * value [d], maximum (log2 domain) and sum; and for the joining launch
+// how many parts there are, and which tile begins in which.  Every part says so of itself, so that whatever the memory held is not read.
+struct TreeChain { int b, h_kv, tile, count; };          // count <= 1: none begins here that has several
+struct TreeScratch {
+    float *base;
+    int rows, d, slots;
+    __device__ __forceinline__ int *parts() const { return reinterpret_cast<int *>(base); }
+    __device__ __forceinline__ TreeChain *chain(int i) const { return reinterpret_cast<TreeChain *>(base) + 1 + i; }
+    __device__ __forceinline__ float *sums(int part, int n) const { return base + 4 * (slots + 1) + ((int64_t)part * rows + n) * 2; }
+    __device__ __forceinline__ float *values(int part, int n) const { return base + 4 * (slots + 1) + (int64_t)slots * rows * 2 + ((int64_t)part * rows + n) * d; }
+    // by one thread of each workgroup
+    __device__ __forceinline__ void enter(const TreePart &p, bool some) const
+    {
+        if (blockIdx.x == 0) *parts() = p.parts;
+        if (some) *chain(p.slot) = {p.b, p.h_kv, p.tile, p.r0 == 0 ? p.count : 0};
+    }
+};
+inline size_t tree_scratch_bytes(int rows, int d, int slots) { return sizeof(float) * (4 * ((size_t)slots + 1) + (size_t)slots * rows * (d + 2)); }
+// Which of the 32 keys from drafted number c0 on (below 0: the tokens in front of them) drafted token i of its sequence sees; `bits`: its words
+__device__ __forceinline__ uint32_t keys_seen(const TreeArgs &a, const uint64_t *bits, int i, int c0)
+{
+    if (a.tree == nullptr) {
+        const int last = i - c0;
+        return last < 0 ? 0u : last >= 31 ? ~0u : (2u << last) - 1;
+    }
+    if (c0 <= -32) return ~0u;
+    const int from = max(c0, 0), word = from >> 6, sh = from & 63;
+    uint64_t seen = word < a.words ? bits[word] >> sh : 0;
+    if (sh > 32 && word + 1 < a.words) seen |= bits[word + 1] << (64 - sh);
+    return c0 >= 0 ? (uint32_t)seen : (uint32_t)seen << -c0 | ((1u << -c0) - 1);
 }
 
 } // namespace lss

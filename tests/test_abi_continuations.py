@@ -47,7 +47,7 @@ def test_append_with_positions(lib, change, code):
 @pytest.mark.parametrize("change,code", [
     (dict(d=96), -3), (dict(eb=3), -2), (dict(H=5), -2), (dict(H_kv=3), -2), (dict(H=0), -2), (dict(B=-1), -2), (dict(B=(1 << 24) + 1), -2), (dict(page=17), -2),
     (dict(n_pages=0), -2), (dict(max_pages=1 << 60), -2), (dict(max_len=65), -5), (dict(max_len=-1), -5), (dict(qs=200), -2), (dict(qs=257), -4), (dict(rows=-1), -2),
-    (dict(rows=(1 << 22) + 1), -2), (dict(words=0), -2), (dict(words=1025), -2), (dict(q=0), -1), (dict(kc=0), -1), (dict(vc=0), -1), (dict(lengths=0), -1),
+    (dict(rows=(1 << 22) + 1), -2), (dict(B=(1 << 21) + 1), -2), (dict(words=0), -2), (dict(words=1025), -2), (dict(q=0), -1), (dict(kc=0), -1), (dict(vc=0), -1), (dict(lengths=0), -1),
     (dict(table=0), -1), (dict(cu=0), -1), (dict(out=0), -1), (dict(lse=0), -1), (dict(q=0x1004), -4), (dict(vc=0x3008), -4), (dict(out=0x6004), -4), (dict(table=0x5002), -4),
     (dict(cu=0x5102), -4), (dict(tree=0x5204), -4), (dict(lse=0x7001), -4), (dict(ws=0x10008, wn=1 << 30), -4), (dict(max_pages=4096, max_len=65536, ws=0x10000, wn=100), -6),
     (dict(max_pages=4096, max_len=65536), -6), (dict(out=0x1010), -5), (dict(out=0x1000 + 0x9f0), -5), (dict(qs=1024, out=0x1000 + 4 * 0x800 + 0x1f0), -5),

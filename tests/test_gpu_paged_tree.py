@@ -118,6 +118,7 @@ def test_what_a_row_does_not_see_stays_there(dtype, d, garbage, tree):
     clean = [x.cuda() for x in (q, kc, vc, table, torch.tensor(lengths, dtype=torch.int32), cu)]
     kw = dict(tree=bits.cuda() if tree else None)
     want, want_lse = lss.lss_paged_attn_tree(*clean, **kw)
+    exact, exact_lse, ob, lb = co.tree_attention(q, kc, vc, table, lengths, cu, bits if tree else None)
     mine = torch.zeros(kc.shape[:2], dtype=torch.bool)
     for b, n in enumerate(lengths):
         for p in range(n):
@@ -134,9 +135,10 @@ def test_what_a_row_does_not_see_stays_there(dtype, d, garbage, tree):
                 sees[int(cu[b]) + i] = (int(bits[int(cu[b]) + i, 0]) >> c & 1) != 0 if tree else c <= i
         out, lse = lss.lss_paged_attn_tree(clean[0], bad_k.cuda(), bad_v.cuda(), *clean[3:], **kw)
         torch.cuda.synchronize()
-        assert torch.equal(sv.bits(out[~sees]), sv.bits(want[~sees])) and torch.equal(sv.bits(lse[~sees]), sv.bits(want_lse[~sees]))
+        # (a key that other rows see may make them raise their running maximum, and with them the rows beside them: other roundings, within the bounds)
+        sv.check(out[~sees], exact[~sees], ob[~sees], "out"), sv.check(lse[~sees], exact_lse[~sees], lb[~sees], "lse")
         if what == "v":
-            assert torch.equal(sv.bits(lse), sv.bits(want_lse))
+            assert torch.equal(sv.bits(out[~sees]), sv.bits(want[~sees])) and torch.equal(sv.bits(lse), sv.bits(want_lse))
             spoilt = out[sees].float().cpu()
             if math.isnan(garbage):
                 assert bool(spoilt.isnan().all())
