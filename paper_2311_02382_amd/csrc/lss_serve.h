@@ -202,29 +202,26 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b)
 struct TreePart {
     int b, h_kv, tile, tiles, begin, n, length;         // n: drafted tokens, from row `begin` on
     int r0, r1, count, slot;                            // rounds; parts of the tile of rows, whose numbers are `tiles` apart; this one's
-    int parts;                                          // of the launch (set in any case)
+    int item, items;                                    // which tile of rows of any head, of how many (the latter is set in any case)
 };
 __device__ __forceinline__ int64_t lane64(int64_t x, int lane)        // of that lane, wavefront-uniform
 {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32);
 }
-__device__ __forceinline__ int64_t lanes_upto(int64_t x, int lane)    // inclusive sum
+// inclusive sums over the wavefront of numbers from 0 to 2^50: two 32-bit ones (by shuffles of 64 bits: 1 us for the three of tree_part)
+__device__ __forceinline__ int64_t lanes_upto(int64_t x)
 {
-#pragma unroll
-    for (int sh = 1; sh < 64; sh *= 2) {
-        const int64_t below = __shfl_up(x, sh);
-        if (lane >= sh) x += below;
-    }
-    return x;
+    const int low = lane_sum_scan((int)(x & 0xffffff)), high = lane_sum_scan((int)(x >> 24));
+    return ((int64_t)high << 24) + low;
 }
 // Workgroup `id`'s part; false: there is none.  Parts are numbered by sequence, head, part of the keys and tile of rows, and each XCD (workgroups go to them in turn) has a run
 // of them: tiles of rows that read the same keys do so at the same time from one L2.  All lanes active; wavefront-uniform.
-template <int ROUND, int BR, int LEAST>
-__device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, int target, int slots, TreePart &p)
+template <int ROUND, int BR>
+__device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, int target, int least, int slots, TreePart &p)
 {
     const int G = a.H / a.H_kv;
     struct Some { int length, begin, n, tiles, R; };
-    const auto load = [&](int b0) {
+    const auto load = [&](int b0) __attribute__((always_inline)) {
         Some s{0, 0, 0, 0, 0};
         if (b0 + lane < a.B) {
             s.length = max(0, min(a.lengths[b0 + lane], a.max_len));
@@ -235,31 +232,41 @@ __device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, i
         return s;
     };
     Some s = load(0);
-    int64_t rounds = lane64(lanes_upto((int64_t)s.tiles * s.R, lane), 63);
+    int64_t rounds = lane64(lanes_upto((int64_t)s.tiles * s.R), 63);
+    int all_tiles = __builtin_amdgcn_readlane(lane_sum_scan(s.tiles), 63);
     for (int b0 = 64; b0 < a.B; b0 += 64) {
         const Some t = load(b0);
-        rounds += lane64(lanes_upto((int64_t)t.tiles * t.R, lane), 63);
+        rounds += lane64(lanes_upto((int64_t)t.tiles * t.R), 63);
+        all_tiles += __builtin_amdgcn_readlane(lane_sum_scan(t.tiles), 63);
     }
     const int64_t wanted = divide(rounds * a.H_kv + target - 1, target);
-    const int S = (int)min(max(wanted, (int64_t)LEAST), (int64_t)1 << 30);
-    const auto parts = [&](const Some &t) { return (int64_t)t.tiles * ((t.R + S - 1) / S); };
-    int64_t mine = parts(s), upto = lanes_upto(mine, lane), all = lane64(upto, 63);
-    for (int b0 = 64; b0 < a.B; b0 += 64) all += lane64(lanes_upto(parts(load(b0)), lane), 63);
-    // (`slots`: how many there can be where cu ascends)
-    all = min(all * a.H_kv, (int64_t)slots);
-    p.parts = (int)all;
+    int S = wanted < least ? least : wanted < 1 << 30 ? (int)wanted : 1 << 30;
+    const auto parts = [](const Some &t, int S) { return (int64_t)t.tiles * ((t.R + S - 1) / S); };
+    int64_t mine, upto, all;
+    // (a part too many for the workgroups that there is room for at once waits for all of another: a few sizes are tried, where one part a tile fits)
+    for (int tries = 0;; ++tries) {
+        mine = parts(s, S), upto = lanes_upto(mine), all = lane64(upto, 63);
+        for (int b0 = 64; b0 < a.B; b0 += 64) all += lane64(lanes_upto(parts(load(b0), S)), 63);
+        if (all * a.H_kv <= target || (int64_t)all_tiles * a.H_kv > target || tries == 4 || S >= 1 << 24) break;
+        const int64_t more = divide((all * a.H_kv - target) * S, target);
+        S += more < 1 ? 1 : more < S ? (int)more : S;
+    }
+    all *= a.H_kv;
+    if (all > slots) return p.items = 0, false;         // (cu does not ascend)
+    p.items = all_tiles * a.H_kv;
     const int64_t per_xcd = (all + 7) / 8, at = id % 8 * per_xcd + id / 8;
     if (id / 8 >= per_xcd || at >= all) return false;
     const int64_t nth = divide(at, a.H_kv);             // (some sequence has it)
     int64_t before = 0;
-    int b0 = 0;
+    int b0 = 0, tiles_before = 0;
     while (before + lane64(upto, 63) <= nth) {
         before += lane64(upto, 63);
+        tiles_before += __builtin_amdgcn_readlane(lane_sum_scan(s.tiles), 63);
         b0 += 64;
         if (b0 >= a.B) return false;
         s = load(b0);
-        mine = parts(s);
-        upto = lanes_upto(mine, lane);
+        mine = parts(s, S);
+        upto = lanes_upto(mine);
     }
     const int l = __ffsll((long long)__ballot(before + upto > nth)) - 1;
     const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
@@ -268,28 +275,29 @@ __device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, i
     p.h_kv = within / (tiles * c), p.tiles = tiles, p.tile = rest % tiles;
     p.count = c, p.r0 = rest / tiles * S, p.r1 = min(R, p.r0 + S);
     p.slot = (int)at;
+    p.item = (tiles_before + of(lane_sum_scan(s.tiles) - s.tiles)) * a.H_kv + p.h_kv * tiles + p.tile;
     return true;
 }
 // row of out and lse of row r of a sequence that begins with drafted token `begin`
 __device__ __forceinline__ int64_t tree_row(const TreeArgs &a, int begin, int G, int h_kv, int r) { return (int64_t)(begin + r / G) * a.H + h_kv * G + r % G; }
 // Scratch memory of `slots` parts, for those of tiles that have several: of each row sum of weight * value [d], maximum (log2 domain) and sum; and for the joining launch
-// how many parts there are, and which tile begins in which.  Every part says so of itself, so that whatever the memory held is not read.
-struct TreeChain { int b, h_kv, tile, count; };          // count <= 1: none begins here that has several
+// how many tiles of rows there are, and where the parts of each begin (its first part says so).
+struct TreeChain { int b, h_kv, tile, first, count, tiles, unused[2]; };
 struct TreeScratch {
     float *base;
-    int rows, d, slots;
-    __device__ __forceinline__ int *parts() const { return reinterpret_cast<int *>(base); }
+    int rows, d, slots, tiles;
+    __device__ __forceinline__ int *items() const { return reinterpret_cast<int *>(base); }
     __device__ __forceinline__ TreeChain *chain(int i) const { return reinterpret_cast<TreeChain *>(base) + 1 + i; }
-    __device__ __forceinline__ float *sums(int part, int n) const { return base + 4 * (slots + 1) + ((int64_t)part * rows + n) * 2; }
-    __device__ __forceinline__ float *values(int part, int n) const { return base + 4 * (slots + 1) + (int64_t)slots * rows * 2 + ((int64_t)part * rows + n) * d; }
+    __device__ __forceinline__ float *sums(int part, int n) const { return base + 8 * (tiles + 1) + ((int64_t)part * rows + n) * 2; }
+    __device__ __forceinline__ float *values(int part, int n) const { return base + 8 * (tiles + 1) + (int64_t)slots * rows * 2 + ((int64_t)part * rows + n) * d; }
     // by one thread of each workgroup
     __device__ __forceinline__ void enter(const TreePart &p, bool some) const
     {
-        if (blockIdx.x == 0) *parts() = p.parts;
-        if (some) *chain(p.slot) = {p.b, p.h_kv, p.tile, p.r0 == 0 ? p.count : 0};
+        if (blockIdx.x == 0) *items() = p.items;
+        if (some && p.r0 == 0) *chain(p.item) = {p.b, p.h_kv, p.tile, p.slot, p.count, p.tiles, {0, 0}};
     }
 };
-inline size_t tree_scratch_bytes(int rows, int d, int slots) { return sizeof(float) * (4 * ((size_t)slots + 1) + (size_t)slots * rows * (d + 2)); }
+inline size_t tree_scratch_bytes(int rows, int d, int slots, int tiles) { return sizeof(float) * (8 * ((size_t)tiles + 1) + (size_t)slots * rows * (d + 2)); }
 // Which of the 32 keys from drafted number c0 on (below 0: the tokens in front of them) drafted token i of its sequence sees; `bits`: its words
 __device__ __forceinline__ uint32_t keys_seen(const TreeArgs &a, const uint64_t *bits, int i, int c0)
 {

@@ -7,54 +7,70 @@ namespace lss {
 
 namespace {
 
-// Joins the parts of the tile of rows that begins in part blockIdx.x, in their order: LANES lanes have a row, or in long chains S such groups, which meet in LDS
+// Joins the parts of tile of rows blockIdx.x, in their order: LANES lanes have a row, or in long chains S such groups with a part each, which meet in LDS
 template <typename T, int D>
-__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float *__restrict__ scratch, int rows, int slots, T *__restrict__ out, float *__restrict__ lse)
+__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float *__restrict__ scratch, int rows, int slots, int most_tiles, T *__restrict__ out,
+                                                         float *__restrict__ lse)
 {
-    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES, AHEAD = 4;
     __shared__ f32x4 acc[GROUPS][LANES];
-    __shared__ float totals[GROUPS];
-    const TreeScratch parts{const_cast<float *>(scratch), rows, D, slots};
-    if ((int)blockIdx.x >= *parts.parts()) return;
-    const TreeChain chain = *parts.chain(blockIdx.x);
-    if (chain.count <= 1) return;
+    __shared__ float tops[GROUPS], totals[GROUPS];
+    const TreeScratch parts{const_cast<float *>(scratch), rows, D, slots, most_tiles};
+    const TreeChain chain = *parts.chain(blockIdx.x);   // (there is room for one of each workgroup)
+    if ((int)blockIdx.x >= *parts.items() || chain.count <= 1) return;
     const int G = a.H / a.H_kv, grp = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     int begin, n_rows;
     queries_of(a, chain.b, begin, n_rows);
     n_rows *= G;
-    const int tiles = (n_rows + rows - 1) / rows, n_q = min(rows, n_rows - chain.tile * rows);
-    const int S = chain.count <= 8 ? 1 : chain.count <= 32 ? 4 : GROUPS, at_once = GROUPS / S, share = grp % S;
-    const auto part_of = [&](int i) { return (int)min((int64_t)blockIdx.x + (int64_t)i * tiles, (int64_t)slots - 1); };
+    const int n_q = min(rows, n_rows - chain.tile * rows);
+    const int S = chain.count <= 4 ? 1 : chain.count <= 16 ? 4 : GROUPS, at_once = GROUPS / S, share = grp % S;
     for (int n0 = blockIdx.y * at_once; n0 < n_q; n0 += gridDim.y * at_once) {
         const int n = min(n0 + grp / S, n_q - 1);
-        float top = -INFINITY;
-        for (int i = lane; i < chain.count; i += LANES) top = fmaxf(top, parts.sums(part_of(i), n)[0]);
-#pragma unroll
-        for (int sh = LANES / 2; sh >= 1; sh >>= 1) top = fmaxf(top, __shfl_xor(top, sh));
-        const float use = top == -INFINITY ? 0.f : top;
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        float total = 0.f;
-#pragma unroll 4
-        for (int i = share; i < chain.count; i += S) {
-            const int part = part_of(i);
-            const float weight = fast_exp2(parts.sums(part, n)[0] - use);
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(parts.values(part, n) + 4 * lane);
-            total += weight * parts.sums(part, n)[1];
+        float top = -INFINITY, total = 0.f;
+        for (int i0 = share; i0 < chain.count; i0 += AHEAD * S) {
+            float m[AHEAD], l[AHEAD];
+            f32x4 v[AHEAD];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, v[e], sum[e]);
+            for (int j = 0; j < AHEAD; ++j) {
+                const int i = i0 + j * S, part = chain.first + min(i, chain.count - 1) * chain.tiles;
+                m[j] = parts.sums(part, n)[0];
+                l[j] = i < chain.count ? parts.sums(part, n)[1] : 0.f;
+                v[j] = *reinterpret_cast<const f32x4 *>(parts.values(part, n) + 4 * lane);
+            }
+            float higher = top;
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) higher = fmaxf(higher, m[j]);
+            const float use = higher == -INFINITY ? 0.f : higher, alpha = fast_exp2(top - use);
+            top = higher;
+            total *= alpha;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] *= alpha;
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                const float weight = i0 + j * S < chain.count ? fast_exp2(m[j] - use) : 0.f;
+                total += weight * l[j];
+                if (i0 + j * S < chain.count)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, v[j][e], sum[e]);
+            }
         }
         if (S > 1) {
             __syncthreads();
             acc[grp][lane] = sum;
-            if (lane == 0) totals[grp] = total;
+            if (lane == 0) tops[grp] = top, totals[grp] = total;
             __syncthreads();
+            const int first = grp / S * S;
+            for (int i = 0; i < S; ++i) top = fmaxf(top, tops[first + i]);
+            const float use = top == -INFINITY ? 0.f : top;
             total = 0.f;
             sum = f32x4{0.f, 0.f, 0.f, 0.f};
             for (int i = 0; i < S; ++i) {
-                const f32x4 v = acc[grp / S * S + i][lane];
-                total += totals[grp / S * S + i];
+                const f32x4 v = acc[first + i][lane];
+                const float weight = fast_exp2(tops[first + i] - use);
+                total += weight * totals[first + i];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[e] += v[e];
+                for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, v[e], sum[e]);
             }
         }
         if (share != 0 || n0 + grp / S >= n_q) continue;
@@ -66,20 +82,26 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float
     }
 }
 
-// The form of a launch, from what the host knows: rows, sequences and a bound on their lengths, not the lengths
+// The form of a launch, from what the host knows: rows, sequences and a bound on their lengths, not the lengths.
+//   * bf16, more than 16 rows to a head of keys of an average sequence: wide.  24 sequences of 1 to 8192 tokens, 32 heads, 8 of keys, d = 128: 2 drafted tokens (8 rows)
+//     37.7 us, narrow 33.6; 4 39.8 and 35.3; 8 37.3 and 49.5; 32 53 and 93; 48 sequences of 2048 to 6500 with 64: 268 and 1736.  Float is always narrow.
+//   * Parts: as many as are resident at once (wide: two workgroups a compute unit), of 512 keys at least.  One sequence of 30,000 tokens, 16 drafted: 39.5 us, with half
+//     as many again 52; d = 64, 24 sequences with 8: 18.6, parts of 768 keys 21, of 1024 24.
+//   * Lengths up to 512, or many tiles of up to 64 sequences (which then start with the longest): a tile each and no joining launch.  48 x 64 drafted tokens, 768 tiles: 268,
+//     in parts 310.
 TreePlan pick(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem_bytes)
 {
-    const int G = H / H_kv;
-    TreePlan p{elem_bytes == 2 && rows * G > (int64_t)16 * B, 128, 0, 0};
-    if (!p.wide) p.rows = rows * G > (int64_t)16 * B ? 32 : 16;
-    const int64_t tiles = (rows * G / p.rows + std::min<int64_t>(rows, B)) * H_kv;
-    if (p.wide) {
-        p.target = 1024;
-        if (tiles < 768 && max_len > 512) p.slots = (int)(p.target + tiles);
-    } else {
-        p.target = 1024;
-        if (max_len > 512) p.slots = (int)(p.target + tiles);
-    }
+    const int64_t in_a_head = rows * (H / H_kv);
+    const bool some = in_a_head > (int64_t)16 * B, wide = elem_bytes == 2 && some;
+    TreePlan p;
+    p.wide = wide;
+    p.rows = wide ? 128 : some ? 32 : 16;
+    p.target = wide ? 512 : 256 * tree_per_cu(elem_bytes, d, p.rows / 16);
+    p.least = wide ? 8 : 2;
+    p.tiles = (int)((in_a_head / p.rows + std::min<int64_t>(rows, B)) * H_kv);
+    p.slots = 0;
+    if (max_len > 512 && !(wide && p.tiles >= 768 && B <= 64)) p.slots = p.target + p.tiles;
+    else p.least = 1 << 30;
     return p;
 }
 
@@ -88,7 +110,7 @@ TreePlan pick(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem
 size_t paged_tree_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem_bytes)
 {
     const TreePlan p = pick(rows, B, H, H_kv, d, max_len, elem_bytes);
-    return p.slots ? tree_scratch_bytes(p.rows, d, p.slots) : 0;
+    return p.slots ? tree_scratch_bytes(p.rows, d, p.slots, p.tiles) : 0;
 }
 
 template <typename T>
@@ -104,9 +126,9 @@ hipError_t launch_paged_tree(const TreeArgs &a, const T *q, const T *k_cache, co
     }
     if (e != hipSuccess || p.slots == 0) return e;
     TimedLaunch tl(K_TREE_MERGE, st);
-    const dim3 grid((unsigned)p.slots, (unsigned)std::max(1, p.rows * a.d / 4096)), block(256);
-    if (a.d == 64) hipLaunchKernelGGL((tree_merge_kernel<T, 64>), grid, block, 0, st, a, scratch, p.rows, p.slots, out, lse);
-    else hipLaunchKernelGGL((tree_merge_kernel<T, 128>), grid, block, 0, st, a, scratch, p.rows, p.slots, out, lse);
+    const dim3 grid((unsigned)p.tiles, (unsigned)std::min(p.rows, 32)), block(256);
+    if (a.d == 64) hipLaunchKernelGGL((tree_merge_kernel<T, 64>), grid, block, 0, st, a, scratch, p.rows, p.slots, p.tiles, out, lse);
+    else hipLaunchKernelGGL((tree_merge_kernel<T, 128>), grid, block, 0, st, a, scratch, p.rows, p.slots, p.tiles, out, lse);
     return hipGetLastError();
 }
 
