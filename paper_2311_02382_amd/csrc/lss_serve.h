@@ -252,8 +252,8 @@ __device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, i
         S += more < 1 ? 1 : more < S ? (int)more : S;
     }
     all *= a.H_kv;
-    if (all > slots) return p.items = 0, false;         // (cu does not ascend)
-    p.items = all_tiles * a.H_kv;
+    p.items = all > slots ? 0 : all_tiles * a.H_kv;     // (more than there can be: cu does not ascend)
+    if (p.items == 0) return false;
     const int64_t per_xcd = (all + 7) / 8, at = id % 8 * per_xcd + id / 8;
     if (id / 8 >= per_xcd || at >= all) return false;
     const int64_t nth = divide(at, a.H_kv);             // (some sequence has it)
