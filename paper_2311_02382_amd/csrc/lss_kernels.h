@@ -112,7 +112,7 @@ enum KernelId { K_FWD_F32 = 0, K_FWD_MERGE, K_ROWDOT, K_BWD_MAIN_F32, K_DQ_MERGE
                 K_PE_FWD, K_PE_BWD, K_LN_FWD, K_LN_BWD, K_LN_PARAMS, K_GELU_FWD, K_GELU_BWD, K_LINEAR_FWD, K_LINEAR_BWD, K_RESIDUAL, K_LINEAR_WGRAD,
                 K_FWD_BF16, K_BWD_PREP_BF16, K_BWD_SKINNY_BF16, K_LN_BWD_SHORT, K_PROJ_FWD_SMALL, K_PROJ_BWD_SMALL, K_LINEAR_FWD_SMALL,
                 K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_BF16, K_PACKED_F32, K_PACKED_MERGE, K_PAGED_TREE, K_FORK_CLEAR,
-                K_FORK_TABLE, K_FORK_PLAN, K_FORK_COPY, K_PAGED_COMPACT, K_BEAM_ROWS, K_BEAM_SELECT, K_TREE_BF16, K_TREE_MERGE, K_COUNT };
+                K_FORK_TABLE, K_FORK_PLAN, K_FORK_COPY, K_PAGED_COMPACT, K_BEAM_ROWS, K_BEAM_SELECT, K_TREE_BF16, K_TREE_MERGE, K_FORK_SMALL, K_COUNT };
 void timing_begin(int id, hipStream_t st);
 void timing_end(int id, hipStream_t st);
 struct TimedLaunch {    // RAII bracket around one kernel launch

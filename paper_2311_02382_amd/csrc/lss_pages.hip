@@ -14,6 +14,7 @@ namespace lss {
 namespace {
 
 constexpr int kNobody = INT_MAX, kReader = -1, kPlanThreads = 1024, kPerThread = 16;
+constexpr int kSmallSequences = 256, kSmallPages = 4096, kSmallEntries = 16384;        // what one workgroup goes over at once
 
 // what sequence s of the result has from its parent, and what it will need
 struct Heir {
@@ -41,6 +42,17 @@ __device__ __forceinline__ int page_at(const ForkArgs &a, int parent, int nth)  
     return (uint32_t)page < (uint32_t)a.pt.n_pages ? page : -1;
 }
 
+// What a sequence does to its partly filled page: the page if it is to write into it, else -1; and the pages that it takes besides one to move out of that into
+struct Wish {
+    int tail, taken;
+    int64_t past;           // pages that its table has no entry for
+};
+__device__ __forceinline__ Wish wish_of(const ForkArgs &a, const Heir &h)
+{
+    const int tail = h.part > 0 && h.room > 0 ? page_at(a, h.parent, h.full) : -1;
+    return {tail, max(0, h.table_pages - pages_before(h)), h.wanted - h.table_pages};
+}
+
 __global__ __launch_bounds__(256) void fork_clear_kernel(ForkArgs a, int32_t *__restrict__ owner)
 {
     const int i = blockIdx.x * 256 + threadIdx.x;
@@ -48,11 +60,16 @@ __global__ __launch_bounds__(256) void fork_clear_kernel(ForkArgs a, int32_t *__
 }
 
 // The entries of sequence blockIdx.x's table, 256 at a time
-__global__ __launch_bounds__(256) void fork_table_kernel(ForkArgs a, int32_t *__restrict__ owner, int32_t *__restrict__ table_out, int32_t *__restrict__ lengths_out)
+__global__ __launch_bounds__(256) void fork_table_kernel(ForkArgs a, int32_t *__restrict__ owner, int4 *__restrict__ wishes, int32_t *__restrict__ table_out,
+                                                         int32_t *__restrict__ lengths_out)
 {
     const int s = blockIdx.x;
     const Heir h = heir_of(a, s);
-    if (blockIdx.y == 0 && threadIdx.x == 0) lengths_out[s] = (int)min((int64_t)h.length + h.room, (int64_t)a.pt.max_pages << a.pt.page_shift);
+    if (blockIdx.y == 0 && threadIdx.x == 0) {
+        lengths_out[s] = (int)min((int64_t)h.length + h.room, (int64_t)a.pt.max_pages << a.pt.page_shift);
+        const Wish w = wish_of(a, h);
+        wishes[s] = {w.tail, w.taken, (int)w.past, 0};       // (2^31 tokens are 2^27 pages)
+    }
     for (int nth = blockIdx.y * 256 + threadIdx.x; nth < a.pt.max_pages; nth += gridDim.y * 256) {
         const int page = nth < pages_before(h) ? page_at(a, h.parent, nth) : -1;
         if (page >= 0) {
@@ -63,29 +80,17 @@ __global__ __launch_bounds__(256) void fork_table_kernel(ForkArgs a, int32_t *__
     }
 }
 
-// does the sequence move out of its partly filled page, and how many pages does it take
-__device__ __forceinline__ bool moves_out(const ForkArgs &a, const Heir &h, int s, const int32_t *owner)
-{
-    if (h.part == 0 || h.room == 0) return false;
-    const int page = page_at(a, h.parent, h.full);
-    return page >= 0 && owner[page] != s;
-}
-__device__ __forceinline__ int takes(const Heir &h, bool moves) { return moves + max(0, h.table_pages - pages_before(h)); }
-
-// inclusive sums over the workgroup
+// inclusive sums over a workgroup of kPlanThreads, and of all
 __device__ __forceinline__ int64_t group_scan(int64_t x, int64_t *waves, int64_t &all)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int sh = 1; sh < 64; sh *= 2) {
-        const int64_t y = __shfl_up(x, sh);
-        if (lane >= sh) x += y;
-    }
+    x = lanes_upto(x);
     __syncthreads();
     if (lane == 63) waves[wave] = x;
     __syncthreads();
     int64_t before = 0;
     all = 0;
+#pragma unroll
     for (int w = 0; w < kPlanThreads / 64; ++w) {
         if (w < wave) before += waves[w];
         all += waves[w];
@@ -93,39 +98,33 @@ __device__ __forceinline__ int64_t group_scan(int64_t x, int64_t *waves, int64_t
     return x + before;
 }
 
-// One workgroup: what each sequence takes, the list of the lowest free pages, as many as are taken; `first`[s]: a sequence's first one in it, ~ where it moves out
-__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkArgs a, const int32_t *__restrict__ owner, int32_t *__restrict__ first,
-                                                                 int32_t *__restrict__ free_pages, int32_t *__restrict__ n_free, int32_t *__restrict__ missing)
+// By one workgroup: of each sequence its first page in the list of the lowest free ones, ~ where it moves out of its partly filled one; that list, as long as is taken.
+// wish(s), owner(page): of sequence s, of a page
+template <typename WishOf, typename OwnerOf>
+__device__ __forceinline__ void plan(const ForkArgs &a, int64_t *waves, WishOf &&wish, OwnerOf &&owner, int32_t *first, int32_t *free_pages, int32_t *n_free, int32_t *missing)
 {
-    __shared__ int64_t waves[kPlanThreads / 64];
     const int tid = threadIdx.x;
-    int64_t need = 0, beyond = 0, all;
+    int64_t need = 0, past = 0, all;
     for (int s0 = 0; s0 < a.B_out; s0 += kPlanThreads) {
         const int s = s0 + tid;
-        int64_t mine = 0, past = 0;
-        bool moves = false;
-        if (s < a.B_out) {
-            const Heir h = heir_of(a, s);
-            moves = moves_out(a, h, s, owner);
-            mine = takes(h, moves);
-            past = h.wanted - h.table_pages;
-        }
-        const int64_t upto = group_scan(mine, waves, all);
+        Wish w{-1, 0, 0};
+        if (s < a.B_out) w = wish(s);
+        const bool moves = w.tail >= 0 && owner(w.tail) != s;
+        const int64_t mine = (int64_t)moves + w.taken, upto = group_scan(mine, waves, all);
         // (a place in the list of free pages past its end is as good as any other)
         const int at = (int)min(need + upto - mine, (int64_t)a.pt.n_pages);
         if (s < a.B_out) first[s] = moves ? ~at : at;
         need += all;
-        group_scan(past, waves, all);
-        beyond += all;
+        past += w.past;
     }
+    group_scan(past, waves, past);
     const int wanted = (int)min(need, (int64_t)a.pt.n_pages);
     int found = 0;
     for (int p0 = 0; p0 < a.pt.n_pages && found < wanted; p0 += kPlanThreads * kPerThread) {
         const int p = p0 + tid * kPerThread;
         uint32_t mine = 0;
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i)
-            if (p + i < a.pt.n_pages && owner[p + i] == kNobody) mine |= 1u << i;
+        for (int i = 0; i < kPerThread; ++i) mine |= (uint32_t)(p + i < a.pt.n_pages && owner(min(p + i, a.pt.n_pages - 1)) == kNobody) << i;
         int at = found + (int)group_scan(__popc(mine), waves, all) - __popc(mine);
         for (; mine != 0 && at < wanted; mine &= mine - 1, ++at) free_pages[at] = p + __ffs(mine) - 1;
         found += (int)all;
@@ -133,8 +132,50 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkArgs a, con
     found = min(found, wanted);
     if (tid == 0) {
         *n_free = found;
-        *missing = (int)min(need - found + beyond, (int64_t)INT_MAX);
+        *missing = (int)min(need - found + past, (int64_t)INT_MAX);
     }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkArgs a, const int32_t *__restrict__ owner, const int4 *__restrict__ wishes, int32_t *__restrict__ first,
+                                                                 int32_t *__restrict__ free_pages, int32_t *__restrict__ n_free, int32_t *__restrict__ missing)
+{
+    __shared__ int64_t waves[kPlanThreads / 64];
+    const auto wish = [&](int s) {
+        const int4 w = wishes[s];
+        return Wish{w.x, w.y, w.z};
+    };
+    plan(a, waves, wish, [&](int page) { return owner[page]; }, first, free_pages, n_free, missing);
+}
+
+// Few sequences, short tables and few pages: the three launches above by one workgroup, who has what in LDS
+__global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(ForkArgs a, int32_t *__restrict__ first, int32_t *__restrict__ free_pages, int32_t *__restrict__ n_free,
+                                                                  int32_t *__restrict__ missing, int32_t *__restrict__ table_out, int32_t *__restrict__ lengths_out)
+{
+    __shared__ int64_t waves[kPlanThreads / 64];
+    __shared__ int owner[kSmallPages];
+    __shared__ Heir heirs[kSmallSequences];
+    const int tid = threadIdx.x;
+    Heir mine{};
+    Wish w{-1, 0, 0};
+    if (tid < a.B_out) mine = heir_of(a, tid);
+    for (int i = tid; i < a.pt.n_pages; i += kPlanThreads) owner[i] = a.held && a.held[i] ? kReader : kNobody;
+    if (tid < a.B_out) {
+        heirs[tid] = mine;
+        w = wish_of(a, mine);
+        lengths_out[tid] = (int)min((int64_t)mine.length + mine.room, (int64_t)a.pt.max_pages << a.pt.page_shift);
+    }
+    __syncthreads();
+    const int entries = a.B_out * a.pt.max_pages;
+#pragma unroll 4
+    for (int i = tid; i < entries; i += kPlanThreads) {
+        const int s = i / a.pt.max_pages, nth = i - s * a.pt.max_pages;
+        const Heir &h = heirs[s];
+        const int page = nth < pages_before(h) ? page_at(a, h.parent, nth) : -1;
+        if (page >= 0) atomicMin(owner + page, nth == h.full && h.room > 0 ? s : kReader);
+        table_out[i] = page;
+    }
+    __syncthreads();
+    plan(a, waves, [&](int) { return w; }, [&](int page) { return owner[page]; }, first, free_pages, n_free, missing);
 }
 
 // Sequence blockIdx.x: its new pages into its table (blockIdx.y = 0), what its partly filled page holds into a new one (all of them)
@@ -146,7 +187,7 @@ __global__ __launch_bounds__(256) void fork_copy_kernel(ForkArgs a, const int32_
     const int s = blockIdx.x, found = *n_free;
     const Heir h = heir_of(a, s);
     const bool moves = first[s] < 0;
-    const int at = moves ? ~first[s] : first[s], n = takes(h, moves), begin = pages_before(h) - moves;
+    const int at = moves ? ~first[s] : first[s], begin = pages_before(h) - moves, n = moves + max(0, h.table_pages - pages_before(h));
     if (blockIdx.y == 0)
         for (int i = threadIdx.x; i < n; i += 256)
             table_out[(int64_t)s * a.pt.max_pages + begin + i] = at + i < found ? free_pages[at + i] : -1;
@@ -209,25 +250,29 @@ __global__ __launch_bounds__(256) void paged_compact_kernel(CompactArgs a, int r
 
 } // namespace
 
-size_t paged_fork_workspace_bytes(int64_t n_pages, int64_t B_out) { return sizeof(int32_t) * (size_t)(2 * n_pages + B_out + 4); }
+size_t paged_fork_workspace_bytes(int64_t n_pages, int64_t B_out) { return sizeof(int32_t) * (size_t)(4 * B_out + 2 * n_pages + B_out + 4); }
 
 hipError_t launch_paged_fork(const ForkArgs &a, int row_bytes, void *k_cache, void *v_cache, int32_t *scratch, int32_t *table_out, int32_t *lengths_out, int32_t *missing,
                              hipStream_t st)
 {
     // (a launch has fewer than 2^32 threads)
     const auto shared = [&](int64_t workgroups) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(workgroups, ((int64_t)1 << 22) / std::max(a.B_out, 1))); };
-    int32_t *const owner = scratch, *const free_pages = owner + a.pt.n_pages, *const first = free_pages + a.pt.n_pages, *const n_free = first + a.B_out;
-    {
-        TimedLaunch tl(K_FORK_CLEAR, st);
-        hipLaunchKernelGGL(fork_clear_kernel, dim3((unsigned)((a.pt.n_pages + 255ll) / 256)), dim3(256), 0, st, a, owner);
-    }
-    if (a.B_out > 0) {
-        TimedLaunch tl(K_FORK_TABLE, st);
-        hipLaunchKernelGGL(fork_table_kernel, dim3((unsigned)a.B_out, shared((a.pt.max_pages + 255) / 256)), dim3(256), 0, st, a, owner, table_out, lengths_out);
-    }
-    {
+    int4 *const wishes = reinterpret_cast<int4 *>(scratch);
+    int32_t *const owner = scratch + 4 * (int64_t)a.B_out, *const free_pages = owner + a.pt.n_pages, *const first = free_pages + a.pt.n_pages, *const n_free = first + a.B_out;
+    if (a.B_out <= kSmallSequences && a.pt.n_pages <= kSmallPages && (int64_t)a.B_out * a.pt.max_pages <= kSmallEntries) {
+        TimedLaunch tl(K_FORK_SMALL, st);
+        hipLaunchKernelGGL(fork_small_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, first, free_pages, n_free, missing, table_out, lengths_out);
+    } else {
+        {
+            TimedLaunch tl(K_FORK_CLEAR, st);
+            hipLaunchKernelGGL(fork_clear_kernel, dim3((unsigned)((a.pt.n_pages + 255ll) / 256)), dim3(256), 0, st, a, owner);
+        }
+        if (a.B_out > 0) {
+            TimedLaunch tl(K_FORK_TABLE, st);
+            hipLaunchKernelGGL(fork_table_kernel, dim3((unsigned)a.B_out, shared((a.pt.max_pages + 255) / 256)), dim3(256), 0, st, a, owner, wishes, table_out, lengths_out);
+        }
         TimedLaunch tl(K_FORK_PLAN, st);
-        hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, owner, first, free_pages, n_free, missing);
+        hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, owner, wishes, first, free_pages, n_free, missing);
     }
     if (a.B_out > 0) {
         const int64_t bytes = 2 * ((int64_t)row_bytes << a.pt.page_shift);
