@@ -5,6 +5,7 @@
 //
 // Rows are cut into chunks, a wavefront each (beam_rows_kernel), so that few rows fill the chip; a second launch, a workgroup per prompt, joins a row's chunks and
 // its beams (beam_select_kernel).  Where rows are short (kDirect) the second kernel goes over them itself and there is no first one.
+#include "lss_device_once.h"
 #include "lss_serve.h"
 
 #include <algorithm>
@@ -131,10 +132,18 @@ struct Best {
     __device__ __forceinline__ Best(char *lds, int n_, int lane_)
         : list((LdsCandidate *)lds), held((__attribute__((address_space(3))) float *)(lds + kCap * sizeof(Candidate))), n(n_), lane(lane_) {}
     __device__ __forceinline__ int count() const { return bound.count; }
-    // of 64 values, one a lane, at least n of which are at or above the bound's, at least n are at or above what this returns
-    __device__ __forceinline__ uint32_t nth(uint32_t v) const
+    // of 64 R values, R a lane, at least n of which are at or above the bound's, at least n are at or above what this returns
+    template <int R> __device__ __forceinline__ uint32_t nth(const uint32_t (&v)[R]) const
     {
-        return at_least(bound.value, wave_max_of(v), n, n + n / 4, [&](uint32_t least) __attribute__((always_inline)) { return count_of(v >= least); });
+        uint32_t most = 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r) most = max(most, v[r]);
+        return at_least(bound.value, wave_max_of(most), n, n + n / 4, [&](uint32_t least) __attribute__((always_inline)) {
+            int c = 0;
+#pragma unroll
+            for (int r = 0; r < R; ++r) c += count_of(v[r] >= least);
+            return c;
+        });
     }
     __device__ __forceinline__ void raise(uint32_t v)
     {
@@ -213,14 +222,20 @@ __device__ __forceinline__ ChunkStats scan_row(const T *row, int64_t v0, int64_t
         for (int i = 0; i < kLoads; ++i) part[i & 1] += exp_of(x[i] - use);
         sum = sum * (double)exp_of(top - use) + (double)(part[0] + part[1]);
         top = higher;
-        // the bound from the lanes' largest: n of them are candidates themselves
-        if (count_of(most >= best.value_f) >= best.n) {
-            const uint32_t t = best.nth(ascending(most));
+        // the bound from the eights' largest: n of them are candidates themselves
+        int candidates = 0;
+#pragma unroll
+        for (int g = 0; g < kLoads / 8; ++g) candidates += count_of(of_eight[g] >= best.value_f);
+        if (candidates >= best.n) {
+            uint32_t largest[kLoads / 8];
+#pragma unroll
+            for (int g = 0; g < kLoads / 8; ++g) largest[g] = ascending(of_eight[g]);
+            const uint32_t t = best.nth(largest);
             if (t > best.bound.value) best.raise(t);
         }
         // Few eights of a lane's logits have a candidate: they go through LDS, up to 64 of them at a time, to all lanes.  (Slot by slot, 32 tests and an offer for each
         // candidate: 8 of 23 us for 256 rows of 128,256; lane by lane 6.5.)
-        if (!__any(most >= best.value_f)) continue;
+        if (candidates == 0) continue;
         int n = 0;
         const auto offer_held = [&] __attribute__((always_inline)) {
             wave_sync();
@@ -334,15 +349,16 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
                 if (i0 > 0)
 #pragma unroll
                     for (int i = 0; i < kAtOnce; ++i) c[i] = list[min(i0 + i * 64 + lane, n_list - 1)];
-                uint32_t most = 0;
+                uint32_t values[kAtOnce];
+                int candidates = 0;
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) {
-                    if (i0 + i * 64 + lane >= n_list) c[i].value = 0u;
-                    most = max(most, c[i].value);
+                    values[i] = i0 + i * 64 + lane < n_list ? c[i].value : 0u;
+                    candidates += count_of(values[i] > best.bound.value);
                 }
-                if (count_of(most > best.bound.value) >= a.N) best.raise(max(best.bound.value, best.nth(most)));
+                if (candidates >= a.N) best.raise(max(best.bound.value, best.nth(values)));
 #pragma unroll
-                for (int i = 0; i < kAtOnce; ++i) best.offer(c[i].value, c[i].index);
+                for (int i = 0; i < kAtOnce; ++i) best.offer(values[i], c[i].index);
             }
         }
         best.cut(per_beam);
@@ -359,17 +375,19 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
     }
     __syncthreads();
     const int n = n_candidates;
-    uint32_t bound = 0;                                 // of the totals in 32 bits, as ascending whole numbers: n_out are at or above it
-    if (n > 256)
-        for (int bit = 31; bit >= 0; --bit) {
+    // a bound of the totals in 32 bits, as ascending whole numbers: n_out are at or above it
+    uint32_t bound = 0;
+    if (n > 256) {
+        int step = 0;
+        bound = at_least(0, ascending(3.402823466e38f), a.N, 256, [&](uint32_t least) {
             int mine = 0;
-            for (int i = tid; i < n; i += blockDim.x) mine += ascending((float)total[i]) >= (bound | 1u << bit);
-#pragma unroll
-            for (int sh = 32; sh >= 1; sh >>= 1) mine += __shfl_xor(mine, sh);
-            if (lane == 0) atomicAdd(&above[bit], mine);
+            for (int i = tid; i < n; i += blockDim.x) mine += ascending((float)total[i]) >= least;
+            mine = lane_sum_scan(mine);
+            if (lane == 63) atomicAdd(&above[step], mine);
             __syncthreads();
-            if (above[bit] >= a.N) bound |= 1u << bit;
-        }
+            return __builtin_amdgcn_readfirstlane(above[step++]);       // (32 steps at most)
+        });
+    }
     const auto put = [&](int better, double x, uint32_t place) {
         if (better >= a.N) return;
         const int k = (int)(place / (uint32_t)a.V), token = (int)(place - (uint32_t)k * a.V);
@@ -434,13 +452,15 @@ BeamArgs chunked(int64_t stride, int B, int K, int V, int N, int end_token)
     a.chunks = (int)((batches + each - 1) / each);
     return a;
 }
+// (32 beams of 206 logits, 64 prompts: two rows by each wavefront one after the other would take longer than a launch)
+bool is_direct(int K, int V) { return V <= kDirect && K <= 16; }
 size_t lists_bytes(const BeamArgs &a) { return ((size_t)a.B * a.K * a.chunks * a.kept * sizeof(Candidate) + 15) & ~(size_t)15; }
 
 } // namespace
 
 size_t beam_select_workspace_bytes(int B, int K, int V, int N)
 {
-    if (V <= kDirect) return 0;
+    if (is_direct(K, V)) return 0;
     const BeamArgs a = chunked(0, B, K, V, N, 0);
     return lists_bytes(a) + (size_t)B * K * a.chunks * sizeof(ChunkStats);
 }
@@ -451,11 +471,22 @@ hipError_t launch_beam_select(const T *logits, int64_t stride, const float *scor
 {
     const BeamArgs a = chunked(stride, B, K, V, N, end_token);
     Candidate *const lists = static_cast<Candidate *>(workspace);
-    ChunkStats *const stats = reinterpret_cast<ChunkStats *>(static_cast<char *>(workspace) + (V <= kDirect ? 0 : lists_bytes(a)));
-    // (64 KB of LDS: 12 bytes a candidate, of 4096 at most, and 5 KB a wavefront)
-    const int per_beam = K * N <= 2048 ? 2 * N : N, waves = std::min({K, 16, (65536 - 1024 - 12 * K * per_beam) / kWaveLds});
+    ChunkStats *const stats = reinterpret_cast<ChunkStats *>(static_cast<char *>(workspace) + (is_direct(K, V) ? 0 : lists_bytes(a)));
+    // (12 bytes of LDS a candidate, of 4096 at most, and 5 KB a wavefront: more than the 64 KB that a launch may have without asking)
+    const int per_beam = K * N <= 1024 ? 2 * N : N, waves = std::min(K, 16);
     const size_t lds = (((size_t)K * per_beam * 12 + 15) & ~(size_t)15) + (size_t)waves * kWaveLds;
-    if (V <= kDirect) {
+    if (lds > 65536 - 1024) {
+        static DeviceOnce once;
+        int dev = 0;
+        if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
+        const hipError_t e = once.run(dev, [] {
+            for (const void *kernel : {reinterpret_cast<const void *>(beam_select_kernel<T, true>), reinterpret_cast<const void *>(beam_select_kernel<T, false>)})
+                if (hipError_t err = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 4096 * 12 + 16 * kWaveLds); err != hipSuccess) return err;
+            return hipSuccess;
+        });
+        if (e != hipSuccess) return e;
+    }
+    if (is_direct(K, V)) {
         TimedLaunch tl(K_BEAM_SELECT, st);
         hipLaunchKernelGGL((beam_select_kernel<T, true>), dim3((unsigned)B), dim3(64 * waves), lds, st, a, logits, scores, finished, lists, stats, per_beam, scores_out,
                            parents, tokens, finished_out);

@@ -98,6 +98,6 @@ def test_scratch(lib):
                 (64, 4, 32, 8, 128, -1, 2), (64, 4, 32, 8, 128, 4096, 3), (1 << 20, 4, 32, 8, 128, 4096, 2)):
         assert tree(*bad) == 0
     assert fork(100, 7) >= 4 * (2 * 100 + 7) and fork(0, 7) == 0 and fork(100, -1) == 0
-    assert select(2, 3, 100, 4) == 0 and select(2, 3, 50000, 4) > 0
+    assert select(2, 3, 100, 4) == 0 and select(2, 3, 50000, 4) > 0 and select(2, 17, 100, 4) > 0
     for bad in ((0, 3, 50000, 4), (2, 0, 50000, 4), (2, 65, 50000, 4), (2, 3, 50000, 65)):
         assert select(*bad) == 0
