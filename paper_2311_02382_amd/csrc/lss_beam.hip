@@ -21,7 +21,8 @@ constexpr int kDirect = 2 * kBatch;
 constexpr int kHeld = 12;           // floats of eight logits in LDS, behind which stands whose they are; neighbours in other banks
 constexpr int kWaveLds = kCap * 8 + 64 * kHeld * 4;     // a wavefront's: its list, and 64 of those
 constexpr int kAtOnce = 6;          // candidates of a row that a lane of the second launch looks at at once
-constexpr int kRanked = 320;        // candidates that the wavefronts of a workgroup compare with the others together; room for them in one wavefront's list
+constexpr int kUnbounded = 128;     // totals of a prompt's candidates that are ranked as they are; of more those at or above a bound
+constexpr int kRanked = 320;        // of those, at most, that are compared with one another only; room for them in one wavefront's list
 
 struct Candidate { uint32_t value, index; };            // value: a float as an ascending whole number; 0: none
 struct ChunkStats { double sum; float top, unused; };   // sum of exp(x - top)
@@ -377,9 +378,9 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
     const int n = n_candidates;
     // a bound of the totals in 32 bits, as ascending whole numbers: n_out are at or above it
     uint32_t bound = 0;
-    if (n > 256) {
+    if (n > kUnbounded) {
         int step = 0;
-        bound = at_least(0, ascending(3.402823466e38f), a.N, 256, [&](uint32_t least) {
+        bound = at_least(0, ascending(3.402823466e38f), a.N, max(kUnbounded / 2, 2 * a.N), [&](uint32_t least) {
             int mine = 0;
             for (int i = tid; i < n; i += blockDim.x) mine += ascending((float)total[i]) >= least;
             mine = lane_sum_scan(mine);
@@ -397,42 +398,43 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
         tokens[to] = token;
         if (finished_out) finished_out[to] = token == a.end_token;          // (what a beam that has ended goes on with, too)
     };
-    const auto better_than = [&](double x, uint32_t place, int from, int to) {
+    const auto better_than = [&](const double *totals, const uint32_t *places, double x, uint32_t place, int from, int to) __attribute__((always_inline)) {
         int better = 0;
 #pragma unroll 8
         for (int j = from; j < to; ++j) {               // (no branch: reads ahead of one another)
-            const double y = total[j];
-            const uint32_t at = flat[j];
+            const double y = totals[j];
+            const uint32_t at = places[j];
             better += (int)(y > x) | ((int)(y == x) & (int)(at < place));
         }
         return better;
     };
-    // (the lists are done with: which candidates are at or above the bound, and how many are better than each)
-    int *const better = reinterpret_cast<int *>(lds);
-    uint16_t *const who = reinterpret_cast<uint16_t *>(better + kRanked);
-    for (int i = tid; i < min(n, kRanked); i += blockDim.x) better[i] = 0;
-    for (int i = tid; i < n; i += blockDim.x)
-        if (n <= 256) who[i] = (uint16_t)i;
-        else if (ascending((float)total[i]) >= bound) {
-            const int at = atomicAdd(&n_above, 1);
-            if (at < kRanked) who[at] = (uint16_t)i;
-        }
+    // (The lists are done with: there go those at or above the bound, and how many are better than each.  Whoever is better than one of them is one of them.)
+    double *const high = reinterpret_cast<double *>(lds);
+    uint32_t *const high_flat = reinterpret_cast<uint32_t *>(high + kRanked);
+    int *const better = reinterpret_cast<int *>(high_flat + kRanked);
+    static_assert(kRanked * 16 <= kWaveLds, "");
+    for (int i = tid; i < n; i += blockDim.x) {
+        const double x = total[i];
+        if (ascending((float)x) < bound) continue;
+        const int at = n <= kUnbounded ? i : atomicAdd(&n_above, 1);
+        if (at < kRanked) high[at] = x, high_flat[at] = flat[i], better[at] = 0;
+    }
     __syncthreads();
-    const int m = n <= 256 ? n : n_above;
+    const int m = n <= kUnbounded ? n : n_above;
     if (m <= kRanked) {
         // the others are shared out among as many groups of wavefronts as there are
-        const int in_a_group = (m + 63) & ~63, groups = max(1, (int)blockDim.x / max(in_a_group, 1)), each = (n + groups - 1) / groups;
+        const int in_a_group = (m + 63) & ~63, groups = max(1, (int)blockDim.x / max(in_a_group, 1)), each = (m + groups - 1) / groups;
         for (int s = tid; s < in_a_group * groups; s += blockDim.x) {
             const int i = s % in_a_group, group = s / in_a_group;
             if (i >= m) continue;
-            const int count = better_than(total[who[i]], flat[who[i]], min(n, group * each), min(n, (group + 1) * each));
+            const int count = better_than(high, high_flat, high[i], high_flat[i], min(m, group * each), min(m, (group + 1) * each));
             if (count > 0) atomicAdd(&better[i], count);
         }
         __syncthreads();
-        for (int i = tid; i < m; i += blockDim.x) put(better[i], total[who[i]], flat[who[i]]);
+        for (int i = tid; i < m; i += blockDim.x) put(better[i], high[i], high_flat[i]);
     } else {
         // (more than that alike)
-        for (int i = tid; i < n; i += blockDim.x) put(better_than(total[i], flat[i], 0, n), total[i], flat[i]);
+        for (int i = tid; i < n; i += blockDim.x) put(better_than(total, flat, total[i], flat[i], 0, n), total[i], flat[i]);
     }
     for (int i = n + tid; i < a.N; i += blockDim.x) {
         const int64_t to = (int64_t)b * a.N + i;
@@ -442,11 +444,12 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
     }
 }
 
-// Chunks of a row: a batch at least, and as many as it takes to have 4096 wavefronts
+// Chunks of a row: a batch at least, and as many as it takes to have 4096 wavefronts, but no more than 16384 candidates for the workgroup that joins them (32 beams of
+// 128,256 logits, 64 from each, one prompt: 74 us, 87 without that; 16 of 50,000, 32 from each: 24.4, with 4096 candidates 30.7).
 BeamArgs chunked(int64_t stride, int B, int K, int V, int N, int end_token)
 {
     BeamArgs a{stride, B, K, V, N, end_token, 0, std::min(N + N / 4 + 4, 64), 0};
-    const int64_t batches = ((int64_t)V + kBatch - 1) / kBatch, wanted = std::max<int64_t>(1, 4096 / ((int64_t)B * K));
+    const int64_t batches = ((int64_t)V + kBatch - 1) / kBatch, wanted = std::max<int64_t>(1, std::min<int64_t>(4096 / ((int64_t)B * K), 16384 / (K * a.kept)));
     const int64_t each = (batches + wanted - 1) / wanted;
     a.chunk = each * kBatch;
     a.chunks = (int)((batches + each - 1) / each);

@@ -67,6 +67,17 @@ def test_equal_logits_go_to_the_lower_token(dtype, V):
     assert _check(signs, torch.zeros(1, 1), 4)[2].tolist() == [[3, 5, V - 1, 0]]
 
 
+@pytest.mark.parametrize("V", [130, 9000])
+@pytest.mark.parametrize("K", [8, 20, 64])
+def test_more_alike_than_are_wanted(K, V):
+    # all beams alike: the lowest beam's lowest tokens; totals that 32 bits cannot tell apart: the best of them all the same
+    alike = torch.zeros(K, V)
+    for n_out in (33, 64):
+        got = _check(alike, torch.full((1, K), -3.0), n_out)
+        assert got[2].tolist()[0] == list(range(n_out)) and set(got[1].tolist()[0]) == {0}
+    _check(torch.randn(K, V, generator=torch.Generator().manual_seed(65)).mul(0.25), torch.full((1, K), -1.0e9), 50)
+
+
 @pytest.mark.parametrize("dtype", sv.DTYPES)
 @pytest.mark.parametrize("V", [700, 12000])
 def test_ascending_and_descending_logits(dtype, V):
