@@ -20,6 +20,7 @@ constexpr int kCap = 256;           // candidates that a wavefront keeps before 
 constexpr int kDirect = 2 * kBatch;
 constexpr int kHeld = 12;           // floats of eight logits in LDS, behind which stands whose they are; neighbours in other banks
 constexpr int kWaveLds = kCap * 8 + 64 * kHeld * 4;     // a wavefront's: its list, and 64 of those
+constexpr int kFew = 16;            // lanes' largest suffice to find a bound that little more than so many reach
 constexpr int kAtOnce = 6;          // candidates of a row that a lane of the second launch looks at at once
 constexpr int kUnbounded = 128;     // totals of a prompt's candidates that are ranked as they are; of more those at or above a bound
 constexpr int kRanked = 320;        // of those, at most, that are compared with one another only; room for them in one wavefront's list
@@ -223,20 +224,24 @@ __device__ __forceinline__ ChunkStats scan_row(const T *row, int64_t v0, int64_t
         for (int i = 0; i < kLoads; ++i) part[i & 1] += exp_of(x[i] - use);
         sum = sum * (double)exp_of(top - use) + (double)(part[0] + part[1]);
         top = higher;
-        // the bound from the eights' largest: n of them are candidates themselves
-        int candidates = 0;
+        // the bound from the largest of the lanes, or where they would be too few of their eights: n of them are candidates themselves
+        if (best.n <= kFew) {
+            if (count_of(most >= best.value_f) >= best.n) best.raise(max(best.bound.value, best.nth<1>({ascending(most)})));
+        } else {
+            int candidates = 0;
 #pragma unroll
-        for (int g = 0; g < kLoads / 8; ++g) candidates += count_of(of_eight[g] >= best.value_f);
-        if (candidates >= best.n) {
-            uint32_t largest[kLoads / 8];
+            for (int g = 0; g < kLoads / 8; ++g) candidates += count_of(of_eight[g] >= best.value_f);
+            if (candidates >= best.n) {
+                uint32_t largest[kLoads / 8];
 #pragma unroll
-            for (int g = 0; g < kLoads / 8; ++g) largest[g] = ascending(of_eight[g]);
-            const uint32_t t = best.nth(largest);
-            if (t > best.bound.value) best.raise(t);
+                for (int g = 0; g < kLoads / 8; ++g) largest[g] = ascending(of_eight[g]);
+                const uint32_t t = best.nth(largest);
+                if (t > best.bound.value) best.raise(t);
+            }
         }
         // Few eights of a lane's logits have a candidate: they go through LDS, up to 64 of them at a time, to all lanes.  (Slot by slot, 32 tests and an offer for each
         // candidate: 8 of 23 us for 256 rows of 128,256; lane by lane 6.5.)
-        if (candidates == 0) continue;
+        if (!__any(most >= best.value_f)) continue;
         int n = 0;
         const auto offer_held = [&] __attribute__((always_inline)) {
             wave_sync();
@@ -350,14 +355,20 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
                 if (i0 > 0)
 #pragma unroll
                     for (int i = 0; i < kAtOnce; ++i) c[i] = list[min(i0 + i * 64 + lane, n_list - 1)];
-                uint32_t values[kAtOnce];
+                uint32_t values[kAtOnce], most = 0;
                 int candidates = 0;
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) {
                     values[i] = i0 + i * 64 + lane < n_list ? c[i].value : 0u;
-                    candidates += count_of(values[i] > best.bound.value);
+                    most = max(most, values[i]);
                 }
-                if (candidates >= a.N) best.raise(max(best.bound.value, best.nth(values)));
+                if (a.N <= kFew) {
+                    if (count_of(most > best.bound.value) >= a.N) best.raise(max(best.bound.value, best.nth<1>({most})));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kAtOnce; ++i) candidates += count_of(values[i] > best.bound.value);
+                    if (candidates >= a.N) best.raise(max(best.bound.value, best.nth(values)));
+                }
 #pragma unroll
                 for (int i = 0; i < kAtOnce; ++i) best.offer(values[i], c[i].index);
             }
@@ -409,15 +420,19 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
         return better;
     };
     // (The lists are done with: there go those at or above the bound, and how many are better than each.  Whoever is better than one of them is one of them.)
-    double *const high = reinterpret_cast<double *>(lds);
-    uint32_t *const high_flat = reinterpret_cast<uint32_t *>(high + kRanked);
-    int *const better = reinterpret_cast<int *>(high_flat + kRanked);
+    double *const high = n <= kUnbounded ? total : reinterpret_cast<double *>(lds);
+    uint32_t *const high_flat = n <= kUnbounded ? flat : reinterpret_cast<uint32_t *>(lds + 8 * kRanked);
+    int *const better = reinterpret_cast<int *>(lds + 12 * kRanked);
     static_assert(kRanked * 16 <= kWaveLds, "");
-    for (int i = tid; i < n; i += blockDim.x) {
-        const double x = total[i];
-        if (ascending((float)x) < bound) continue;
-        const int at = n <= kUnbounded ? i : atomicAdd(&n_above, 1);
-        if (at < kRanked) high[at] = x, high_flat[at] = flat[i], better[at] = 0;
+    if (n <= kUnbounded) {
+        for (int i = tid; i < n; i += blockDim.x) better[i] = 0;
+    } else {
+        for (int i = tid; i < n; i += blockDim.x) {
+            const double x = total[i];
+            if (ascending((float)x) < bound) continue;
+            const int at = atomicAdd(&n_above, 1);
+            if (at < kRanked) high[at] = x, high_flat[at] = flat[i], better[at] = 0;
+        }
     }
     __syncthreads();
     const int m = n <= kUnbounded ? n : n_above;
