@@ -43,14 +43,15 @@ __device__ __forceinline__ int page_at(const ForkArgs &a, int parent, int nth)  
 }
 
 // What a sequence does to its partly filled page: the page if it is to write into it, else -1; and the pages that it takes besides one to move out of that into
-struct Wish {
+struct alignas(16) Wish {
     int tail, taken;
-    int64_t past;           // pages that its table has no entry for
+    int past;               // pages that its table has no entry for (2^31 tokens are 2^27 pages)
+    int part, before;       // tokens in its partly filled page; pages that it has from its parent
 };
 __device__ __forceinline__ Wish wish_of(const ForkArgs &a, const Heir &h)
 {
     const int tail = h.part > 0 && h.room > 0 ? page_at(a, h.parent, h.full) : -1;
-    return {tail, max(0, h.table_pages - pages_before(h)), h.wanted - h.table_pages};
+    return {tail, max(0, h.table_pages - pages_before(h)), (int)(h.wanted - h.table_pages), h.part, pages_before(h)};
 }
 
 __global__ __launch_bounds__(256) void fork_clear_kernel(ForkArgs a, int32_t *__restrict__ owner)
@@ -60,23 +61,28 @@ __global__ __launch_bounds__(256) void fork_clear_kernel(ForkArgs a, int32_t *__
 }
 
 // The entries of sequence blockIdx.x's table, 256 at a time
-__global__ __launch_bounds__(256) void fork_table_kernel(ForkArgs a, int32_t *__restrict__ owner, int4 *__restrict__ wishes, int32_t *__restrict__ table_out,
+__global__ __launch_bounds__(256) void fork_table_kernel(ForkArgs a, int32_t *__restrict__ owner, Wish *__restrict__ wishes, int32_t *__restrict__ table_out,
                                                          int32_t *__restrict__ lengths_out)
 {
     const int s = blockIdx.x;
+    int nth = blockIdx.y * 256 + threadIdx.x;
+    // (an entry is on its way with the length that says whether it counts)
+    const int p = a.parents[s];
+    int entry = nth < a.pt.max_pages && (uint32_t)p < (uint32_t)a.B ? page_at(a, p, nth) : -1;
     const Heir h = heir_of(a, s);
-    if (blockIdx.y == 0 && threadIdx.x == 0) {
-        lengths_out[s] = (int)min((int64_t)h.length + h.room, (int64_t)a.pt.max_pages << a.pt.page_shift);
-        const Wish w = wish_of(a, h);
-        wishes[s] = {w.tail, w.taken, (int)w.past, 0};       // (2^31 tokens are 2^27 pages)
-    }
-    for (int nth = blockIdx.y * 256 + threadIdx.x; nth < a.pt.max_pages; nth += gridDim.y * 256) {
-        const int page = nth < pages_before(h) ? page_at(a, h.parent, nth) : -1;
+    while (nth < a.pt.max_pages) {
+        const int page = nth < pages_before(h) ? entry : -1;
         if (page >= 0) {
             if (nth == h.full && h.room > 0) atomicMin(owner + page, s);
             else __hip_atomic_store(owner + page, kReader, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
         table_out[(int64_t)s * a.pt.max_pages + nth] = page;
+        nth += gridDim.y * 256;
+        entry = nth < min(pages_before(h), a.pt.max_pages) ? page_at(a, h.parent, nth) : -1;
+    }
+    if (blockIdx.y == 0 && threadIdx.x == 0) {
+        lengths_out[s] = (int)min((int64_t)h.length + h.room, (int64_t)a.pt.max_pages << a.pt.page_shift);
+        wishes[s] = wish_of(a, h);
     }
 }
 
@@ -105,9 +111,15 @@ __device__ __forceinline__ void plan(const ForkArgs &a, int64_t *waves, WishOf &
 {
     const int tid = threadIdx.x;
     int64_t need = 0, past = 0, all;
+    int of_page[kPerThread];                            // the first kPlanThreads * kPerThread pages', on their way while the sequences are gone over
+    const auto load = [&](int p) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) of_page[i] = owner(min(p + i, a.pt.n_pages - 1));
+    };
+    load(tid * kPerThread);
     for (int s0 = 0; s0 < a.B_out; s0 += kPlanThreads) {
         const int s = s0 + tid;
-        Wish w{-1, 0, 0};
+        Wish w{-1, 0, 0, 0, 0};
         if (s < a.B_out) w = wish(s);
         const bool moves = w.tail >= 0 && owner(w.tail) != s;
         const int64_t mine = (int64_t)moves + w.taken, upto = group_scan(mine, waves, all);
@@ -123,8 +135,9 @@ __device__ __forceinline__ void plan(const ForkArgs &a, int64_t *waves, WishOf &
     for (int p0 = 0; p0 < a.pt.n_pages && found < wanted; p0 += kPlanThreads * kPerThread) {
         const int p = p0 + tid * kPerThread;
         uint32_t mine = 0;
+        if (p0 > 0) load(p);
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i) mine |= (uint32_t)(p + i < a.pt.n_pages && owner(min(p + i, a.pt.n_pages - 1)) == kNobody) << i;
+        for (int i = 0; i < kPerThread; ++i) mine |= (uint32_t)(p + i < a.pt.n_pages && of_page[i] == kNobody) << i;
         int at = found + (int)group_scan(__popc(mine), waves, all) - __popc(mine);
         for (; mine != 0 && at < wanted; mine &= mine - 1, ++at) free_pages[at] = p + __ffs(mine) - 1;
         found += (int)all;
@@ -136,19 +149,15 @@ __device__ __forceinline__ void plan(const ForkArgs &a, int64_t *waves, WishOf &
     }
 }
 
-__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkArgs a, const int32_t *__restrict__ owner, const int4 *__restrict__ wishes, int32_t *__restrict__ first,
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(ForkArgs a, const int32_t *__restrict__ owner, const Wish *__restrict__ wishes, int32_t *__restrict__ first,
                                                                  int32_t *__restrict__ free_pages, int32_t *__restrict__ n_free, int32_t *__restrict__ missing)
 {
     __shared__ int64_t waves[kPlanThreads / 64];
-    const auto wish = [&](int s) {
-        const int4 w = wishes[s];
-        return Wish{w.x, w.y, w.z};
-    };
-    plan(a, waves, wish, [&](int page) { return owner[page]; }, first, free_pages, n_free, missing);
+    plan(a, waves, [&](int s) { return wishes[s]; }, [&](int page) { return owner[page]; }, first, free_pages, n_free, missing);
 }
 
 // Few sequences, short tables and few pages: the three launches above by one workgroup, who has what in LDS
-__global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(ForkArgs a, int32_t *__restrict__ first, int32_t *__restrict__ free_pages, int32_t *__restrict__ n_free,
+__global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(ForkArgs a, Wish *__restrict__ wishes, int32_t *__restrict__ first, int32_t *__restrict__ free_pages, int32_t *__restrict__ n_free,
                                                                   int32_t *__restrict__ missing, int32_t *__restrict__ table_out, int32_t *__restrict__ lengths_out)
 {
     __shared__ int64_t waves[kPlanThreads / 64];
@@ -156,12 +165,12 @@ __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(ForkArgs a, in
     __shared__ Heir heirs[kSmallSequences];
     const int tid = threadIdx.x;
     Heir mine{};
-    Wish w{-1, 0, 0};
+    Wish w{-1, 0, 0, 0, 0};
     if (tid < a.B_out) mine = heir_of(a, tid);
     for (int i = tid; i < a.pt.n_pages; i += kPlanThreads) owner[i] = a.held && a.held[i] ? kReader : kNobody;
     if (tid < a.B_out) {
         heirs[tid] = mine;
-        w = wish_of(a, mine);
+        wishes[tid] = w = wish_of(a, mine);
         lengths_out[tid] = (int)min((int64_t)mine.length + mine.room, (int64_t)a.pt.max_pages << a.pt.page_shift);
     }
     __syncthreads();
@@ -180,20 +189,20 @@ __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(ForkArgs a, in
 
 // Sequence blockIdx.x: its new pages into its table (blockIdx.y = 0), what its partly filled page holds into a new one (all of them)
 template <typename Vec>
-__global__ __launch_bounds__(256) void fork_copy_kernel(ForkArgs a, const int32_t *__restrict__ first, const int32_t *__restrict__ free_pages,
-                                                        const int32_t *__restrict__ n_free, int row_vecs, Vec *__restrict__ k_cache, Vec *__restrict__ v_cache,
-                                                        int32_t *__restrict__ table_out)
+__global__ __launch_bounds__(256) void fork_copy_kernel(ForkArgs a, const Wish *__restrict__ wishes, const int32_t *__restrict__ first,
+                                                        const int32_t *__restrict__ free_pages, const int32_t *__restrict__ n_free, int row_vecs,
+                                                        Vec *__restrict__ k_cache, Vec *__restrict__ v_cache, int32_t *__restrict__ table_out)
 {
-    const int s = blockIdx.x, found = *n_free;
-    const Heir h = heir_of(a, s);
-    const bool moves = first[s] < 0;
-    const int at = moves ? ~first[s] : first[s], begin = pages_before(h) - moves, n = moves + max(0, h.table_pages - pages_before(h));
+    const int s = blockIdx.x, found = *n_free, of_list = first[s];
+    const Wish w = wishes[s];
+    const bool moves = of_list < 0;
+    const int at = moves ? ~of_list : of_list, begin = w.before - moves, n = moves + w.taken;
     if (blockIdx.y == 0)
         for (int i = threadIdx.x; i < n; i += 256)
             table_out[(int64_t)s * a.pt.max_pages + begin + i] = at + i < found ? free_pages[at + i] : -1;
     if (!moves || at >= found) return;
-    const int64_t from = ((int64_t)page_at(a, h.parent, h.full) << a.pt.page_shift) * row_vecs, to = ((int64_t)free_pages[at] << a.pt.page_shift) * row_vecs;
-    const int64_t vecs = (int64_t)h.part * row_vecs;
+    const int64_t from = ((int64_t)w.tail << a.pt.page_shift) * row_vecs, to = ((int64_t)free_pages[at] << a.pt.page_shift) * row_vecs;
+    const int64_t vecs = (int64_t)w.part * row_vecs;
     for (int64_t i = blockIdx.y * 256 + threadIdx.x; i < vecs; i += gridDim.y * 256) {
         k_cache[to + i] = k_cache[from + i];
         v_cache[to + i] = v_cache[from + i];
@@ -250,18 +259,18 @@ __global__ __launch_bounds__(256) void paged_compact_kernel(CompactArgs a, int r
 
 } // namespace
 
-size_t paged_fork_workspace_bytes(int64_t n_pages, int64_t B_out) { return sizeof(int32_t) * (size_t)(4 * B_out + 2 * n_pages + B_out + 4); }
+size_t paged_fork_workspace_bytes(int64_t n_pages, int64_t B_out) { return sizeof(Wish) * (size_t)B_out + sizeof(int32_t) * (size_t)(2 * n_pages + B_out + 4); }
 
 hipError_t launch_paged_fork(const ForkArgs &a, int row_bytes, void *k_cache, void *v_cache, int32_t *scratch, int32_t *table_out, int32_t *lengths_out, int32_t *missing,
                              hipStream_t st)
 {
     // (a launch has fewer than 2^32 threads)
     const auto shared = [&](int64_t workgroups) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(workgroups, ((int64_t)1 << 22) / std::max(a.B_out, 1))); };
-    int4 *const wishes = reinterpret_cast<int4 *>(scratch);
-    int32_t *const owner = scratch + 4 * (int64_t)a.B_out, *const free_pages = owner + a.pt.n_pages, *const first = free_pages + a.pt.n_pages, *const n_free = first + a.B_out;
+    Wish *const wishes = reinterpret_cast<Wish *>(scratch);
+    int32_t *const owner = reinterpret_cast<int32_t *>(wishes + a.B_out), *const free_pages = owner + a.pt.n_pages, *const first = free_pages + a.pt.n_pages, *const n_free = first + a.B_out;
     if (a.B_out <= kSmallSequences && a.pt.n_pages <= kSmallPages && (int64_t)a.B_out * a.pt.max_pages <= kSmallEntries) {
         TimedLaunch tl(K_FORK_SMALL, st);
-        hipLaunchKernelGGL(fork_small_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, first, free_pages, n_free, missing, table_out, lengths_out);
+        hipLaunchKernelGGL(fork_small_kernel, dim3(1), dim3(kPlanThreads), 0, st, a, wishes, first, free_pages, n_free, missing, table_out, lengths_out);
     } else {
         {
             TimedLaunch tl(K_FORK_CLEAR, st);
@@ -277,8 +286,8 @@ hipError_t launch_paged_fork(const ForkArgs &a, int row_bytes, void *k_cache, vo
     if (a.B_out > 0) {
         const int64_t bytes = 2 * ((int64_t)row_bytes << a.pt.page_shift);
         TimedLaunch tl(K_FORK_COPY, st);
-        hipLaunchKernelGGL(fork_copy_kernel<f32x4>, dim3((unsigned)a.B_out, shared(std::min<int64_t>(64, bytes / 32768))), dim3(256), 0, st, a, first,
-                           free_pages, n_free, row_bytes / 16, static_cast<f32x4 *>(k_cache), static_cast<f32x4 *>(v_cache), table_out);
+        hipLaunchKernelGGL(fork_copy_kernel<f32x4>, dim3((unsigned)a.B_out, shared(std::min<int64_t>(64, bytes / 32768))), dim3(256), 0, st, a, wishes,
+                           first, free_pages, n_free, row_bytes / 16, static_cast<f32x4 *>(k_cache), static_cast<f32x4 *>(v_cache), table_out);
     }
     return hipGetLastError();
 }
