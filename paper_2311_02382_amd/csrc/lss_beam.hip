@@ -181,7 +181,8 @@ __device__ __forceinline__ double lanes_total(double x)
 }
 
 // exp(x), log2 e in two parts: one rounding of it would shift a row's weights all the same way, and the row's sum with them
-__device__ __forceinline__ float exp_of(float x) { return fast_exp2(fmaf(x, 1.9259629e-8f, x * 1.44269502f)); }
+constexpr float kLog2eUp = 1.44269502f;
+__device__ __forceinline__ float exp_of(float x) { return fast_exp2(fmaf(x, 1.9259629e-8f, x * kLog2eUp)); }
 
 // Tokens v0 .. v1 - 1 of a row (v0 a multiple of kBatch): the best of them go to `best`.  Which lane has which token does not depend on where the row lies (rows of an
 // odd number of logits are not 16-byte aligned, and loads need not be): rows alike have sums alike to the last bit, and equal totals then go to the lower beam.
@@ -220,9 +221,19 @@ __device__ __forceinline__ ChunkStats scan_row(const T *row, int64_t v0, int64_t
         }
         const float higher = fmaxf(top, most), use = higher == -INFINITY ? 0.f : higher;
         float part[2] = {0.f, 0.f};
+        if (__all(fabsf(use) <= 16384.f)) {
+            // exp(x - use) = 2^(x c - m) 2^(m - use c), c log2 e rounded, m use c rounded: one instruction a logit ahead of its exponential, and what m is off by is made up for
+            // in the sum.  (Off by x - use times 1.3e-8 and half a step of the exponent.)
+            const float m = use * kLog2eUp;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) part[i & 1] += exp_of(x[i] - use);
-        sum = sum * (double)exp_of(top - use) + (double)(part[0] + part[1]);
+            for (int i = 0; i < kLoads; ++i) part[i & 1] += fast_exp2(fmaf(x[i], kLog2eUp, -m));
+            part[0] = (part[0] + part[1]) * fast_exp2(-fmaf(use, kLog2eUp, -m));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) part[i & 1] += exp_of(x[i] - use);
+            part[0] += part[1];
+        }
+        sum = sum * (double)exp_of(top - use) + (double)part[0];
         top = higher;
         // the bound from the largest of the lanes, or where they would be too few of their eights: n of them are candidates themselves
         if (best.n <= kFew) {
