@@ -509,6 +509,8 @@ int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t 
  *              overlap in time on one GPU need a buffer each
  * A row that sees no key gives zeros and lse = -infinity; a key that a row does not see does not reach its result, whatever its value.  Rows of no sequence are
  * not touched.  rows * H <= 2^24, B * H_kv <= 2^22, words <= 1024 (LSS_ERR_SHAPE otherwise).
+ * bf16: with up to 16 rows per head of keys in a sequence (on average) a weight enters the product with the values as two parts, off by 2^-16, else rounded to bf16, off by
+ * 2^-8; an infinite value in front of the drafted tokens at a weight below 2^-126 may give NaN.
  */
 size_t lss_paged_attn_tree_workspace_bytes(int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int64_t max_len, int elem_bytes);
 int lss_paged_attn_tree(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
@@ -530,7 +532,8 @@ int lss_paged_attn_tree(const void *q, int64_t q_stride, const void *k_cache, co
  *   held    [n_pages] or NULL: not 0 where somebody else has the page
  *   table_out [B_out, max_pages], lengths_out [B_out]: lengths[p] + room[s], at most what a table holds (written)
  *   missing [1] (written): pages that there were too few of, or that the tables have no entry for; their entries are -1, a partly filled page's that could not be
- *           copied too.  Nothing that the old table names has been written then, so the call can be made again from it
+ *           copied too.  The tokens of all sequences that are a parent are as they were then, so the call can be made again from the old table, with
+ *           these parents or some of them
  *   workspace  DEVICE buffer of lss_paged_fork_workspace_bytes() bytes, 16-byte aligned; NULL: the registered one
  * An entry that names no page stays one that names none.  Outputs lie over no input (LSS_ERR_RANGE).  B, B_out <= 2^20 (LSS_ERR_SHAPE otherwise).
  */
@@ -544,6 +547,7 @@ int lss_paged_fork(const int32_t *lengths, const int32_t *block_table, const int
  * lss_paged_compact: of sequence b's n_b = cu_q[b + 1] - cu_q[b] last tokens (of lengths[b]) the kept ones move to their front:
  *     token lengths[b] - n_b + i  becomes what token lengths[b] - n_b + kept[b, i] was,  i < m_b = min(n_kept[b], max_kept, n_b)
  *   kept [B, max_kept], n_kept [B]: numbers below n_b, ascending; one that is not (or below its place i) leaves its place as it is, or with another's of the list
+ *   The pages that these tokens lie in are their sequence's alone (as lss_paged_fork leaves them): moves of two sequences over one page are in no order
  *   lengths_out [B] (written): lengths[b] - n_b + m_b.  It lies over no input (LSS_ERR_RANGE)
  * Tokens without a page neither move nor are moved to.  Uses no workspace.  B <= 2^18 (LSS_ERR_SHAPE otherwise).
  */
@@ -563,7 +567,7 @@ int lss_paged_compact(const int32_t *lengths, const int32_t *block_table, const 
  *   workspace DEVICE buffer of lss_beam_select_workspace_bytes() bytes (0 where V is small), 16-byte aligned; NULL: the registered one
  * No continuation: of a beam whose score is not finite or whose row's log-sum-exp is not (a NaN or +infinity in it, nothing but -infinity); a logit of -infinity.
  * Where there are fewer than n_out: -infinity, -1, -1 and 1.  Within a beam logits are compared as they are; totals are made and compared in 64 bits, of a
- * log-sum-exp that is off by 2^-19 at most (alike for rows that are).  K, n_out <= 64, K V < 2^31, B K <= 2^20 (LSS_ERR_SHAPE otherwise).  Outputs lie over no input (LSS_ERR_RANGE).
+ * log-sum-exp that is off by less than 2^-18 (alike for rows that are).  K, n_out <= 64, K V < 2^31, B K <= 2^20 (LSS_ERR_SHAPE otherwise).  Outputs lie over no input (LSS_ERR_RANGE).
  */
 size_t lss_beam_select_workspace_bytes(int64_t B, int64_t K, int64_t V, int64_t n_out);
 int lss_beam_select(const void *logits, int64_t stride, const float *scores, const uint8_t *finished, int64_t end_token,

@@ -386,13 +386,14 @@ def lss_paged_fork(k_cache, v_cache, block_table, lengths, parents, room=None, h
     more than one sequence writes into, or that somebody else reads, is copied; pages that no sequence of the result names are free, unless held[page] (int32
     [n_pages]) is not 0.  A parent outside [0, B): a sequence without tokens.
 
-    Returns (table_out [S, max_pages], lengths_out [S]: with the room, missing [1]: pages that there were too few; the old table is as it was)."""
+    Returns (table_out [S, max_pages], lengths_out [S]: with the room, missing [1]: pages that there were too few).  With too few the parents' tokens are as they
+    were, and the call can be made again from the old table (which is only read)."""
     return (_native or _bind()).paged_fork(k_cache, v_cache, block_table, lengths, parents, room, held, table_out, lengths_out, missing, stream, workspace)
 
 
 def lss_paged_compact(k_cache, v_cache, block_table, lengths, cu_q, kept, n_kept, lengths_out=None, stream=None):
     """The drafted tokens that are kept move to the front of them: of sequence b's n_b = cu_q[b + 1] - cu_q[b] last tokens the numbers kept[b, :n_kept[b]]
-    (int32 [B, most], ascending) become the first n_kept[b].  Returns lengths_out int32 [B]: the lengths without those that are not kept."""
+    (int32 [B, most], ascending) become the first n_kept[b]; their pages are the sequence's own.  Returns lengths_out int32 [B]: the lengths without those that are not kept."""
     return (_native or _bind()).paged_compact(k_cache, v_cache, block_table, lengths, cu_q, kept, n_kept, lengths_out, stream)
 
 

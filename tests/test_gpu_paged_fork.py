@@ -85,6 +85,29 @@ def test_too_few_pages():
     assert int(got[2]) > 10 ** 6 // 16
 
 
+def test_too_few_pages_and_again():
+    # what parents have is untouched by a call that had too few pages (only a sequence that is nobody's parent gives its own up): made again where there is room, it is whole
+    page, lengths, parents = 16, [16, 20, 40, 70], [0, 0, 1, 1, 1, 2, 2]
+    table, n = sv.tables(lengths, page, 21, spare=0, extra=1)
+    kc, vc = (sv.normal(n + 8, page, 2, 64, seed=62 + i) for i in (0, 1))
+    gk, gv, gt, gl, gp = kc.cuda(), vc.cuda(), table.cuda(), _i32(lengths).cuda(), _i32(parents).cuda()
+    held = torch.zeros(n + 8, dtype=torch.int32)
+    held[n:] = 1
+    held[table[3].long()[:5]] = 1
+    want = co.fork(kc, vc, table, lengths, parents, None, held)
+    first = lss.lss_paged_fork(gk, gv, gt, gl, gp, held=held.cuda())
+    assert int(first[2]) == want[4] > 0 and torch.equal(first[0].cpu(), want[2])
+    for b in range(3):
+        for nth in range(-(-lengths[b] // page)):
+            rows = min(page, lengths[b] - nth * page)
+            _same(gk[int(table[b, nth]), :rows], kc[int(table[b, nth]), :rows], "a parent's keys")
+            _same(gv[int(table[b, nth]), :rows], vc[int(table[b, nth]), :rows], "a parent's values")
+    want = co.fork(gk.cpu(), gv.cpu(), table, lengths, parents)
+    again = lss.lss_paged_fork(gk, gv, gt, gl, gp)
+    assert int(again[2]) == 0 == want[4] and torch.equal(again[0].cpu(), want[2]) and torch.equal(again[1].cpu(), want[3])
+    _same(gk, want[0], "k_cache"), _same(gv, want[1], "v_cache")
+
+
 def test_pages_that_others_hold():
     page, lengths = 16, [20, 33, 8]
     table, n = sv.tables(lengths, page, 15, spare=12, extra=2)
