@@ -273,7 +273,8 @@ __device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, i
     const int R = of(s.R), tiles = of(s.tiles), c = (R + S - 1) / S, within = (int)(at - (before + lane64(upto - mine, l)) * a.H_kv), rest = within % (tiles * c);
     p.b = b0 + l, p.begin = of(s.begin), p.n = of(s.n), p.length = of(s.length);
     p.h_kv = within / (tiles * c), p.tiles = tiles, p.tile = rest % tiles;
-    p.count = c, p.r0 = rest / tiles * S, p.r1 = min(R, p.r0 + S);
+    const int part = rest / tiles, even = R / c, more_of = R - even * c;       // (as equal as they can be)
+    p.count = c, p.r0 = part * even + min(part, more_of), p.r1 = p.r0 + even + (part < more_of);
     p.slot = (int)at;
     p.item = (tiles_before + of(lane_sum_scan(s.tiles) - s.tiles)) * a.H_kv + p.h_kv * tiles + p.tile;
     return true;
