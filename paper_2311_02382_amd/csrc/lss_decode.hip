@@ -553,7 +553,7 @@ __global__ __launch_bounds__(64 * kWaves, tree_per_cu(sizeof(T), D, NQ)) void pa
     __shared__ __attribute__((aligned(1024))) char smem[kWaves * C::REGION];
     __shared__ float sums[kWaves][2][16];
     TreePart p;
-    const bool some = tree_part<C::ROUND, 16 * NQ>(a, threadIdx.x & 63, blockIdx.x, target, least, slots ? slots : gridDim.x, p);
+    const bool some = tree_part<C::ROUND, 16 * NQ>(a, threadIdx.x & 63, blockIdx.x, target, target, least, slots ? slots : gridDim.x, p);
     if (slots && threadIdx.x == 0) TreeScratch{scratch, 16 * NQ, D, slots, tiles}.enter(p, some);
     if (!some) return;
     decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, true, 0, 1, 0, 0, p.b, 0, p.length, p, slots, tiles);

@@ -211,7 +211,7 @@ hipError_t launch_paged_tree(const TreeArgs &a, const T *q, const T *k_cache, co
 // (lss_decode.hip).  tiles of rows, at most; slots: parts that there are room for, `target` of them where the sequences are long, of `least` rounds at least; 0: a workgroup per tile of rows
 struct TreePlan {
     bool wide;
-    int rows, target, least, slots, tiles;
+    int rows, target, most, least, slots, tiles;
 };
 // workgroups of the latter on a compute unit (with two sixteens of rows one less than there, or registers would go to scratch memory)
 constexpr int tree_per_cu(int elem_bytes, int d, int sixteens) { return d == 64 ? (sixteens == 1 ? 3 : 2) : elem_bytes == 2 && sixteens == 1 ? 2 : 1; }

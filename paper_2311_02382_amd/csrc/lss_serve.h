@@ -216,8 +216,11 @@ __device__ __forceinline__ int64_t lanes_upto(int64_t x)
 }
 // Workgroup `id`'s part; false: there is none.  Parts are numbered by sequence, head, part of the keys and tile of rows, and each XCD (workgroups go to them in turn) has a run
 // of them: tiles of rows that read the same keys do so at the same time from one L2.  All lanes active; wavefront-uniform.
+// `most`: as many where as many more are resident at once, each of them slower; taken where parts become so much shorter that it is worth it.  d = 64, two and three workgroups
+// a compute unit: a round takes 17 twelfths as long, and a part some three rounds of its own (its start, its share of the joining launch).  24 sequences of 6000 tokens, 64
+// drafted: 85.4 us by 512, 69.1 by 768; 48 137.9 and 121.5; one of 36,000 with a chain of 256, whose tiles fill either: 64.4 and 68.6.
 template <int ROUND, int BR>
-__device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, int target, int least, int slots, TreePart &p)
+__device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, int target, int most, int least, int slots, TreePart &p)
 {
     const int G = a.H / a.H_kv;
     struct Some { int length, begin, n, tiles, R; };
@@ -239,18 +242,29 @@ __device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, i
         rounds += lane64(lanes_upto((int64_t)t.tiles * t.R), 63);
         all_tiles += __builtin_amdgcn_readlane(lane_sum_scan(t.tiles), 63);
     }
-    const int64_t wanted = divide(rounds * a.H_kv + target - 1, target);
-    int S = wanted < least ? least : wanted < 1 << 30 ? (int)wanted : 1 << 30;
     const auto parts = [](const Some &t, int S) { return (int64_t)t.tiles * ((t.R + S - 1) / S); };
-    int64_t mine, upto, all;
-    // (a part too many for the workgroups that there is room for at once waits for all of another: a few sizes are tried, where one part a tile fits)
-    for (int tries = 0;; ++tries) {
-        mine = parts(s, S), upto = lanes_upto(mine), all = lane64(upto, 63);
-        for (int b0 = 64; b0 < a.B; b0 += 64) all += lane64(lanes_upto(parts(load(b0), S)), 63);
-        if (all * a.H_kv <= target || (int64_t)all_tiles * a.H_kv > target || tries == 4 || S >= 1 << 24) break;
-        const int64_t more = divide((all * a.H_kv - target) * S, target);
-        S += more < 1 ? 1 : more < S ? (int)more : S;
+    struct Fit { int S; int64_t mine, upto, all; };
+    const auto fit = [&](int target) __attribute__((always_inline)) {
+        Fit f;
+        const int64_t wanted = divide(rounds * a.H_kv + target - 1, target);
+        f.S = wanted < least ? least : wanted < 1 << 30 ? (int)wanted : 1 << 30;
+        // (a part too many for the workgroups that there is room for at once waits for all of another: a few sizes are tried, where one part a tile fits)
+        for (int tries = 0;; ++tries) {
+            f.mine = parts(s, f.S), f.upto = lanes_upto(f.mine), f.all = lane64(f.upto, 63);
+            for (int b0 = 64; b0 < a.B; b0 += 64) f.all += lane64(lanes_upto(parts(load(b0), f.S)), 63);
+            if (f.all * a.H_kv <= target || (int64_t)all_tiles * a.H_kv > target || tries == 4 || f.S >= 1 << 24) break;
+            const int64_t more = divide((f.all * a.H_kv - target) * f.S, target);
+            f.S += more < 1 ? 1 : more < f.S ? (int)more : f.S;
+        }
+        return f;
+    };
+    Fit f = fit(target);
+    if (most > target && rounds * a.H_kv >= (int64_t)20 * most) {
+        const Fit g = fit(most);
+        if ((int64_t)17 * g.S + 36 < (int64_t)12 * f.S) f = g;
     }
+    const int S = f.S;
+    int64_t mine = f.mine, upto = f.upto, all = f.all;
     all *= a.H_kv;
     p.items = all > slots ? 0 : all_tiles * a.H_kv;     // (more than there can be: cu does not ascend)
     if (p.items == 0) return false;

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float
 // The form of a launch, from what the host knows: rows, sequences and a bound on their lengths, not the lengths.
 //   * bf16, more than 16 rows to a head of keys of an average sequence: wide.  24 sequences of 1 to 8192 tokens, 32 heads, 8 of keys, d = 128: 2 drafted tokens (8 rows)
 //     37.7 us, narrow 33.6; 4 39.8 and 35.3; 8 37.3 and 49.5; 32 53 and 93; 48 sequences of 2048 to 6500 with 64: 268 and 1736.  Float is always narrow.
-//   * Parts: as many as are resident at once (wide: two workgroups a compute unit), of 384 keys at least.  One sequence of 30,000 tokens, 16 drafted: 39.5 us, with half
+//   * Parts: as many as are resident at once (wide: two workgroups a compute unit, or at d = 64 three, see tree_part), of 384 keys at least.  One sequence of 30,000 tokens, 16 drafted: 39.5 us, with half
 //     as many again 52; d = 64, 24 sequences with 8: 17.7, parts of 512 keys 18.7, of 768 21, of 1024 24.
 //   * Lengths up to 512, or many tiles of up to 64 sequences (which then start with the longest): a tile each and no joining launch.  48 x 64 drafted tokens, 768 tiles: 268,
 //     in parts 310.
@@ -97,10 +97,11 @@ TreePlan pick(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem
     p.wide = wide;
     p.rows = wide ? 128 : some ? 32 : 16;
     p.target = wide ? 512 : 256 * tree_per_cu(elem_bytes, d, p.rows / 16);
+    p.most = wide && d == 64 ? 768 : p.target;
     p.least = wide ? 6 : 2;
     p.tiles = (int)((in_a_head / p.rows + std::min<int64_t>(rows, B)) * H_kv);
     p.slots = 0;
-    if (max_len > 512 && !(wide && p.tiles >= 768 && B <= 64)) p.slots = p.target + p.tiles;
+    if (max_len > 512 && !(wide && p.tiles >= 768 && B <= 64)) p.slots = p.most + p.tiles;
     else p.least = 1 << 30;
     return p;
 }

@@ -76,6 +76,12 @@ def test_a_chunk_of_a_long_prompt():
     _run([513, 100], [1800, 100], 4, 4, 64, 16, seed=511, tree=False)
 
 
+def test_more_parts_than_two_a_compute_unit():
+    # 192 tiles of rows of 90 to 94 rounds: four parts each where three workgroups are resident, two where two are
+    for tree in (True, False):
+        _run([64] * 24, [6000 - 11 * b for b in range(24)], 16, 4, 64, 32, seed=515, tree=tree)
+
+
 def test_many_sequences():
     _run([b % 4 for b in range(200)], [(37 * b) % 90 + 3 for b in range(200)], 8, 2, 64, 16, seed=520)
     _run([1 + b % 3 for b in range(90)], [(67 * b) % 900 + 3 for b in range(90)], 4, 1, 128, 32, seed=521)
