@@ -4,7 +4,11 @@
 // logits alone, in one pass over them that also keeps a running maximum and sum per lane; only n_out of each beam's get a total, in 64 bits.
 //
 // Rows are cut into chunks, a wavefront each (beam_rows_kernel), so that few rows fill the chip; a second launch, a workgroup per prompt, joins a row's chunks and
-// its beams (beam_select_kernel).  Where rows are short (kDirect) the second kernel goes over them itself and there is no first one.
+// its beams (beam_select_kernel).  Where rows are short (kDirect) and few the second kernel goes over them itself and there is no first one.
+//
+// What bounds them: long rows by vector issue (an exponential, a conversion, a product, a sum and half a maximum a logit): 256 rows of 128,256 in bf16, 66 MB, 18 to 19 us, 3.5 TB/s,
+// the vector ALU busy 59 % of the cycles, loads alone 12.1; short ones by latency (64 rows of 32,001: 6 us).  The second launch is 7 to 10 us of steps one behind the other: lists, a bound, totals,
+// ranking.  All of it, 32 prompts x 8 beams of 128,256: 25.6 us; 8 x 8 of 32,001, 16 chosen, 15.2; 4 beams of 256 6.3.
 #include "lss_device_once.h"
 #include "lss_serve.h"
 

@@ -7,7 +7,8 @@ namespace lss {
 
 namespace {
 
-// Joins the parts of tile of rows blockIdx.x, in their order: LANES lanes have a row, or in long chains S such groups with a part each, which meet in LDS
+// Joins the parts of tile of rows blockIdx.x, in their order: LANES lanes have a row, or in long chains S such groups with a part each, which meet in LDS.  What bounds it is a chain of
+// loads (where the parts are, whose rows, their sums and values): 5.7 us for 7 MB, 13 for 34.  Two groups for 5 to 8 parts: 16,016 rows of 6 parts of 64 8.7 us, four groups 11.6.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float *__restrict__ scratch, int rows, int slots, int most_tiles, T *__restrict__ out,
                                                          float *__restrict__ lse)
@@ -23,7 +24,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float
     queries_of(a, chain.b, begin, n_rows);
     n_rows *= G;
     const int n_q = min(rows, n_rows - chain.tile * rows);
-    const int S = chain.count <= 4 ? 1 : chain.count <= 16 ? 4 : GROUPS, at_once = GROUPS / S, share = grp % S;
+    const int S = chain.count <= 4 ? 1 : chain.count <= 8 ? 2 : chain.count <= 16 ? 4 : GROUPS, at_once = GROUPS / S, share = grp % S;
     for (int n0 = blockIdx.y * at_once; n0 < n_q; n0 += gridDim.y * at_once) {
         const int n = min(n0 + grp / S, n_q - 1);
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
