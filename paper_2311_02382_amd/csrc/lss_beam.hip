@@ -9,7 +9,6 @@
 // What bounds them: long rows by vector issue (an exponential, a conversion, a product, a sum and half a maximum a logit): 256 rows of 128,256 in bf16, 66 MB, 18 to 19 us, 3.5 TB/s,
 // the vector ALU busy 59 % of the cycles, loads alone 12.1; short ones by latency (64 rows of 32,001: 6 us).  The second launch is 7 to 10 us of steps one behind the other: lists, a bound, totals,
 // ranking.  All of it, 32 prompts x 8 beams of 128,256: 25.6 us; 8 x 8 of 32,001, 16 chosen, 15.2; 4 beams of 256 6.3.
-#include "lss_device_once.h"
 #include "lss_serve.h"
 
 #include <algorithm>
@@ -392,8 +391,8 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
         wave_sync();
         const double lse = (double)s.top + log(s.sum);
         if (!(fabs(lse) < (double)INFINITY)) continue;
-        int first = 0;
-        if (lane == 0) first = atomicAdd(&n_candidates, best.count());
+        int first = __builtin_amdgcn_readfirstlane(best.count());
+        if (lane == 0) first = atomicAdd(&n_candidates, first);
         first = __builtin_amdgcn_readfirstlane(first);
         for (int i = lane; i < best.count(); i += 64) {
             total[first + i] = (double)score + ((double)descend(best.list[i].value) - lse);
@@ -508,18 +507,13 @@ hipError_t launch_beam_select(const T *logits, int64_t stride, const float *scor
     // (12 bytes of LDS a candidate, of 4096 at most, and 5 KB a wavefront: more than the 64 KB that a launch may have without asking)
     const int per_beam = K * N <= 1024 ? 2 * N : N, waves = std::min(K, 16);
     const size_t lds = (((size_t)K * per_beam * 12 + 15) & ~(size_t)15) + (size_t)waves * kWaveLds;
+    const bool direct = is_direct(K, V);
     if (lds > 65536 - 1024) {
-        static DeviceOnce once;
-        int dev = 0;
-        if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
-        const hipError_t e = once.run(dev, [] {
-            for (const void *kernel : {reinterpret_cast<const void *>(beam_select_kernel<T, true>), reinterpret_cast<const void *>(beam_select_kernel<T, false>)})
-                if (hipError_t err = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 4096 * 12 + 16 * kWaveLds); err != hipSuccess) return err;
-            return hipSuccess;
-        });
+        static DeviceOnce once[2];
+        const hipError_t e = allow_lds(direct ? beam_select_kernel<T, true> : beam_select_kernel<T, false>, 4096 * 12 + 16 * kWaveLds, once[direct]);
         if (e != hipSuccess) return e;
     }
-    if (is_direct(K, V)) {
+    if (direct) {
         TimedLaunch tl(K_BEAM_SELECT, st);
         hipLaunchKernelGGL((beam_select_kernel<T, true>), dim3((unsigned)B), dim3(64 * waves), lds, st, a, logits, scores, finished, lists, stats, per_beam, scores_out,
                            parents, tokens, finished_out);

@@ -181,10 +181,10 @@ struct DirectTile {
                          : : "s"(lds0), "s"(lds1), "v"(off[0]), "v"(off[1]), "s"(k_uniform), "s"(v_uniform) : "memory", "m0");
         else
             asm volatile("s_nop 4\n\ts_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %6, 0 offen lds\n\tbuffer_load_dwordx4 %3, %6, 0 offen offset:1024 lds\n\t"
-                         "buffer_load_dwordx4 %4, %6, 0 offen offset:2048 lds\n\tbuffer_load_dwordx4 %5, %6, 0 offen offset:3072 lds\n\t"
+                         "buffer_load_dwordx4 %4, %6, 0 offen offset:2048 lds\n\tbuffer_load_dwordx4 %5, %6, 0 offen offset:%8 lds\n\t"
                          "s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %7, 0 offen lds\n\tbuffer_load_dwordx4 %3, %7, 0 offen offset:1024 lds\n\t"
-                         "buffer_load_dwordx4 %4, %7, 0 offen offset:2048 lds\n\tbuffer_load_dwordx4 %5, %7, 0 offen offset:3072 lds"
-                         : : "s"(lds0), "s"(lds1), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(k_uniform), "s"(v_uniform) : "memory", "m0");
+                         "buffer_load_dwordx4 %4, %7, 0 offen offset:2048 lds\n\tbuffer_load_dwordx4 %5, %7, 0 offen offset:%8 lds"
+                         : : "s"(lds0), "s"(lds1), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(k_uniform), "s"(v_uniform), "n"(3 * 1024) : "memory", "m0");
     }
     // byte offset inside the tile of the 16-byte chunk c of row r
     static __device__ __forceinline__ int chunk_offset(int r, int c) { return r * (D * 2) + ((c ^ tile_swizzle<D>(r)) * 16); }
