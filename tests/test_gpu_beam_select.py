@@ -181,3 +181,23 @@ def test_refusals_of_the_binding():
         lss.lss_beam_select(x, s, 65)
     with pytest.raises(lss.LssError, match="LSS_ERR_RANGE"):
         lss.lss_beam_select(x, s, scores_out=s)
+
+
+@pytest.mark.parametrize("V", [1454, 20000])
+def test_wide_beams_captured(V):
+    # more shared memory than a launch has without asking; a graph follows its inputs
+    inputs = [_inputs(3, 32, V, torch.bfloat16, seed=90 + i) for i in range(3)]
+    logits, scores = (x.cuda() for x in inputs[0])
+    eager = [tuple(x.clone() for x in lss.lss_beam_select(l.cuda(), s.cuda(), 64)[:3]) for l, s in inputs]
+    ws = torch.empty(lss.lss_beam_select_workspace_bytes(3, 32, V, 64), dtype=torch.uint8, device="cuda")
+    outs = torch.empty(3, 64, device="cuda"), torch.empty(3, 64, dtype=torch.int32, device="cuda"), torch.empty(3, 64, dtype=torch.int32, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lss.lss_beam_select(logits, scores, 64, scores_out=outs[0], parents=outs[1], tokens=outs[2], workspace=ws)
+    for i in (0, 1, 2, 1):
+        logits.copy_(inputs[i][0]), scores.copy_(inputs[i][1])
+        for x in outs:
+            x.fill_(-7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs, eager[i]))
