@@ -335,8 +335,8 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
 #pragma unroll
             for (int i = 0; i < S::V_LOADS; ++i) S::store_value(mine, (i * 64 + lane) / S::CHUNKS, lane % S::CHUNKS, values[i]);
         };
-        // ... and their weights and sums
-        const auto weights = [&]() __attribute__((always_inline)) {
+        // ... and their weights and sums; `drafted`: sums so far may hold an infinite value of a drafted token's
+        const auto weights = [&](auto drafted) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
                 float top = -INFINITY;
@@ -349,10 +349,17 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
                     top = fmaxf(top, __shfl_xor(top, 32));
                     const float m_new = fmaxf(m[i], top * c), alpha = m_new > m[i] ? fast_exp2(m[i] - m_new) : 1.f;
                     l[i] *= alpha;
+                    if (decltype(drafted)::value && __any(alpha == 0.f && m[i] > -INFINITY)) {
 #pragma unroll
-                    for (int db = 0; db < D / 16; ++db)
+                        for (int db = 0; db < D / 16; ++db)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[i][db][e] *= alpha;
+                            for (int e = 0; e < 4; ++e) o[i][db][e] = add_scaled(alpha, o[i][db][e], 0.f);
+                    } else {
+#pragma unroll
+                        for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[i][db][e] *= alpha;
+                    }
                     m[i] = m_new;
                 }
                 const float m_use = m[i] == -INFINITY ? 0.f : m[i];
@@ -370,7 +377,7 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
         for (; j0 < j_end && (!TREE || j0 + TILE <= first_drafted); j0 += ROUND) {
             scores(j0);
             if (j0 + ROUND < j_end) load(j0 + ROUND);
-            weights();
+            weights(std::false_type{});
             S::template add_values<NQ>(mine, p, o, lane);
         }
         if constexpr (TREE)
@@ -396,7 +403,7 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             if (!(seen[i] >> (16 * hf + 4 * g + e) & 1)) p[i][hf][e] = -INFINITY;
-                weights();
+                weights(std::true_type{});
                 // 0 times a value that is not finite is NaN: such values are taken out of the tile, and added by themselves where their key is seen, with a weight
                 // that is not 0 then
                 const bool plain = !__any(!finite);
@@ -452,13 +459,23 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
                     total += weight[w] * sums[w][1][row];
                 }
                 float r[D / 16];
+                const auto join = [&](auto add) __attribute__((always_inline)) {
 #pragma unroll
-                for (int e = 0; e < D / 16; ++e) r[e] = 0.f;
+                    for (int e = 0; e < D / 16; ++e) r[e] = 0.f;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w)
+                    for (int w = 0; w < kWaves; ++w)
 #pragma unroll
-                    for (int e = 0; e < D / 16; ++e)
-                        r[e] = fmaf(weight[w], *reinterpret_cast<const float *>(smem + w * REGION + (row * ROW_STRIDE + col + e) * 4), r[e]);
+                        for (int e = 0; e < D / 16; ++e)
+                            r[e] = add(weight[w], *reinterpret_cast<const float *>(smem + w * REGION + (row * ROW_STRIDE + col + e) * 4), r[e]);
+                };
+                join([](float w, float x, float sum) { return fmaf(w, x, sum); });
+                if constexpr (TREE) {
+                    // (0 times infinity, or a NaN of its own: seldom)
+                    bool some = false;
+#pragma unroll
+                    for (int e = 0; e < D / 16; ++e) some = some || r[e] != r[e];
+                    if (some) join([](float w, float x, float sum) { return add_scaled(w, x, sum); });
+                }
                 if (TREE ? tp.count == 1 : r0 == 0 && r1 == R) {
                     const float inv = total == 0.f ? 0.f : 1.f / total;
                     int64_t row_out = (int64_t)b * a.H + h0 + nth;

@@ -520,7 +520,7 @@ __device__ __forceinline__ void fwd_bf16_body(char *smem, const View &s, const D
         wait_vmem_all();                                // the last, redundant prefetches must land before the workgroup's LDS is given away
     }
     if constexpr (PAGED) {
-        // values that are not finite in the tiles that drafted tokens are in, to the rows that see them: their weights are above 0, whatever they are
+        // values that are not finite in the tiles that drafted tokens are in, to the rows that see them: their weights are above 0, whatever they are (what joins parts keeps that: add_scaled)
         if (s_tiles > 0 && *s.spoilt && rw0 < s.l_s) {
             const int token = min(r, s.l_s - 1) / G;
             for (int key = max(max(s.first, 0) / C::BC, s_begin) * C::BC; key < min(s.l_x, (s_begin + s_tiles) * C::BC); ++key) {

@@ -312,6 +312,9 @@ struct TreeScratch {
         if (some && p.r0 == 0) *chain(p.item) = {p.b, p.h_kv, p.tile, p.slot, p.count, p.tiles, {0, 0}};
     }
 };
+// sum + factor * x, x a sum of weights times values and the factor what those weights are off by: above 0, but 0 in 32 bits where x's scores lie 2^7 or more (in powers of 2) below others.
+// 0 times a sum that is infinite would be NaN: such a one stays what it is.
+__device__ __forceinline__ float add_scaled(float factor, float x, float sum) { return fmaf(fabsf(x) < INFINITY ? factor : 1.f, x, sum); }
 inline size_t tree_scratch_bytes(int rows, int d, int slots, int tiles) { return sizeof(float) * (8 * ((size_t)tiles + 1) + (size_t)slots * rows * (d + 2)); }
 // Which of the 32 keys from drafted number c0 on (below 0: the tokens in front of them) drafted token i of its sequence sees; `bits`: its words
 __device__ __forceinline__ uint32_t keys_seen(const TreeArgs &a, const uint64_t *bits, int i, int c0)

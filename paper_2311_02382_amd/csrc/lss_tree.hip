@@ -46,14 +46,14 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float
             top = higher;
             total *= alpha;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] *= alpha;
+            for (int e = 0; e < 4; ++e) sum[e] = add_scaled(alpha, sum[e], 0.f);
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 const float weight = i0 + j * S < chain.count ? fast_exp2(m[j] - use) : 0.f;
                 total += weight * l[j];
                 if (i0 + j * S < chain.count)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, v[j][e], sum[e]);
+                    for (int e = 0; e < 4; ++e) sum[e] = add_scaled(weight, v[j][e], sum[e]);
             }
         }
         if (S > 1) {
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float
                 const float weight = fast_exp2(tops[first + i] - use);
                 total += weight * totals[first + i];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, v[e], sum[e]);
+                for (int e = 0; e < 4; ++e) sum[e] = add_scaled(weight, v[e], sum[e]);
             }
         }
         if (share != 0 || n0 + grp / S >= n_q) continue;
