@@ -566,8 +566,8 @@ int lss_paged_compact(const int32_t *lengths, const int32_t *block_table, const 
  *   scores_out, parents, tokens [B, n_out] (written): total, b K + k, v.  finished_out [B, n_out] bytes or NULL (written): 1 if the beam had ended or v is end_token
  *   workspace DEVICE buffer of lss_beam_select_workspace_bytes() bytes (0 where V is small), 16-byte aligned; NULL: the registered one
  * No continuation: of a beam whose score is not finite or whose row's log-sum-exp is not (a NaN or +infinity in it, nothing but -infinity); a logit of -infinity.
- * Where there are fewer than n_out: -infinity, -1, -1 and 1.  Within a beam logits are compared as they are; totals are made and compared in 64 bits, of a
- * log-sum-exp that is off by less than 2^-18 (alike for rows that are).  K, n_out <= 64, K V < 2^31, B K <= 2^20 (LSS_ERR_SHAPE otherwise).  Outputs lie over no input (LSS_ERR_RANGE).
+ * Where there are fewer than n_out: -infinity, -1, -1 and 1.  Within a beam logits are compared as they are, of equal ones the lower v first; those of different beams by totals that are
+ * made in 64 bits, of a log-sum-exp that is off by less than 2^-18 (alike for rows that are), of equal ones the lower k first.  K, n_out <= 64, K V < 2^31, B K <= 2^20 (LSS_ERR_SHAPE otherwise).  Outputs lie over no input (LSS_ERR_RANGE).
  */
 size_t lss_beam_select_workspace_bytes(int64_t B, int64_t K, int64_t V, int64_t n_out);
 int lss_beam_select(const void *logits, int64_t stride, const float *scores, const uint8_t *finished, int64_t end_token,

@@ -1,7 +1,8 @@
 // Beam search's choice over beams and vocabulary (lss_beam_select).
 //
 // total(k, v) = score_k + x_kv - log sum_v exp x_kv.  Within a beam the order of the totals is that of the logits, so a beam's candidates are found by their
-// logits alone, in one pass over them that also keeps a running maximum and sum per lane; only n_out of each beam's get a total, in 64 bits.
+// logits alone, in one pass over them that also keeps a running maximum and sum per lane; only n_out of each beam's get a total, in 64 bits.  Where these may be alike though a
+// beam's logits are not (next to 0, or beside a large score), equal ones of a beam are compared by their logits once more.
 //
 // Rows are cut into chunks, a wavefront each (beam_rows_kernel), so that few rows fill the chip; a second launch, a workgroup per prompt, joins a row's chunks and
 // its beams (beam_select_kernel).  Where rows are short (kDirect) and few the second kernel goes over them itself and there is no first one.
@@ -321,12 +322,12 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
                                                            int32_t *__restrict__ parents, int32_t *__restrict__ tokens, uint8_t *__restrict__ finished_out)
 {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    __shared__ int n_candidates, n_above, above[32];
+    __shared__ int n_candidates, n_above, alike, above[32];
     double *const total = reinterpret_cast<double *>(smem);                        // [K per_beam]
     uint32_t *const flat = reinterpret_cast<uint32_t *>(total + a.K * per_beam);    // beam * V + token
     char *const lds = smem + ((a.K * per_beam * 12 + 15) & ~15);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6, b = blockIdx.x;
-    if (tid == 0) n_candidates = n_above = 0;
+    if (tid == 0) n_candidates = n_above = alike = 0;
     if (tid < 32) above[tid] = 0;
     __syncthreads();
     for (int k = wave; k < a.K; k += waves) {
@@ -394,10 +395,17 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
         int first = __builtin_amdgcn_readfirstlane(best.count());
         if (lane == 0) first = atomicAdd(&n_candidates, first);
         first = __builtin_amdgcn_readfirstlane(first);
+        // Two of its logits differ by 2^-24 of either at least, their totals' roundings by less than 2^-51 of |logit| + |lse| + |score|: totals may be alike where the logits are not only where
+        // a logit that is not 0 is below 2^-26 of |lse| + |score|
+        const float beside = (float)(fabs(lse) + fabs((double)score));
+        bool next_to_0 = false;
         for (int i = lane; i < best.count(); i += 64) {
-            total[first + i] = (double)score + ((double)descend(best.list[i].value) - lse);
+            const float x = descend(best.list[i].value);
+            total[first + i] = (double)score + ((double)x - lse);
             flat[first + i] = (uint32_t)k * a.V + best.list[i].index;
+            next_to_0 = next_to_0 || (x != 0.f && fabsf(x) * 0x1p26f < beside);
         }
+        if (next_to_0) alike = 1;
     }
     __syncthreads();
     const int n = n_candidates;
@@ -425,6 +433,23 @@ __global__ __launch_bounds__(1024) void beam_select_kernel(BeamArgs a, const T *
     };
     const auto better_than = [&](const double *totals, const uint32_t *places, double x, uint32_t place, int from, int to) __attribute__((always_inline)) {
         int better = 0;
+        if (alike) {
+            // of equal totals of one beam the larger logit, as it is
+            const uint32_t V = (uint32_t)a.V, k = place / V;
+            const T *const row = logits + ((int64_t)b * a.K + k) * a.stride;
+#pragma unroll 1
+            for (int j = from; j < to; ++j) {
+                const double y = totals[j];
+                const uint32_t at = places[j];
+                bool before = at < place;
+                if (y == x && at != place && at / V == k) {
+                    const float theirs = (float)row[at - k * V], mine = (float)row[place - k * V];
+                    before = theirs > mine || (theirs == mine && before);
+                }
+                better += (int)(y > x) | ((int)(y == x) & (int)before);
+            }
+            return better;
+        }
 #pragma unroll 8
         for (int j = from; j < to; ++j) {               // (no branch: reads ahead of one another)
             const double y = totals[j];
