@@ -60,7 +60,8 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedArgs a, PackedP
         if ((bad >> (i * LANES) & ((uint64_t)1 << (LANES - 1) << 1) - 1) == 0) continue;
         const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, i * LANES); };
         const int ti = of(t), hi = of(h), bi = of(b), h_kv = hi / (a.H / a.H_kv);
-        const int k_begin = max(0, min(a.cu_k[bi], a.rows_k)), n_k = max(0, min(a.cu_k[bi + 1], a.rows_k) - k_begin);
+        int k_begin, n_k;
+        keys_of(a, bi, k_begin, n_k);
         const int seen = a.causal ? max(0, min(n_k, n_k - (min(of(end), a.rows_q) - ti) + 1)) : n_k;
         row_attention<T, D, 2>(q + ti * a.q_stride + (int64_t)hi * D, k + k_begin * a.k_stride + (int64_t)h_kv * D, a.k_stride,
                             v + k_begin * a.v_stride + (int64_t)h_kv * D, a.v_stride, seen, __builtin_bit_cast(float, of(__builtin_bit_cast(int, row_lse))), lane,

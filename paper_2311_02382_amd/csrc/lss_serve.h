@@ -3,6 +3,7 @@
 #pragma once
 #include "lss_common.h"
 #include "lss_kernels.h"
+#include "lss_starts.h"
 
 #include <type_traits>
 
@@ -54,18 +55,19 @@ struct PackedTile { int q_begin, n_q, k_begin, n_k, tile, b; };
 // floor(cu[b] G / BR) + b on -- room for all of them, one at most too much --, which is found like a row's sequence.
 __device__ __forceinline__ void sequence_rows(const int32_t *cu, int b, int rows, int &begin, int &n)
 {
-    begin = max(0, min(cu[b], rows));
-    n = max(0, min(cu[b + 1], rows) - begin);
+    const int start = cu[b];
+    begin = start_within(start, rows);
+    n = rows_between(start, cu[b + 1], rows);
 }
 __device__ __forceinline__ void queries_of(const PackedArgs &a, int b, int &begin, int &n) { sequence_rows(a.cu_q, b, a.rows_q, begin, n); }
 __device__ __forceinline__ void keys_of(const PackedArgs &a, int b, int &begin, int &n) { sequence_rows(a.cu_k, b, a.rows_k, begin, n); }
-__device__ __forceinline__ int first_query(const PackedArgs &a, int b) { return max(0, min(a.cu_q[b], a.rows_q)); }
+__device__ __forceinline__ int first_query(const PackedArgs &a, int b) { return start_within(a.cu_q[b], a.rows_q); }
 __device__ __forceinline__ int most_keys(const PackedArgs &a) { return a.rows_k; }
 __device__ __forceinline__ bool is_causal(const PackedArgs &a) { return a.causal; }
 // ... of drafted tokens, whose keys are in the cache (their number; they begin nowhere)
 __device__ __forceinline__ void queries_of(const TreeArgs &a, int b, int &begin, int &n) { sequence_rows(a.cu, b, a.rows, begin, n); }
 __device__ __forceinline__ void keys_of(const TreeArgs &a, int b, int &begin, int &n) { begin = 0, n = max(0, min(a.lengths[b], a.max_len)); }
-__device__ __forceinline__ int first_query(const TreeArgs &a, int b) { return max(0, min(a.cu[b], a.rows)); }
+__device__ __forceinline__ int first_query(const TreeArgs &a, int b) { return start_within(a.cu[b], a.rows); }
 __device__ __forceinline__ int most_keys(const TreeArgs &a) { return a.max_len; }
 __device__ __forceinline__ bool is_causal(const TreeArgs &a) { return a.tree == nullptr; }
 template <int BR, typename Args>
