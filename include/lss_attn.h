@@ -505,7 +505,7 @@ int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t 
  *   q     [rows, H, d];  out [rows, H, d] contiguous (written);  lse [rows, H] float (written)
  *   cu_q  [B + 1] int32, ascending
  *   tree  [rows, words] int64 or NULL; a drafted token past its words is seen by nobody.  A row sees itself only where its own bit is set
- *   workspace  DEVICE buffer of lss_paged_attn_tree_workspace_bytes() bytes, 16-byte aligned; NULL: the one registered with lss_set_workspace().  Calls that
+ *   workspace  DEVICE buffer of lss_paged_attn_tree_workspace_bytes() bytes (at most 70 MB, whatever the sizes), 16-byte aligned; NULL: the one registered with lss_set_workspace().  Calls that
  *              overlap in time on one GPU need a buffer each
  * A row that sees no key gives zeros and lse = -infinity; a key that a row does not see does not reach its result, whatever its value.  Rows of no sequence are
  * not touched.  rows * H <= 2^24, B * H_kv <= 2^22, words <= 1024 (LSS_ERR_SHAPE otherwise).

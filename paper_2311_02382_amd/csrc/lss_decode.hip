@@ -226,7 +226,7 @@ template <typename T, int D, int NQ, bool STREAM, typename Args>
 __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (&sums)[kWaves][2][16], const T *__restrict__ q,
                                               const T *__restrict__ k_cache, const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,
                                               float *__restrict__ scratch, bool whole, int64_t at, int64_t end, int64_t share, int64_t base, int b, int v_head, int length,
-                                              const TreePart &tp = TreePart{}, int slots = 0, int tree_tiles = 0)
+                                              const TreePart &tp = TreePart{}, int slots = 0, int chains = 0)
 {
     typedef Decode<T, D> C;
     typedef Step<T, D> S;
@@ -239,7 +239,7 @@ __device__ __forceinline__ void decode_rounds(const Args &a, char *smem, float (
     const int G = a.H / a.H_kv, n_rows = TREE ? tp.n * G : G, groups = TREE ? tp.tiles : (G + 16 * NQ - 1) / (16 * NQ), v_heads = a.H_kv * groups;
     constexpr int PARTS = parts_of(sizeof(T), D, NQ);
     const Scratch parts{scratch, min(G, 16 * NQ), D, PARTS};
-    const TreeScratch tree_parts{scratch, 16 * NQ, D, slots, tree_tiles};
+    const TreeScratch tree_parts{scratch, 16 * NQ, D, slots, chains};
     const bool by_item = (int64_t)a.B * v_heads <= PARTS;
     // (a page is at most 2^29 elements: what lies within 16 rows of one is 32 bits away)
     const int64_t row_bytes = (int64_t)a.H_kv * D * (int)sizeof(T);
@@ -565,16 +565,16 @@ __global__ __launch_bounds__(64 * kWaves, parts_of(sizeof(T), D, NQ) / 256) void
 template <typename T, int D, int NQ>
 __global__ __launch_bounds__(64 * kWaves, tree_per_cu(sizeof(T), D, NQ)) void paged_tree_kernel(TreeArgs a, const T *__restrict__ q, const T *__restrict__ k_cache,
                                                                     const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,
-                                                                    float *__restrict__ scratch, int target, int least, int slots, int tiles)
+                                                                    float *__restrict__ scratch, int target, int least, int slots, int chains)
 {
     typedef Decode<T, D> C;
     __shared__ __attribute__((aligned(1024))) char smem[kWaves * C::REGION];
     __shared__ float sums[kWaves][2][16];
     TreePart p;
-    const bool some = tree_part<C::ROUND, 16 * NQ>(a, threadIdx.x & 63, blockIdx.x, target, target, least, slots ? slots : gridDim.x, p);
-    if (slots && threadIdx.x == 0) TreeScratch{scratch, 16 * NQ, D, slots, tiles}.enter(p, some);
+    const bool some = tree_part<C::ROUND, 16 * NQ>(a, threadIdx.x & 63, blockIdx.x, target, target, least, gridDim.x, p);
+    if (slots && threadIdx.x == 0) TreeScratch{scratch, 16 * NQ, D, slots, chains}.enter(p, some);
     if (!some) return;
-    decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, true, 0, 1, 0, 0, p.b, 0, p.length, p, slots, tiles);
+    decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, true, 0, 1, 0, 0, p.b, 0, p.length, p, slots, chains);
 }
 
 // Joins the parts of the sequences that more than one workgroup had rounds of, in their order: workgroup x those of chain x, queries y, y + gridDim.y ..
@@ -678,10 +678,9 @@ hipError_t launch_paged_decode(const DecodeArgs &a, const T *q, const T *k_cache
 template <typename T>
 hipError_t launch_tree_narrow(const TreeArgs &a, const TreePlan &p, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st)
 {
-    const int64_t tiles = ((int64_t)a.rows * (a.H / a.H_kv) / p.rows + std::min(a.rows, a.B)) * a.H_kv;
-    const dim3 grid((unsigned)(((p.slots ? p.slots : tiles) + 7) / 8 * 8)), block(64 * kWaves);
+    const dim3 grid((unsigned)(((p.slots ? p.most : 0) + p.tiles + 7) / 8 * 8)), block(64 * kWaves);
     TimedLaunch tl(K_PAGED_TREE, st);
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, q, k_cache, v_cache, out, lse, scratch, p.target, p.least, p.slots, p.tiles); };
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, q, k_cache, v_cache, out, lse, scratch, p.target, p.least, p.slots, p.chains); };
     if (a.d == 64) p.rows == 16 ? go(paged_tree_kernel<T, 64, 1>) : go(paged_tree_kernel<T, 64, 2>);
     else p.rows == 16 ? go(paged_tree_kernel<T, 128, 1>) : go(paged_tree_kernel<T, 128, 2>);
     return hipGetLastError();

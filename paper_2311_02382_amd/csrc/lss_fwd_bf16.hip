@@ -700,14 +700,14 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void packed_bf16_ker
 template <int D, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void tree_bf16_kernel(TreeArgs a, const bf16_t *__restrict__ q, const bf16_t *__restrict__ k_cache,
                                                           const bf16_t *__restrict__ v_cache, bf16_t *__restrict__ out, float *__restrict__ lse,
-                                                          float *__restrict__ scratch, int n_tiles, int target, int most, int least, int slots, int tiles)
+                                                          float *__restrict__ scratch, int n_tiles, int target, int most, int least, int slots, int chains)
 {
     using C = FwdBf16Cfg<D, 4, 1>;
     __shared__ __attribute__((aligned(1024))) char smem[C::lds(false)];
     __shared__ int spoilt;
     const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5, G = a.H / a.H_kv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const TreeScratch parts{scratch, C::BR, D, slots, tiles};
+    const TreeScratch parts{scratch, C::BR, D, slots, chains};
     TreePart p;
     if constexpr (WHOLE) {
         int rank;
@@ -716,7 +716,7 @@ __global__ __launch_bounds__(256, 2) void tree_bf16_kernel(TreeArgs a, const bf1
         if (!packed_tile<C::BR>(a, G, rank, lane, t)) return;
         p.b = t.b, p.tile = t.tile, p.begin = t.q_begin, p.n = t.n_q, p.length = t.n_k, p.r0 = 0, p.r1 = (t.n_k + C::BC - 1) / C::BC, p.count = 1, p.slot = 0;
     } else {
-        const bool some = tree_part<C::BC, C::BR>(a, lane, blockIdx.x, target, most, least, slots, p);
+        const bool some = tree_part<C::BC, C::BR>(a, lane, blockIdx.x, target, most, least, gridDim.x, p);
         if (threadIdx.x == 0) parts.enter(p, some);
         if (!some) return;
     }
@@ -763,8 +763,8 @@ hipError_t launch_tree_bf16_main(const TreeArgs &a, const TreePlan &p, const bf1
 {
     const int n_tiles = (int)((int64_t)a.rows * (a.H / a.H_kv) / 128) + (a.B <= 64 && a.rows < a.B ? a.rows : a.B);
     TimedLaunch tl(K_TREE_BF16, st);
-    const dim3 grid((unsigned)(p.slots == 0 ? xcd_grid(a.H_kv, n_tiles) : (p.slots + 7) / 8 * 8)), block(256);
-    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, q, k_cache, v_cache, out, lse, scratch, n_tiles, p.target, p.most, p.least, p.slots, p.tiles); };
+    const dim3 grid((unsigned)(p.slots == 0 ? xcd_grid(a.H_kv, n_tiles) : (p.most + p.tiles + 7) / 8 * 8)), block(256);
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, q, k_cache, v_cache, out, lse, scratch, n_tiles, p.target, p.most, p.least, p.slots, p.chains); };
     if (a.d == 64) p.slots == 0 ? go(tree_bf16_kernel<64, true>) : go(tree_bf16_kernel<64, false>);
     else p.slots == 0 ? go(tree_bf16_kernel<128, true>) : go(tree_bf16_kernel<128, false>);
     return hipGetLastError();

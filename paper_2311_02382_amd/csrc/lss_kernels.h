@@ -208,10 +208,11 @@ size_t paged_tree_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, i
 template <typename T>
 hipError_t launch_paged_tree(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st);
 // How a call is run.  wide (bf16): workgroups of 128 rows by the packed forward's body (lss_fwd_bf16.hip), else of `rows` by the attention of one token's
-// (lss_decode.hip).  tiles of rows, at most; slots: parts that there are room for, `target` of them where the sequences are long, of `least` rounds at least; 0: a workgroup per tile of rows
+// (lss_decode.hip).  tiles of rows, at most; parts of their keys, `target` (or `most`) of them where the sequences are long, of `least` rounds at least.  slots: parts that scratch memory
+// has room for, of `chains` tiles that are cut (tree_part); 0: a workgroup per tile of rows, none is cut
 struct TreePlan {
     bool wide;
-    int rows, target, most, least, slots, tiles;
+    int rows, target, most, least, slots, chains, tiles;
 };
 // workgroups of the latter on a compute unit (with two sixteens of rows one less than there, or registers would go to scratch memory)
 constexpr int tree_per_cu(int elem_bytes, int d, int sixteens) { return d == 64 ? (sixteens == 1 ? 3 : 2) : elem_bytes == 2 && sixteens == 1 ? 2 : 1; }

@@ -199,12 +199,15 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b)
 }
 
 // ---- drafted tokens (lss_paged_attn_tree).  Sequence b has n_b G rows per head of keys and values, row r of them query head r % G of its drafted token r / G: tiles
-// of BR rows.  The rounds of a tile (ROUND keys each) are cut into parts of as many as it takes to have about `target` of all sequences together, at least LEAST; a
+// of BR rows.  The rounds of a tile (ROUND keys each) are cut into parts of as many as it takes to have about `target` of all sequences together, at least `least`; a
 // workgroup has one.
+// Only tiles that are cut need scratch memory and joining.  Their parts are of S rounds, S >= (all rounds) / target: a tile of R > S rounds has c < R / S + 1 < 2 R / S of them, so that all cut
+// tiles together have fewer than 2 target parts, and there are fewer than target of those tiles, whatever the number of rows, sequences and heads.
 struct TreePart {
     int b, h_kv, tile, tiles, begin, n, length;         // n: drafted tokens, from row `begin` on
-    int r0, r1, count, slot;                            // rounds; parts of the tile of rows, whose numbers are `tiles` apart; this one's
-    int item, items;                                    // which tile of rows of any head, of how many (the latter is set in any case)
+    int r0, r1, count, slot;                            // rounds; parts of the tile of rows, of several this one's number among those of all cut tiles: a tile's are `tiles` apart
+    int item, items;                                    // of several parts: which cut tile of rows of any head, of how many
+    int64_t all;                                        // parts of all tiles.  (This and items are set in any case)
 };
 __device__ __forceinline__ int64_t lane64(int64_t x, int lane)        // of that lane, wavefront-uniform
 {
@@ -221,8 +224,9 @@ __device__ __forceinline__ int64_t lanes_upto(int64_t x)
 // `most`: as many where as many more are resident at once, each of them slower; taken where parts become so much shorter that it is worth it.  d = 64, two and three workgroups
 // a compute unit: a round takes 17 twelfths as long, and a part some three rounds of its own (its start, its share of the joining launch).  24 sequences of 6000 tokens, 64
 // drafted: 85.4 us by 512, 69.1 by 768; 48 137.9 and 121.5; one of 36,000 with a chain of 256, whose tiles fill either: 64.4 and 68.6.
+// `room`: workgroups, target and a part for every tile of rows at least.
 template <int ROUND, int BR>
-__device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, int target, int most, int least, int slots, TreePart &p)
+__device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, int target, int most, int least, int room, TreePart &p)
 {
     const int G = a.H / a.H_kv;
     struct Some { int length, begin, n, tiles, R; };
@@ -241,19 +245,26 @@ __device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, i
     int all_tiles = __builtin_amdgcn_readlane(lane_sum_scan(s.tiles), 63);
     for (int b0 = 64; b0 < a.B; b0 += 64) {
         const Some t = load(b0);
-        rounds += lane64(lanes_upto((int64_t)t.tiles * t.R), 63);
+        // (no sum of rows that there are comes near the limit; starts that do not ascend may)
+        rounds = min(rounds + lane64(lanes_upto((int64_t)t.tiles * t.R), 63), (int64_t)1 << 46);
         all_tiles += __builtin_amdgcn_readlane(lane_sum_scan(t.tiles), 63);
     }
     const auto parts = [](const Some &t, int S) { return (int64_t)t.tiles * ((t.R + S - 1) / S); };
-    struct Fit { int S; int64_t mine, upto, all; };
+    const auto cut_tiles = [](const Some &t, int S) __attribute__((always_inline)) { return t.R > S ? t.tiles : 0; };
+    const auto last_of = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(x, 63); };
+    struct Fit { int S, behind; int64_t mine, upto, all; };     // behind: cut tiles of the sequences from number 64 on
     const auto fit = [&](int target) __attribute__((always_inline)) {
         Fit f;
         const int64_t wanted = divide(rounds * a.H_kv + target - 1, target);
         f.S = wanted < least ? least : wanted < 1 << 30 ? (int)wanted : 1 << 30;
         // (a part too many for the workgroups that there is room for at once waits for all of another: a few sizes are tried, where one part a tile fits)
         for (int tries = 0;; ++tries) {
-            f.mine = parts(s, f.S), f.upto = lanes_upto(f.mine), f.all = lane64(f.upto, 63);
-            for (int b0 = 64; b0 < a.B; b0 += 64) f.all += lane64(lanes_upto(parts(load(b0), f.S)), 63);
+            f.mine = parts(s, f.S), f.upto = lanes_upto(f.mine), f.all = lane64(f.upto, 63), f.behind = 0;
+            for (int b0 = 64; b0 < a.B; b0 += 64) {
+                const Some t = load(b0);
+                f.all += lane64(lanes_upto(parts(t, f.S)), 63);
+                f.behind += last_of(lane_sum_scan(cut_tiles(t, f.S)));
+            }
             if (f.all * a.H_kv <= target || (int64_t)all_tiles * a.H_kv > target || tries == 4 || f.S >= 1 << 24) break;
             const int64_t more = divide((f.all * a.H_kv - target) * f.S, target);
             f.S += more < 1 ? 1 : more < f.S ? (int)more : f.S;
@@ -268,21 +279,27 @@ __device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, i
     const int S = f.S;
     int64_t mine = f.mine, upto = f.upto, all = f.all;
     all *= a.H_kv;
-    p.items = all > slots ? 0 : all_tiles * a.H_kv;     // (more than there can be: cu does not ascend)
-    if (p.items == 0) return false;
+    int cut = cut_tiles(s, S), cut_upto = 0;
+    const bool some_cut = __any(cut != 0) || f.behind > 0;      // (where none is, nothing needs their numbers)
+    if (some_cut) cut_upto = lane_sum_scan(cut);
+    p.all = all;
+    p.items = (last_of(cut_upto) + f.behind) * a.H_kv;
+    if (all > room) return false;                       // (more than there can be: cu does not ascend)
     const int64_t per_xcd = (all + 7) / 8, at = id % 8 * per_xcd + id / 8;
     if (id / 8 >= per_xcd || at >= all) return false;
     const int64_t nth = divide(at, a.H_kv);             // (some sequence has it)
     int64_t before = 0;
-    int b0 = 0, tiles_before = 0;
+    int b0 = 0, cut_before = 0, slots_before = 0;
+    const auto slots_of = [](int64_t mine, int cut) __attribute__((always_inline)) { return cut ? (int)mine : 0; };
     while (before + lane64(upto, 63) <= nth) {
         before += lane64(upto, 63);
-        tiles_before += __builtin_amdgcn_readlane(lane_sum_scan(s.tiles), 63);
+        if (some_cut) cut_before += last_of(cut_upto), slots_before += last_of(lane_sum_scan(slots_of(mine, cut)));
         b0 += 64;
         if (b0 >= a.B) return false;
         s = load(b0);
         mine = parts(s, S);
         upto = lanes_upto(mine);
+        if (some_cut) cut = cut_tiles(s, S), cut_upto = lane_sum_scan(cut);
     }
     const int l = __ffsll((long long)__ballot(before + upto > nth)) - 1;
     const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
@@ -291,33 +308,37 @@ __device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, i
     p.h_kv = within / (tiles * c), p.tiles = tiles, p.tile = rest % tiles;
     const int part = rest / tiles, even = R / c, more_of = R - even * c;       // (as equal as they can be)
     p.count = c, p.r0 = part * even + min(part, more_of), p.r1 = p.r0 + even + (part < more_of);
-    p.slot = (int)at;
-    p.item = (tiles_before + of(lane_sum_scan(s.tiles) - s.tiles)) * a.H_kv + p.h_kv * tiles + p.tile;
+    p.slot = p.item = 0;
+    if (c > 1) {
+        const int slots = slots_of(mine, cut);
+        p.slot = (slots_before + of(lane_sum_scan(slots) - slots)) * a.H_kv + within;
+        p.item = (cut_before + of(cut_upto - cut)) * a.H_kv + p.h_kv * tiles + p.tile;
+    }
     return true;
 }
 // row of out and lse of row r of a sequence that begins with drafted token `begin`
 __device__ __forceinline__ int64_t tree_row(const TreeArgs &a, int begin, int G, int h_kv, int r) { return (int64_t)(begin + r / G) * a.H + h_kv * G + r % G; }
-// Scratch memory of `slots` parts, for those of tiles that have several: of each row sum of weight * value [d], maximum (log2 domain) and sum; and for the joining launch
-// how many tiles of rows there are, and where the parts of each begin (its first part says so).
+// Scratch memory of `slots` parts, for those of tiles that are cut: of each row sum of weight * value [d], maximum (log2 domain) and sum; and for the joining launch
+// how many such tiles of rows there are, `chains` at most, and where the parts of each begin (its first part says so).
 struct TreeChain { int b, h_kv, tile, first, count, tiles, unused[2]; };
 struct TreeScratch {
     float *base;
-    int rows, d, slots, tiles;
+    int rows, d, slots, chains;
     __device__ __forceinline__ int *items() const { return reinterpret_cast<int *>(base); }
     __device__ __forceinline__ TreeChain *chain(int i) const { return reinterpret_cast<TreeChain *>(base) + 1 + i; }
-    __device__ __forceinline__ float *sums(int part, int n) const { return base + 8 * (tiles + 1) + ((int64_t)part * rows + n) * 2; }
-    __device__ __forceinline__ float *values(int part, int n) const { return base + 8 * (tiles + 1) + (int64_t)slots * rows * 2 + ((int64_t)part * rows + n) * d; }
+    __device__ __forceinline__ float *sums(int part, int n) const { return base + 8 * (chains + 1) + ((int64_t)part * rows + n) * 2; }
+    __device__ __forceinline__ float *values(int part, int n) const { return base + 8 * (chains + 1) + (int64_t)slots * rows * 2 + ((int64_t)part * rows + n) * d; }
     // by one thread of each workgroup
     __device__ __forceinline__ void enter(const TreePart &p, bool some) const
     {
-        if (blockIdx.x == 0) *items() = p.items;
-        if (some && p.r0 == 0) *chain(p.item) = {p.b, p.h_kv, p.tile, p.slot, p.count, p.tiles, {0, 0}};
+        if (blockIdx.x == 0) *items() = p.all > gridDim.x ? 0 : p.items;
+        if (some && p.count > 1 && p.r0 == 0) *chain(p.item) = {p.b, p.h_kv, p.tile, p.slot, p.count, p.tiles, {0, 0}};
     }
 };
 // sum + factor * x, x a sum of weights times values and the factor what those weights are off by: above 0, but 0 in 32 bits where x's scores lie 2^7 or more (in powers of 2) below others.
 // 0 times a sum that is infinite would be NaN: such a one stays what it is.
 __device__ __forceinline__ float add_scaled(float factor, float x, float sum) { return fmaf(fabsf(x) < INFINITY ? factor : 1.f, x, sum); }
-inline size_t tree_scratch_bytes(int rows, int d, int slots, int tiles) { return sizeof(float) * (8 * ((size_t)tiles + 1) + (size_t)slots * rows * (d + 2)); }
+inline size_t tree_scratch_bytes(int rows, int d, int slots, int chains) { return sizeof(float) * (8 * ((size_t)chains + 1) + (size_t)slots * rows * (d + 2)); }
 // Which of the 32 keys from drafted number c0 on (below 0: the tokens in front of them) drafted token i of its sequence sees; `bits`: its words
 __device__ __forceinline__ uint32_t keys_seen(const TreeArgs &a, const uint64_t *bits, int i, int c0)
 {

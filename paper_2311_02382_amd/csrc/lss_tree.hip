@@ -7,18 +7,18 @@ namespace lss {
 
 namespace {
 
-// Joins the parts of tile of rows blockIdx.x, in their order: LANES lanes have a row, or in long chains S such groups with a part each, which meet in LDS.  What bounds it is a chain of
+// Joins the parts of cut tile of rows blockIdx.x, in their order: LANES lanes have a row, or in long chains S such groups with a part each, which meet in LDS.  What bounds it is a chain of
 // loads (where the parts are, whose rows, their sums and values): 5.7 us for 7 MB, 13 for 34.  Two groups for 5 to 8 parts: 16,016 rows of 6 parts of 64 8.7 us, four groups 11.6.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float *__restrict__ scratch, int rows, int slots, int most_tiles, T *__restrict__ out,
+__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float *__restrict__ scratch, int rows, int slots, int chains, T *__restrict__ out,
                                                          float *__restrict__ lse)
 {
     constexpr int LANES = D / 4, GROUPS = 256 / LANES, AHEAD = 4;
     __shared__ f32x4 acc[GROUPS][LANES];
     __shared__ float tops[GROUPS], totals[GROUPS];
-    const TreeScratch parts{const_cast<float *>(scratch), rows, D, slots, most_tiles};
+    const TreeScratch parts{const_cast<float *>(scratch), rows, D, slots, chains};
     const TreeChain chain = *parts.chain(blockIdx.x);   // (there is room for one of each workgroup)
-    if ((int)blockIdx.x >= *parts.items() || chain.count <= 1) return;
+    if ((int)blockIdx.x >= *parts.items()) return;
     const int G = a.H / a.H_kv, grp = threadIdx.x / LANES, lane = threadIdx.x % LANES;
     int begin, n_rows;
     queries_of(a, chain.b, begin, n_rows);
@@ -101,8 +101,8 @@ TreePlan pick(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem
     p.most = wide && d == 64 ? 768 : p.target;
     p.least = wide ? 6 : 2;
     p.tiles = (int)((in_a_head / p.rows + std::min<int64_t>(rows, B)) * H_kv);
-    p.slots = 0;
-    if (max_len > 512 && !(wide && p.tiles >= 768 && B <= 64)) p.slots = p.most + p.tiles;
+    p.slots = p.chains = 0;
+    if (max_len > 512 && !(wide && p.tiles >= 768 && B <= 64)) p.slots = 2 * p.most, p.chains = p.most;
     else p.least = 1 << 30;
     return p;
 }
@@ -112,7 +112,7 @@ TreePlan pick(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem
 size_t paged_tree_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem_bytes)
 {
     const TreePlan p = pick(rows, B, H, H_kv, d, max_len, elem_bytes);
-    return p.slots ? tree_scratch_bytes(p.rows, d, p.slots, p.tiles) : 0;
+    return p.slots ? tree_scratch_bytes(p.rows, d, p.slots, p.chains) : 0;
 }
 
 template <typename T>
@@ -128,9 +128,9 @@ hipError_t launch_paged_tree(const TreeArgs &a, const T *q, const T *k_cache, co
     }
     if (e != hipSuccess || p.slots == 0) return e;
     TimedLaunch tl(K_TREE_MERGE, st);
-    const dim3 grid((unsigned)p.tiles, (unsigned)std::min(p.rows, 32)), block(256);
-    if (a.d == 64) hipLaunchKernelGGL((tree_merge_kernel<T, 64>), grid, block, 0, st, a, scratch, p.rows, p.slots, p.tiles, out, lse);
-    else hipLaunchKernelGGL((tree_merge_kernel<T, 128>), grid, block, 0, st, a, scratch, p.rows, p.slots, p.tiles, out, lse);
+    const dim3 grid((unsigned)std::min(p.tiles, p.chains), (unsigned)std::min(p.rows, 32)), block(256);
+    if (a.d == 64) hipLaunchKernelGGL((tree_merge_kernel<T, 64>), grid, block, 0, st, a, scratch, p.rows, p.slots, p.chains, out, lse);
+    else hipLaunchKernelGGL((tree_merge_kernel<T, 128>), grid, block, 0, st, a, scratch, p.rows, p.slots, p.chains, out, lse);
     return hipGetLastError();
 }
 
