@@ -46,14 +46,14 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float
             top = higher;
             total *= alpha;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] = add_scaled(alpha, sum[e], 0.f);
+            for (int e = 0; e < 4; ++e) sum[e] *= alpha;
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 const float weight = i0 + j * S < chain.count ? fast_exp2(m[j] - use) : 0.f;
                 total += weight * l[j];
                 if (i0 + j * S < chain.count)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[e] = add_scaled(weight, v[j][e], sum[e]);
+                    for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, v[j][e], sum[e]);
             }
         }
         if (S > 1) {
@@ -71,10 +71,21 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float
                 const float weight = fast_exp2(tops[first + i] - use);
                 total += weight * totals[first + i];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[e] = add_scaled(weight, v[e], sum[e]);
+                for (int e = 0; e < 4; ++e) sum[e] = fmaf(weight, v[e], sum[e]);
             }
         }
         if (share != 0 || n0 + grp / S >= n_q) continue;
+        if (sum[0] != sum[0] || sum[1] != sum[1] || sum[2] != sum[2] || sum[3] != sum[3]) {
+            // (0 times infinity, or a NaN of its own: seldom; once more from the parts)
+            sum = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < chain.count; ++i) {
+                const int part = chain.first + i * chain.tiles;
+                const float weight = fast_exp2(parts.sums(part, n)[0] - (top == -INFINITY ? 0.f : top));
+                const f32x4 v = *reinterpret_cast<const f32x4 *>(parts.values(part, n) + 4 * lane);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] = add_scaled(weight, v[e], sum[e]);
+            }
+        }
         const int64_t row = tree_row(a, begin, G, chain.h_kv, chain.tile * rows + n);
         T *const to = out + row * D + 4 * lane;
 #pragma unroll
