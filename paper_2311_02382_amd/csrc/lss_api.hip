@@ -1017,7 +1017,7 @@ int lss_paged_attn_tree(const void *q, int64_t q_stride, const void *k_cache, co
     if (int rc = check_arrays(what, {lengths, block_table, cu_q, lse})) return rc;
     if (int rc = get_scratch(what, lss::paged_tree_workspace_bytes(rows, (int)B, (int)H, (int)H_kv, (int)d, (int)max_len, elem_bytes), &workspace, workspace_bytes)) return rc;
     if (int rc = check_apart(what, q, q_stride, out, rows, H, d, elem_bytes)) return rc;
-    const lss::TreeArgs a{pt, lengths, cu_q, reinterpret_cast<const uint64_t *>(tree), q_stride, (int)rows, tree ? (int)words : 0, (int)B, (int)H, (int)H_kv, (int)d, (int)max_len};
+    const lss::TreeArgs a{pt, lengths, cu_q, reinterpret_cast<const uint64_t *>(tree), q_stride, (int)rows, tree ? (int)words : 0, (int)B, (int)H, (int)H_kv, (int)d, (int)max_len, nullptr};
     const auto go = [&](auto zero) {
         typedef decltype(zero) T;
         return lss::launch_paged_tree<T>(a, static_cast<const T *>(q), static_cast<const T *>(k_cache), static_cast<const T *>(v_cache), static_cast<T *>(out), lse,

@@ -570,10 +570,20 @@ __global__ __launch_bounds__(64 * kWaves, tree_per_cu(sizeof(T), D, NQ)) void pa
     typedef Decode<T, D> C;
     __shared__ __attribute__((aligned(1024))) char smem[kWaves * C::REGION];
     __shared__ float sums[kWaves][2][16];
+    static_assert(C::ROUND == tree_round(sizeof(T), false), "");
+    const int lane = threadIdx.x & 63, G = a.H / a.H_kv;
     TreePart p;
-    const bool some = tree_part<C::ROUND, 16 * NQ>(a, threadIdx.x & 63, blockIdx.x, target, target, least, gridDim.x, p);
-    if (slots && threadIdx.x == 0) TreeScratch{scratch, 16 * NQ, D, slots, chains}.enter(p, some);
-    if (!some) return;
+    if (slots == 0 && a.B > 64) {
+        // no tile is cut: found like a packed one
+        int rank;
+        PackedTile t;
+        if (!xcd_item(blockIdx.x, a.H_kv, (int)((int64_t)a.rows * G / (16 * NQ)) + a.B, true, p.h_kv, rank) || !packed_tile<16 * NQ>(a, G, rank, lane, t)) return;
+        p.b = t.b, p.tile = t.tile, p.tiles = 1, p.begin = t.q_begin, p.n = t.n_q, p.length = t.n_k, p.r0 = 0, p.r1 = (max(1, t.n_k) + C::ROUND - 1) / C::ROUND, p.count = 1, p.slot = 0;
+    } else {
+        const bool some = tree_part<C::ROUND, 16 * NQ>(a, lane, blockIdx.x, target, target, least, gridDim.x, p);
+        if (slots && threadIdx.x == 0) TreeScratch{scratch, 16 * NQ, D, slots, chains}.enter(p, some);
+        if (!some) return;
+    }
     decode_rounds<T, D, NQ, false>(a, smem, sums, q, k_cache, v_cache, out, lse, scratch, true, 0, 1, 0, 0, p.b, 0, p.length, p, slots, chains);
 }
 
@@ -678,7 +688,8 @@ hipError_t launch_paged_decode(const DecodeArgs &a, const T *q, const T *k_cache
 template <typename T>
 hipError_t launch_tree_narrow(const TreeArgs &a, const TreePlan &p, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st)
 {
-    const dim3 grid((unsigned)(((p.slots ? p.most : 0) + p.tiles + 7) / 8 * 8)), block(64 * kWaves);
+    const int in_order = (int)((int64_t)a.rows * (a.H / a.H_kv) / p.rows) + a.B;       // (tiles that packed_tile numbers)
+    const dim3 grid((unsigned)(p.slots ? (p.most + p.tiles + 7) / 8 * 8 : a.B > 64 ? xcd_grid(a.H_kv, in_order) : (p.tiles + 7) / 8 * 8)), block(64 * kWaves);
     TimedLaunch tl(K_PAGED_TREE, st);
     const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, q, k_cache, v_cache, out, lse, scratch, p.target, p.least, p.slots, p.chains); };
     if (a.d == 64) p.rows == 16 ? go(paged_tree_kernel<T, 64, 1>) : go(paged_tree_kernel<T, 64, 2>);

@@ -716,6 +716,7 @@ __global__ __launch_bounds__(256, 2) void tree_bf16_kernel(TreeArgs a, const bf1
         if (!packed_tile<C::BR>(a, G, rank, lane, t)) return;
         p.b = t.b, p.tile = t.tile, p.begin = t.q_begin, p.n = t.n_q, p.length = t.n_k, p.r0 = 0, p.r1 = (t.n_k + C::BC - 1) / C::BC, p.count = 1, p.slot = 0;
     } else {
+        static_assert(C::BC == tree_round(2, true), "");
         const bool some = tree_part<C::BC, C::BR>(a, lane, blockIdx.x, target, most, least, gridDim.x, p);
         if (threadIdx.x == 0) parts.enter(p, some);
         if (!some) return;

@@ -112,7 +112,7 @@ enum KernelId { K_FWD_F32 = 0, K_FWD_MERGE, K_ROWDOT, K_BWD_MAIN_F32, K_DQ_MERGE
                 K_PE_FWD, K_PE_BWD, K_LN_FWD, K_LN_BWD, K_LN_PARAMS, K_GELU_FWD, K_GELU_BWD, K_LINEAR_FWD, K_LINEAR_BWD, K_RESIDUAL, K_LINEAR_WGRAD,
                 K_FWD_BF16, K_BWD_PREP_BF16, K_BWD_SKINNY_BF16, K_LN_BWD_SHORT, K_PROJ_FWD_SMALL, K_PROJ_BWD_SMALL, K_LINEAR_FWD_SMALL,
                 K_LINEAR_BWD_SMALL, K_PAGED_APPEND, K_PAGED_DECODE, K_DECODE_MERGE, K_PACKED_BF16, K_PACKED_F32, K_PACKED_MERGE, K_PAGED_TREE, K_FORK_CLEAR,
-                K_FORK_TABLE, K_FORK_PLAN, K_FORK_COPY, K_PAGED_COMPACT, K_BEAM_ROWS, K_BEAM_SELECT, K_TREE_BF16, K_TREE_MERGE, K_FORK_SMALL, K_COUNT };
+                K_FORK_TABLE, K_FORK_PLAN, K_FORK_COPY, K_PAGED_COMPACT, K_BEAM_ROWS, K_BEAM_SELECT, K_TREE_BF16, K_TREE_MERGE, K_FORK_SMALL, K_TREE_COUNT, K_COUNT };
 void timing_begin(int id, hipStream_t st);
 void timing_end(int id, hipStream_t st);
 struct TimedLaunch {    // RAII bracket around one kernel launch
@@ -197,12 +197,14 @@ size_t paged_decode_workspace_bytes(int H, int H_kv, int d, int max_len);
 template <typename T>
 hipError_t launch_paged_decode(const DecodeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st);
 // several continuations of a sequence (lss_tree.hip, lss_pages.hip, lss_beam.hip)
+struct TreeCount;
 struct TreeArgs {
     PageTable pt;
     const int32_t *lengths, *cu;        // cu [B + 1]
     const uint64_t *tree;               // [rows, words] of bits; null: a drafted token sees those in front of it
     int64_t q_stride;
     int rows, words, B, H, H_kv, d, max_len;
+    const TreeCount *count;             // of many sequences, what the launch in front found (tree_part); null: few
 };
 size_t paged_tree_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem_bytes);
 template <typename T>
@@ -211,9 +213,10 @@ hipError_t launch_paged_tree(const TreeArgs &a, const T *q, const T *k_cache, co
 // (lss_decode.hip).  tiles of rows, at most; parts of their keys, `target` (or `most`) of them where the sequences are long, of `least` rounds at least.  slots: parts that scratch memory
 // has room for, of `chains` tiles that are cut (tree_part); 0: a workgroup per tile of rows, none is cut
 struct TreePlan {
-    bool wide;
+    bool wide, counted;         // counted: by a launch in front (tree_count_kernel)
     int rows, target, most, least, slots, chains, tiles;
 };
+constexpr int tree_round(int elem_bytes, bool wide) { return wide || elem_bytes == 4 ? 64 : 128; }     // keys
 // workgroups of the latter on a compute unit (with two sixteens of rows one less than there, or registers would go to scratch memory)
 constexpr int tree_per_cu(int elem_bytes, int d, int sixteens) { return d == 64 ? (sixteens == 1 ? 3 : 2) : elem_bytes == 2 && sixteens == 1 ? 2 : 1; }
 hipError_t launch_tree_bf16_main(const TreeArgs &a, const TreePlan &p, const bf16_t *q, const bf16_t *k_cache, const bf16_t *v_cache, bf16_t *out, float *lse, float *scratch,

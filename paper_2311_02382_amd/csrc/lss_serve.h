@@ -219,77 +219,118 @@ __device__ __forceinline__ int64_t lanes_upto(int64_t x)
     const int low = lane_sum_scan((int)(x & 0xffffff)), high = lane_sum_scan((int)(x >> 24));
     return ((int64_t)high << 24) + low;
 }
+// A sequence's tiles of BR rows and rounds of ROUND keys; none from number B on
+struct TreeSequence { int length, begin, n, tiles, R; };
+__device__ __forceinline__ TreeSequence tree_sequence(const TreeArgs &a, int G, int round, int rows, int b)
+{
+    TreeSequence s{0, 0, 0, 0, 0};
+    if (b < a.B) {
+        s.length = max(0, min(a.lengths[b], a.max_len));
+        queries_of(a, b, s.begin, s.n);
+    }
+    s.tiles = (s.n * G + rows - 1) / rows;              // (rows * H <= 2^24)
+    s.R = (max(1, s.length) + round - 1) / round;
+    return s;
+}
+__device__ __forceinline__ int64_t parts_of_tiles(const TreeSequence &s, int S) { return (int64_t)s.tiles * ((s.R + S - 1) / S); }
+__device__ __forceinline__ int cut_tiles(const TreeSequence &s, int S) { return s.R > S ? s.tiles : 0; }
+// Rounds of a part.  parts(S): how many parts of S rounds there are per head.  (A part too many for the workgroups that there is room for at once waits for all of another: a few sizes are
+// tried, where one part a tile fits.)
+template <typename F> __device__ __forceinline__ int part_rounds(int64_t rounds, int64_t all_tiles, int H_kv, int target, int least, F &&parts)
+{
+    const int64_t wanted = divide(rounds * H_kv + target - 1, target);
+    int S = wanted < least ? least : wanted < 1 << 30 ? (int)wanted : 1 << 30;
+    for (int tries = 0;; ++tries) {
+        const int64_t all = parts(S);
+        if (all * H_kv <= target || all_tiles * H_kv > target || tries == 4 || S >= 1 << 24) return S;
+        const int64_t more = divide((all * H_kv - target) * S, target);
+        S += more < 1 ? 1 : more < S ? (int)more : S;
+    }
+}
+// Are parts of S_most rounds, `most` of them, worth it where `target` of S rounds are the rule?  Where as many more are resident at once, each of them slower, and parts become so much shorter.
+// d = 64, two and three workgroups a compute unit: a round takes 17 twelfths as long, and a part some three rounds of its own (its start, its share of the joining launch).  24 sequences of 6000
+// tokens, 64 drafted: 85.4 us by 512, 69.1 by 768; 48 137.9 and 121.5; one of 36,000 with a chain of 256, whose tiles fill either: 64.4 and 68.6.
+__device__ __forceinline__ bool worth_more(int S, int S_most) { return (int64_t)17 * S_most + 36 < (int64_t)12 * S; }
+// Many sequences: every workgroup would go over all of them to find its part -- 2048 of one token, 8 heads of keys, 1.3 ms, 4096 4.4 --, so that a launch in front does it once
+// (tree_count_kernel) and says per 64 sequences what is in front of them.
+struct TreeCount { int64_t all; int S, cut; };          // per head of keys: parts, rounds of one, cut tiles
+struct TreeBatch { int64_t before; int cut, slots; };   // per head of keys, of the sequences in front: parts, cut tiles, parts of these
+inline size_t tree_count_bytes(int B) { return sizeof(TreeCount) + (size_t)((B + 63) / 64) * sizeof(TreeBatch); }
+
 // Workgroup `id`'s part; false: there is none.  Parts are numbered by sequence, head, part of the keys and tile of rows, and each XCD (workgroups go to them in turn) has a run
 // of them: tiles of rows that read the same keys do so at the same time from one L2.  All lanes active; wavefront-uniform.
-// `most`: as many where as many more are resident at once, each of them slower; taken where parts become so much shorter that it is worth it.  d = 64, two and three workgroups
-// a compute unit: a round takes 17 twelfths as long, and a part some three rounds of its own (its start, its share of the joining launch).  24 sequences of 6000 tokens, 64
-// drafted: 85.4 us by 512, 69.1 by 768; 48 137.9 and 121.5; one of 36,000 with a chain of 256, whose tiles fill either: 64.4 and 68.6.
 // `room`: workgroups, target and a part for every tile of rows at least.
 template <int ROUND, int BR>
 __device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, int target, int most, int least, int room, TreePart &p)
 {
     const int G = a.H / a.H_kv;
-    struct Some { int length, begin, n, tiles, R; };
-    const auto load = [&](int b0) __attribute__((always_inline)) {
-        Some s{0, 0, 0, 0, 0};
-        if (b0 + lane < a.B) {
-            s.length = max(0, min(a.lengths[b0 + lane], a.max_len));
-            queries_of(a, b0 + lane, s.begin, s.n);
-        }
-        s.tiles = (s.n * G + BR - 1) / BR;              // (rows * H <= 2^24)
-        s.R = (max(1, s.length) + ROUND - 1) / ROUND;
-        return s;
-    };
-    Some s = load(0);
-    int64_t rounds = lane64(lanes_upto((int64_t)s.tiles * s.R), 63);
-    int all_tiles = __builtin_amdgcn_readlane(lane_sum_scan(s.tiles), 63);
-    for (int b0 = 64; b0 < a.B; b0 += 64) {
-        const Some t = load(b0);
-        // (no sum of rows that there are comes near the limit; starts that do not ascend may)
-        rounds = min(rounds + lane64(lanes_upto((int64_t)t.tiles * t.R), 63), (int64_t)1 << 46);
-        all_tiles += __builtin_amdgcn_readlane(lane_sum_scan(t.tiles), 63);
-    }
-    const auto parts = [](const Some &t, int S) { return (int64_t)t.tiles * ((t.R + S - 1) / S); };
-    const auto cut_tiles = [](const Some &t, int S) __attribute__((always_inline)) { return t.R > S ? t.tiles : 0; };
+    const auto load = [&](int b0) __attribute__((always_inline)) { return tree_sequence(a, G, ROUND, BR, b0 + lane); };
     const auto last_of = [](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(x, 63); };
-    struct Fit { int S, behind; int64_t mine, upto, all; };     // behind: cut tiles of the sequences from number 64 on
-    const auto fit = [&](int target) __attribute__((always_inline)) {
-        Fit f;
-        const int64_t wanted = divide(rounds * a.H_kv + target - 1, target);
-        f.S = wanted < least ? least : wanted < 1 << 30 ? (int)wanted : 1 << 30;
-        // (a part too many for the workgroups that there is room for at once waits for all of another: a few sizes are tried, where one part a tile fits)
-        for (int tries = 0;; ++tries) {
-            f.mine = parts(s, f.S), f.upto = lanes_upto(f.mine), f.all = lane64(f.upto, 63), f.behind = 0;
-            for (int b0 = 64; b0 < a.B; b0 += 64) {
-                const Some t = load(b0);
-                f.all += lane64(lanes_upto(parts(t, f.S)), 63);
-                f.behind += last_of(lane_sum_scan(cut_tiles(t, f.S)));
-            }
-            if (f.all * a.H_kv <= target || (int64_t)all_tiles * a.H_kv > target || tries == 4 || f.S >= 1 << 24) break;
-            const int64_t more = divide((f.all * a.H_kv - target) * f.S, target);
-            f.S += more < 1 ? 1 : more < f.S ? (int)more : f.S;
-        }
-        return f;
+    TreeSequence s;
+    int S, cut, cut_upto = 0, b0 = 0, cut_before = 0, slots_before = 0;
+    int64_t mine, upto, before = 0, at, nth;
+    bool some_cut;                                      // (where none is, nothing needs their numbers)
+    const auto find = [&](int64_t all) __attribute__((always_inline)) {
+        p.all = all * a.H_kv;
+        if (p.all > room) return false;                 // (more than there can be: cu does not ascend)
+        const int64_t per_xcd = (p.all + 7) / 8;
+        at = id % 8 * per_xcd + id / 8;
+        nth = divide(at, a.H_kv);                       // (some sequence has it)
+        return id / 8 < per_xcd && at < p.all;
     };
-    Fit f = fit(target);
-    if (most > target && rounds * a.H_kv >= (int64_t)20 * most) {
-        const Fit g = fit(most);
-        if ((int64_t)17 * g.S + 36 < (int64_t)12 * f.S) f = g;
+    if (a.count) {
+        const TreeCount c = *a.count;
+        const TreeBatch *const batches = reinterpret_cast<const TreeBatch *>(a.count + 1);
+        S = c.S;
+        some_cut = c.cut > 0;
+        p.items = c.cut * a.H_kv;
+        if (!find(c.all)) return false;
+        int lo = 0, n = (a.B + 63) / 64;                // the last batch that begins with part nth or in front of it: 64 tried at a time
+        while (n > 1) {
+            const int step = (n + 63) / 64, i = lane * step;
+            const uint64_t below = __ballot(i < n && batches[lo + min(i, n - 1)].before <= nth);
+            const int last = 63 - __clzll((long long)(below | 1));
+            lo += last * step;
+            n = min(step, n - last * step);
+        }
+        const TreeBatch batch = batches[lo];
+        b0 = 64 * lo, before = batch.before, cut_before = batch.cut, slots_before = batch.slots;
+        s = load(b0);
+        mine = parts_of_tiles(s, S), upto = lanes_upto(mine), cut = cut_tiles(s, S);
+        if (some_cut) cut_upto = lane_sum_scan(cut);
+    } else {
+        s = load(0);
+        int64_t rounds = lane64(lanes_upto((int64_t)s.tiles * s.R), 63);
+        int all_tiles = last_of(lane_sum_scan(s.tiles));
+        for (int i = 64; i < a.B; i += 64) {
+            const TreeSequence t = load(i);
+            rounds += lane64(lanes_upto((int64_t)t.tiles * t.R), 63);
+            all_tiles += last_of(lane_sum_scan(t.tiles));
+        }
+        int64_t all;
+        int behind;                                     // cut tiles of the sequences from number 64 on
+        const auto parts = [&](int S) __attribute__((always_inline)) {
+            mine = parts_of_tiles(s, S), upto = lanes_upto(mine), all = lane64(upto, 63), behind = 0;
+            for (int i = 64; i < a.B; i += 64) {
+                const TreeSequence t = load(i);
+                all += lane64(lanes_upto(parts_of_tiles(t, S)), 63);
+                behind += last_of(lane_sum_scan(cut_tiles(t, S)));
+            }
+            return all;
+        };
+        S = part_rounds(rounds, all_tiles, a.H_kv, target, least, parts);
+        if (most > target && rounds * a.H_kv >= (int64_t)20 * most) {
+            const int64_t mine_of = mine, upto_of = upto, all_of = all;
+            const int behind_of = behind, S_most = part_rounds(rounds, all_tiles, a.H_kv, most, least, parts);
+            if (worth_more(S, S_most)) S = S_most;
+            else mine = mine_of, upto = upto_of, all = all_of, behind = behind_of;
+        }
+        cut = cut_tiles(s, S);
+        some_cut = __any(cut != 0) || behind > 0;
+        if (some_cut) cut_upto = lane_sum_scan(cut);
+        p.items = (last_of(cut_upto) + behind) * a.H_kv;
+        if (!find(all)) return false;
     }
-    const int S = f.S;
-    int64_t mine = f.mine, upto = f.upto, all = f.all;
-    all *= a.H_kv;
-    int cut = cut_tiles(s, S), cut_upto = 0;
-    const bool some_cut = __any(cut != 0) || f.behind > 0;      // (where none is, nothing needs their numbers)
-    if (some_cut) cut_upto = lane_sum_scan(cut);
-    p.all = all;
-    p.items = (last_of(cut_upto) + f.behind) * a.H_kv;
-    if (all > room) return false;                       // (more than there can be: cu does not ascend)
-    const int64_t per_xcd = (all + 7) / 8, at = id % 8 * per_xcd + id / 8;
-    if (id / 8 >= per_xcd || at >= all) return false;
-    const int64_t nth = divide(at, a.H_kv);             // (some sequence has it)
-    int64_t before = 0;
-    int b0 = 0, cut_before = 0, slots_before = 0;
     const auto slots_of = [](int64_t mine, int cut) __attribute__((always_inline)) { return cut ? (int)mine : 0; };
     while (before + lane64(upto, 63) <= nth) {
         before += lane64(upto, 63);
@@ -297,12 +338,11 @@ __device__ __forceinline__ bool tree_part(const TreeArgs &a, int lane, int id, i
         b0 += 64;
         if (b0 >= a.B) return false;
         s = load(b0);
-        mine = parts(s, S);
-        upto = lanes_upto(mine);
+        mine = parts_of_tiles(s, S), upto = lanes_upto(mine);
         if (some_cut) cut = cut_tiles(s, S), cut_upto = lane_sum_scan(cut);
     }
     const int l = __ffsll((long long)__ballot(before + upto > nth)) - 1;
-    const auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+    const auto of = [&](int x) __attribute__((always_inline)) { return __builtin_amdgcn_readlane(x, l); };
     const int R = of(s.R), tiles = of(s.tiles), c = (R + S - 1) / S, within = (int)(at - (before + lane64(upto - mine, l)) * a.H_kv), rest = within % (tiles * c);
     p.b = b0 + l, p.begin = of(s.begin), p.n = of(s.n), p.length = of(s.length);
     p.h_kv = within / (tiles * c), p.tiles = tiles, p.tile = rest % tiles;

@@ -32,7 +32,8 @@ const char *const kNames[K_COUNT] = {"fwd_f32_kernel", "fwd_merge_kernel", "bwd_
                                      "bwd_skinny_bf16_kernel", "layernorm_bwd_short_kernel", "proj_small_gemm_kernel:project_qkv",
                                      "proj_small_gemm_kernel:project_bwd", "proj_small_gemm_kernel:linear_fwd", "proj_small_gemm_kernel:linear_bwd_input", "paged_append_kernel", "paged_decode_kernel", "decode_merge_kernel",
                                      "packed_bf16_kernel", "packed_f32_kernel", "packed_merge_kernel", "paged_tree_kernel", "fork_clear_kernel",
-                                     "fork_table_kernel", "fork_plan_kernel", "fork_copy_kernel", "paged_compact_kernel", "beam_rows_kernel", "beam_select_kernel", "tree_bf16_kernel", "tree_merge_kernel", "fork_small_kernel"};
+                                     "fork_table_kernel", "fork_plan_kernel", "fork_copy_kernel", "paged_compact_kernel", "beam_rows_kernel", "beam_select_kernel", "tree_bf16_kernel", "tree_merge_kernel", "fork_small_kernel",
+                                     "tree_count_kernel"};
 
 hipEvent_t get_event()
 {

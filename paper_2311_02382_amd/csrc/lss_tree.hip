@@ -7,6 +7,52 @@ namespace lss {
 
 namespace {
 
+// Many sequences, by one workgroup: the size of a part, and what is in front of every 64 of them.  What bounds it is latency, four or five passes over the sequences, each loads and a sum over the
+// workgroup: of 320 7.3 us, 1024 8.5, 4096 18, 65,536 209 (where the main launch takes 73, 216, 822 and 12,950).
+constexpr int kCountThreads = 1024, kCountWaves = kCountThreads / 64;
+__global__ __launch_bounds__(kCountThreads) void tree_count_kernel(TreeArgs a, int round, int rows, int target, int most, int least, TreeCount *__restrict__ count)
+{
+    __shared__ int64_t sums[kCountWaves];
+    __shared__ int cuts[kCountWaves], slots[kCountWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, G = a.H / a.H_kv;
+    const int64_t limit = (int64_t)1 << 46;             // (no sum of rows that there are comes near it; starts that do not ascend may)
+    const auto sum_of = [&](auto &&of) __attribute__((always_inline)) {
+        int64_t sum = 0;
+        for (int b = tid; b < a.B; b += kCountThreads) sum = min(sum + of(tree_sequence(a, G, round, rows, b)), limit);
+        sum = lane64(lanes_upto(sum), 63);
+        __syncthreads();
+        if (lane == 0) sums[wave] = sum;
+        __syncthreads();
+        sum = 0;
+        for (int w = 0; w < kCountWaves; ++w) sum = min(sum + sums[w], limit);
+        return sum;
+    };
+    const int64_t rounds = sum_of([](const TreeSequence &s) { return (int64_t)s.tiles * s.R; }), all_tiles = sum_of([](const TreeSequence &s) { return (int64_t)s.tiles; });
+    const auto parts = [&](int S) { return sum_of([&](const TreeSequence &s) { return parts_of_tiles(s, S); }); };
+    int S = part_rounds(rounds, all_tiles, a.H_kv, target, least, parts);
+    if (most > target && rounds * a.H_kv >= (int64_t)20 * most) {
+        const int S_most = part_rounds(rounds, all_tiles, a.H_kv, most, least, parts);
+        if (worth_more(S, S_most)) S = S_most;
+    }
+    TreeBatch *const batches = reinterpret_cast<TreeBatch *>(count + 1);
+    TreeBatch before{0, 0, 0};
+    for (int b0 = 0; b0 < a.B; b0 += kCountThreads) {
+        const TreeSequence s = tree_sequence(a, G, round, rows, b0 + tid);
+        const int64_t mine = parts_of_tiles(s, S);
+        const int cut = cut_tiles(s, S);
+        const int64_t all = lane64(lanes_upto(mine), 63);
+        const int all_cut = __builtin_amdgcn_readlane(lane_sum_scan(cut), 63), all_slots = __builtin_amdgcn_readlane(lane_sum_scan(cut ? (int)mine : 0), 63);
+        __syncthreads();
+        if (lane == 0) sums[wave] = all, cuts[wave] = all_cut, slots[wave] = all_slots;
+        __syncthreads();
+        for (int w = 0; w < kCountWaves; ++w) {
+            if (w == wave && lane == 0 && b0 + 64 * w < a.B) batches[b0 / 64 + w] = before;
+            before.before += sums[w], before.cut += cuts[w], before.slots += slots[w];
+        }
+    }
+    if (tid == 0) *count = {before.before, S, before.cut};
+}
+
 // Joins the parts of cut tile of rows blockIdx.x, in their order: LANES lanes have a row, or in long chains S such groups with a part each, which meet in LDS.  What bounds it is a chain of
 // loads (where the parts are, whose rows, their sums and values): 5.7 us for 7 MB, 13 for 34.  Two groups for 5 to 8 parts: 16,016 rows of 6 parts of 64 8.7 us, four groups 11.6.
 template <typename T, int D>
@@ -101,6 +147,9 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float
 //     as many again 52; d = 64, 24 sequences with 8: 17.7, parts of 512 keys 18.7, of 768 21, of 1024 24.
 //   * Lengths up to 512, or many tiles of up to 64 sequences (which then start with the longest): a tile each and no joining launch.  48 x 64 drafted tokens, 768 tiles: 268,
 //     in parts 310.
+//   * Counted in front from 257 sequences on.  Of one token, 8 heads of keys, 20 to 700 tokens: 192 sequences 55.7 us without that launch and 59.0 with it, 256 70.0 and 71.1, 320 89.2 and 84.3,
+//     2048 1365 and 436.  (Where no tile is cut, sequences past the 64th are found among their starts, and nothing is counted: 65 21.6 -> 16.9.)
+constexpr int kListed = 256;
 TreePlan pick(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem_bytes)
 {
     const int64_t in_a_head = rows * (H / H_kv);
@@ -112,8 +161,9 @@ TreePlan pick(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem
     p.most = wide && d == 64 ? 768 : p.target;
     p.least = wide ? 6 : 2;
     p.tiles = (int)((in_a_head / p.rows + std::min<int64_t>(rows, B)) * H_kv);
+    p.counted = false;
     p.slots = p.chains = 0;
-    if (max_len > 512 && !(wide && p.tiles >= 768 && B <= 64)) p.slots = 2 * p.most, p.chains = p.most;
+    if (max_len > 512 && !(wide && p.tiles >= 768 && B <= 64)) p.slots = 2 * p.most, p.chains = p.most, p.counted = B > kListed;
     else p.least = 1 << 30;
     return p;
 }
@@ -123,13 +173,21 @@ TreePlan pick(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem
 size_t paged_tree_workspace_bytes(int64_t rows, int B, int H, int H_kv, int d, int max_len, int elem_bytes)
 {
     const TreePlan p = pick(rows, B, H, H_kv, d, max_len, elem_bytes);
-    return p.slots ? tree_scratch_bytes(p.rows, d, p.slots, p.chains) : 0;
+    return (p.counted ? tree_count_bytes(B) : 0) + (p.slots ? tree_scratch_bytes(p.rows, d, p.slots, p.chains) : 0);
 }
 
 template <typename T>
-hipError_t launch_paged_tree(const TreeArgs &a, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st)
+hipError_t launch_paged_tree(const TreeArgs &args, const T *q, const T *k_cache, const T *v_cache, T *out, float *lse, float *scratch, hipStream_t st)
 {
+    TreeArgs a = args;
     const TreePlan p = pick(a.rows, a.B, a.H, a.H_kv, a.d, a.max_len, sizeof(T));
+    if (p.counted) {
+        TreeCount *const count = reinterpret_cast<TreeCount *>(scratch);
+        TimedLaunch tl(K_TREE_COUNT, st);
+        hipLaunchKernelGGL(tree_count_kernel, dim3(1), dim3(kCountThreads), 0, st, a, tree_round(sizeof(T), p.wide), p.rows, p.target, p.most, p.least, count);
+        a.count = count;
+        scratch += tree_count_bytes(a.B) / sizeof(float);
+    }
     hipError_t e = hipSuccess;
     if constexpr (sizeof(T) == 2) {
         if (p.wide) e = launch_tree_bf16_main(a, p, q, k_cache, v_cache, out, lse, scratch, st);

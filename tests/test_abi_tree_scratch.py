@@ -26,7 +26,7 @@ def test_scratch_is_bounded(need, d, eb):
             assert size == 0
             continue
         tried += 1
-        assert size <= most, (rows, B, H, H_kv, max_len, size)
+        assert size <= most + 16 * (B // 64 + 2), (rows, B, H, H_kv, max_len, size)       # (and what is in front of every 64 sequences)
         assert size % 16 == 0
     assert tried > 200
 

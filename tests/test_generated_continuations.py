@@ -20,4 +20,4 @@ def test_no_kernel_keeps_a_register_in_scratch_memory(code):
         for name, size, dynamic in re.findall(r"\.amdhsa_kernel (\S+).*?\.amdhsa_private_segment_fixed_size (\d+).*?\.amdhsa_uses_dynamic_stack (\d)", text, re.S):
             seen += 1
             assert (size, dynamic) == ("0", "0"), (source, name, size, dynamic)
-    assert seen == 16
+    assert seen >= 16
