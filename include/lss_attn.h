@@ -511,6 +511,7 @@ int lss_packed_attn_fwd(const void *q, int64_t q_stride, const void *k, int64_t 
  * not touched.  rows * H <= 2^24, B * H_kv <= 2^22, words <= 1024 (LSS_ERR_SHAPE otherwise).
  * bf16: with up to 16 rows per head of keys in a sequence (on average) a weight enters the product with the values as two parts, off by 2^-16, else rounded to bf16, off by
  * 2^-8.  An infinite value of a drafted token reaches all rows that see it, however small its weight; one in front of the drafted tokens at a weight below 2^-126 may give NaN.
+ * (Values of drafted tokens that are not finite cost time: 48 x 64 drafted a third more, a chain of 1000 4 times as long, of 8000 26 times.)
  */
 size_t lss_paged_attn_tree_workspace_bytes(int64_t rows, int64_t B, int64_t H, int64_t H_kv, int64_t d, int64_t max_len, int elem_bytes);
 int lss_paged_attn_tree(const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,

@@ -9,7 +9,7 @@
 //
 // What bounds them: long rows by vector issue (an exponential, a conversion, a product, a sum and half a maximum a logit): 256 rows of 128,256 in bf16, 66 MB, 18 to 19 us, 3.5 TB/s,
 // the vector ALU busy 59 % of the cycles, loads alone 12.1; short ones by latency (64 rows of 32,001: 6 us).  The second launch is 7 to 10 us of steps one behind the other: lists, a bound, totals,
-// ranking.  All of it, 32 prompts x 8 beams of 128,256: 25.6 us; 8 x 8 of 32,001, 16 chosen, 15.2; 4 beams of 256 6.3.
+// ranking.  All of it, 32 prompts x 8 beams of 128,256: 25.9 us; 8 x 8 of 32,001, 16 chosen, 15.0; 4 beams of 256 6.4.
 #include "lss_serve.h"
 
 #include <algorithm>

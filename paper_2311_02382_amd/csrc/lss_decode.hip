@@ -561,7 +561,7 @@ __global__ __launch_bounds__(64 * kWaves, parts_of(sizeof(T), D, NQ) / 256) void
 }
 
 // Drafted tokens: the same rounds of a part of a tile of rows (tree_part); slots = 0: of all of it.  Weights enter in two parts, as above.  Bound by latency and by memory: 5 rows behind 77 tokens
-// 5.4 us, one round; float, 8 heads of 64, 35 MB: 12.4 (2.9 TB/s) and 4.4 of joining; bf16, 24 sequences of 2 drafted tokens, 32 heads of 128, 8 of keys, 112 MB: 27 (4.1 TB/s).
+// 5.7 us, one round; float, 8 heads of 64, 35 MB: 12.0 to 12.6 (2.9 TB/s) and 4.8 of joining; bf16, 24 sequences of 2 drafted tokens, 32 heads of 128, 8 of keys, 112 MB: 27 (4.1 TB/s).
 template <typename T, int D, int NQ>
 __global__ __launch_bounds__(64 * kWaves, tree_per_cu(sizeof(T), D, NQ)) void paged_tree_kernel(TreeArgs a, const T *__restrict__ q, const T *__restrict__ k_cache,
                                                                     const T *__restrict__ v_cache, T *__restrict__ out, float *__restrict__ lse,

@@ -694,9 +694,9 @@ __global__ __launch_bounds__(64 * RB * KG, D == 64 ? 2 : 1) void packed_bf16_ker
 
 // Drafted tokens over a paged cache (lss_paged_attn_tree): rows as above, keys and values from pages.
 // WHOLE: a workgroup per tile of 128 rows, those with the most keys first; else per part of a tile's keys (tree_part), joined by a second launch.
-//   48 sequences of 2048 to 6500 tokens, 64 drafted, 32 heads of 128, 8 of keys, 951 MB, 2.1e11 flop: 268 to 284 us, 780 TFLOP/s, matrix units busy 45 % and vector ALU 41 % of the cycles: a SIMD's two
-// wavefronts take turns, as over contiguous keys (261).  1001 rows of a chain behind 22,000 tokens, 16 heads of 64, 4 of keys: 135 us, vector ALU 69 %.  24 sequences of up to 8192, trees of 4 to 12,
-// 112 MB: 30.6 us, 3.9 TB/s, 9 of them until the first tile is there.  Weights are rounded to bf16 (off by at most 2^-8 of each), as for packed prompts.
+//   48 sequences of 2048 to 6500 tokens, 64 drafted, 32 heads of 128, 8 of keys, 917 MB, 2.1e11 flop: 266 to 284 us by box, 780 TFLOP/s, matrix units busy 45 % and vector ALU 41 % of the cycles: a SIMD's two
+// wavefronts take turns, as over contiguous keys (261).  1001 rows of a chain behind 23,000 tokens, 16 heads of 64, 4 of keys: 128 to 131 us, vector ALU 68 %.  24 sequences of up to 8192, trees of 4 to 12,
+// 112 MB: 30.7 us, 3.9 TB/s, 9 of them until the first tile is there.  Weights are rounded to bf16 (off by at most 2^-8 of each), as for packed prompts.
 template <int D, bool WHOLE>
 __global__ __launch_bounds__(256, 2) void tree_bf16_kernel(TreeArgs a, const bf16_t *__restrict__ q, const bf16_t *__restrict__ k_cache,
                                                           const bf16_t *__restrict__ v_cache, bf16_t *__restrict__ out, float *__restrict__ lse,

@@ -5,7 +5,7 @@
 // into it.  Marks commute, so the order in which they arrive does not matter.  A sequence whose partly filled page is not its own by that takes a new one and the
 // tokens in it.  New pages are the lowest free numbers, in the order of (sequence, page).
 //   What bounds it is latency: four launches, each of which needs all that the one before wrote.  384 sequences of 48 prompts of 300 to 6000 tokens, 21.5 MB copied (8 heads of 128): 21.9 us, the
-// marks' array cleared in 2.1, tables 6.1, plan 6.3, copies 7.5 (2.9 TB/s).  Few sequences, pages and entries take one workgroup and LDS for the first three: four beams 7.7 us, by all four
+// marks' array cleared in 1.3 to 2.1, tables 6.1, plan 6.3, copies 7.0 to 7.5 (3 TB/s).  Few sequences, pages and entries take one workgroup and LDS for the first three: four beams 7.7 us, by all four
 // launches 15.5.
 #include "lss_serve.h"
 

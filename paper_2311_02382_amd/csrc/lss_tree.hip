@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kCountThreads) void tree_count_kernel(TreeArgs a, i
 }
 
 // Joins the parts of cut tile of rows blockIdx.x, in their order: LANES lanes have a row, or in long chains S such groups with a part each, which meet in LDS.  What bounds it is a chain of
-// loads (where the parts are, whose rows, their sums and values): 5.7 us for 7 MB, 13 for 34.  Two groups for 5 to 8 parts: 16,016 rows of 6 parts of 64 8.7 us, four groups 11.6.
+// loads (where the parts are, whose rows, their sums and values): 5.7 us for 7 MB, 8.2 for 26 (16,016 rows of 6 parts of 64; there two groups, four took 11.6).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float *__restrict__ scratch, int rows, int slots, int chains, T *__restrict__ out,
                                                          float *__restrict__ lse)
@@ -141,12 +141,14 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, const float
 }
 
 // The form of a launch, from what the host knows: rows, sequences and a bound on their lengths, not the lengths.
-//   * bf16, more than 16 rows to a head of keys of an average sequence: wide.  24 sequences of 1 to 8192 tokens, 32 heads, 8 of keys, d = 128: 2 drafted tokens (8 rows)
+//   * bf16, more than 16 rows to a head of keys of an average sequence: wide, all sequences of the call (400 single tokens behind 1000 and a piece of 1000 behind 8000 are not: 1683 us in one call, 313 and
+//     174 in two).  24 sequences of 1 to 8192 tokens, 32 heads, 8 of keys, d = 128: 2 drafted tokens (8 rows)
 //     37.7 us, narrow 33.6; 4 39.8 and 35.3; 8 37.3 and 49.5; 32 53 and 93; 48 sequences of 2048 to 6500 with 64: 268 and 1736.  Float is always narrow.
 //   * Parts: as many as are resident at once (wide: two workgroups a compute unit, or at d = 64 three, see tree_part), of 384 keys at least.  One sequence of 30,000 tokens, 16 drafted: 39.5 us, with half
 //     as many again 52; d = 64, 24 sequences with 8: 17.7, parts of 512 keys 18.7, of 768 21, of 1024 24.
-//   * Lengths up to 512, or many tiles of up to 64 sequences (which then start with the longest): a tile each and no joining launch.  48 x 64 drafted tokens, 768 tiles: 268,
-//     in parts 310.
+//   * Lengths up to 512, or many tiles of up to 64 sequences (which then start with the longest): a tile each and no joining launch.  48 x 64 drafted tokens over 2048 to 6500, 768 tiles: 287,
+//     in parts 338; a chain of 8000 behind 8000 1550 and 1662.  The host does not know the lengths, and there are some that would have it otherwise: 48 x 64 over 1 to 8192 137 and 84, 47 x 64 behind
+//     500 and one behind 100,000 2060 and 340.
 //   * Counted in front from 257 sequences on.  Of one token, 8 heads of keys, 20 to 700 tokens: 192 sequences 55.7 us without that launch and 59.0 with it, 256 70.0 and 71.1, 320 89.2 and 84.3,
 //     2048 1365 and 436.  (Where no tile is cut, sequences past the 64th are found among their starts, and nothing is counted: 65 21.6 -> 16.9.)
 constexpr int kListed = 256;
